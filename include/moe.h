@@ -206,6 +206,150 @@ moe_status moe_prefill_residual(moe_layer_t layer, int32_t n_tokens,
 moe_status moe_rmsnorm(const float* h, void* x, int32_t n_tokens, int32_t d_model,
                        float eps, void* stream);
 
+/* Number formats of 16 bits that the routing and layer norm entry points
+ * below take; the layer itself runs on MOE_F16. */
+enum { MOE_F16 = 0, MOE_BF16 = 1 };
+
+/* ---- Layer norm --------------------------------------------------------
+ * The norm of models whose MoE layers are fed by a layer norm instead of
+ * the RMSNorm above:
+ *   n[t] = (h[t] - mean(h[t])) / sqrt(var(h[t]) + eps),  x = n * gain + bias
+ * with the mean and the (biased) variance of the row in fp32.
+ *  h     device fp32 [n_tokens, d_model] (the residual stream)
+ *  gain  device fp32 [d_model] or NULL (1);  bias  likewise or NULL (0)
+ *  x     device, `type` [n_tokens, d_model] (output, overwritten)
+ *  n_tokens >= 1; d_model a positive multiple of 64, <= 16384; eps >= 0.
+ * Needs no handle; pointers 16-byte aligned; works on the current device. */
+moe_status moe_layernorm(const float* h, const float* gain, const float* bias, void* x,
+                         int32_t type, int32_t n_tokens, int32_t d_model, float eps,
+                         void* stream);
+
+/* Bytes of the workspace of moe_layernorm_backward: the column sums of its
+ * blocks.  0 < *bytes, a multiple of 256. */
+moe_status moe_layernorm_workspace(int32_t n_tokens, int32_t d_model, int64_t* bytes);
+
+/* Backward pass of moe_layernorm.  With a = d_x * gain:
+ *   d_h    = (a - mean(a) - n * mean(a * n)) / sqrt(var(h) + eps)
+ *   d_gain = sum_t d_x * n,   d_bias = sum_t d_x
+ *  d_x     device, `type` [n_tokens, d_model]: the gradient of x
+ *  h, gain, eps as in the forward call (the row statistics are formed again)
+ *  d_h     device fp32 [n_tokens, d_model]: overwritten, or with accumulate
+ *          != 0 added to (the residual branch's gradient is already there)
+ *  d_gain, d_bias  device fp32 [d_model] or NULL: overwritten
+ *  workspace  device, at least moe_layernorm_workspace bytes, 16-byte
+ *          aligned; may be NULL when d_gain and d_bias are.  It holds nothing
+ *          between calls; calls that overlap need one each.
+ * Sums run in a fixed order: the same call gives the same bits. */
+moe_status moe_layernorm_backward(const void* d_x, int32_t type, const float* h,
+                                  const float* gain, float eps, int32_t n_tokens,
+                                  int32_t d_model, float* d_h, int32_t accumulate,
+                                  float* d_gain, float* d_bias, void* workspace, void* stream);
+
+/* ---- Routing rules ------------------------------------------------------
+ * The gate of Eq. 1 for models that do not route by a softmax over the top-k
+ * logits alone.  Per token, with logits l = x Wg^T over all E experts:
+ *   score  s_e = sigmoid(l_e), or the softmax of l over the E experts
+ *   key    s_e + bias_e where there is a bias (it steers the balance of the
+ *          experts and enters nothing but the selection), else l_e (the order
+ *          of the scores)
+ *   groups the experts form n_groups groups of consecutive ones.  A group
+ *          counts the sum of its group_best (1 or 2) largest keys - scores,
+ *          where there is no bias; the top_groups groups that count most stay
+ *   top-k  the top_k largest keys of the experts in those groups, slot 0 the
+ *          largest; exact ties of keys or groups go to the lower index
+ *   weight scale * s_e, with renormalize divided by the sum of the selected s
+ * An expert whose logit or bias is not finite (a masked expert: bias -inf)
+ * is never selected, and one whose logit is not finite has score 0.  If
+ * fewer than top_k experts are left, the last slots hold index -1 and weight
+ * 0.  Selection goes by the logits' sums in 64 bits, so it does not depend
+ * on how many tokens a call has or how its sums are split. */
+typedef struct moe_router* moe_router_t;
+
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+enum { MOE_ROUTER_BACKWARD = 1 };  /* flag: the handle can run the backward pass */
+
+/*  d_model     positive multiple of 64, <= 16384
+ *  n_experts   1..512;  top_k 1..min(16, experts that top_groups groups hold)
+ *  max_tokens  largest n_tokens of any call (sizes the workspace); 1..65536
+ *  type        MOE_F16 or MOE_BF16: the type of x, w_router and d_x
+ *  score       MOE_SCORE_*
+ *  n_groups    1..64, a divisor of n_experts;  top_groups 1..n_groups
+ *  group_best  1 or 2 (a group of one expert counts that one)
+ *  renormalize 0 or 1;  scale finite, > 0
+ *  flags       MOE_ROUTER_BACKWARD or 0 */
+typedef struct {
+    int32_t d_model;
+    int32_t n_experts;
+    int32_t top_k;
+    int32_t max_tokens;
+    int32_t type;
+    int32_t score;
+    int32_t n_groups;
+    int32_t top_groups;
+    int32_t group_best;
+    int32_t renormalize;
+    float scale;
+    uint32_t flags;
+} moe_router_desc;
+
+/* Create a router.
+ *  w_router  device, `type` [n_experts, d_model], 16-byte aligned
+ *  bias      device fp32 [n_experts], 4-byte aligned, or NULL
+ * Both are borrowed: they must stay valid for the life of the handle, and
+ * may be updated in place, in stream order, between calls (training).
+ * Allocates the workspace on the current device.  One handle must not be
+ * used from two streams concurrently.  *out receives the handle. */
+moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, const float* bias,
+                           moe_router_t* out);
+
+/* Route 1 <= n_tokens <= max_tokens tokens.
+ *  x             device, `type` [n_tokens, d_model], 16-byte aligned
+ *  topk_idx      device int32 [n_tokens, top_k]
+ *  topk_w        device fp32 [n_tokens, top_k]
+ *  logits        device fp32 [n_tokens, n_experts] or NULL (the backward
+ *                pass takes them)
+ *  expert_count  device int32 [n_experts] or NULL: how many of the call's
+ *                slots selected each expert (overwritten) */
+moe_status moe_route(moe_router_t router, int32_t n_tokens, const void* x, int32_t* topk_idx,
+                     float* topk_w, float* logits, int32_t* expert_count, void* stream);
+
+/* Backward pass of moe_route, for handles with MOE_ROUTER_BACKWARD: from the
+ * gradients of topk_w and of the logits to those of x and w_router (the
+ * selection itself, and so the bias, has none).
+ *  x, logits, topk_idx  as passed to and written by moe_route; a slot whose
+ *            index is outside [0, n_experts), or whose logit is not finite,
+ *            counts nothing, and equal indices of a token add up
+ *  d_topk_w  device fp32 [n_tokens, top_k]
+ *  d_logits  device fp32 [n_tokens, n_experts] or NULL: the gradient of
+ *            losses on the logits themselves (balance, magnitude)
+ *  d_x       device, `type` [n_tokens, d_model] or NULL: overwritten
+ *  d_w_router  device fp32 [n_experts, d_model] or NULL: overwritten
+ * Pointers 16-byte aligned (topk_idx and d_topk_w 4-byte).  Sums run in a
+ * fixed order: the same call gives the same bits. */
+moe_status moe_route_backward(moe_router_t router, int32_t n_tokens, const void* x,
+                              const float* logits, const int32_t* topk_idx,
+                              const float* d_topk_w, const float* d_logits, void* d_x,
+                              float* d_w_router, void* stream);
+
+/* Free the router and its workspace (synchronises the device first).  Fails
+ * with MOE_ESTATE, freeing nothing, while layers route by it. */
+moe_status moe_router_destroy(moe_router_t router);
+
+/* Route the layer's steps by `router` instead of the layer's own gate (NULL:
+ * the layer's own gate again).  From the next call on, every decode and
+ * prefill entry point of the layer, the allocation-free one among them,
+ * takes its experts and gate values from the router; topk_idx and topk_w
+ * report them.  The Eq. 2 rule ranks a token's slots by gate value (ties:
+ * lower slot) and sums the values normalised over the selected experts; the
+ * expert of the largest one runs at full precision.  A slot without an
+ * expert is reported as index -1 and MOE_PREC_SKIP.
+ *  - The router must be of type MOE_F16, with the layer's d_model, n_experts
+ *    and top_k, at least its max_tokens, and on its device (else MOE_EINVAL).
+ *  - It must outlive its use by the layer; one router may serve several
+ *    layers whose calls do not overlap (its workspace is one).
+ *  - Not while a call of the layer is being enqueued by another thread. */
+moe_status moe_layer_set_router(moe_layer_t layer, moe_router_t router);
+
 /* Copy an expert's quantised copy out (for inspection and parity).
  *  matrix  0 = W1, 1 = W3, 2 = W2;  bits 8, 4 or 2 (the copy must exist)
  *  codes   device u8 [rows, cols*bits/8];  scales device fp16 [rows, cols/32]

@@ -17,6 +17,9 @@ MOE_OK, MOE_EINVAL, MOE_ENOMEM, MOE_EHIP, MOE_ESTATE, MOE_EUNSUPPORTED = 0, -1, 
 TAG_FP16, TAG_INT4, TAG_INT2, TAG_MISS_INT4, TAG_MISS_INT2 = 0, 1, 2, 3, 4
 TAG_INT8, TAG_MISS_INT8_INT2 = 5, 6  # int8 models: int8 high copy, int2 low copy
 PREC_HIGH, PREC_LOW, PREC_SKIP = 0, 1, 2
+MOE_F16, MOE_BF16 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+MOE_ROUTER_BACKWARD = 1
 
 EXPORTED = (
     "moe_layer_init", "moe_set_expert_precision", "moe_decode_step",
@@ -33,6 +36,9 @@ EXPORTED = (
     "moe_store_create", "moe_store_sizes", "moe_store_put", "moe_store_load",
     "moe_store_destroy", "moe_layer_bind_expert", "moe_rmsnorm",
     "moe_decode_step_noalloc",
+    "moe_layernorm", "moe_layernorm_workspace", "moe_layernorm_backward",
+    "moe_router_init", "moe_route", "moe_route_backward", "moe_router_destroy",
+    "moe_layer_set_router",
 )
 
 
@@ -49,6 +55,17 @@ class LayerDesc(ctypes.Structure):
         ("group_size", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
         ("t1", ctypes.c_float), ("t2", ctypes.c_float),
         ("rms_eps", ctypes.c_float), ("flags", ctypes.c_uint32),
+    ]
+
+
+class RouterDesc(ctypes.Structure):
+    _fields_ = [
+        ("d_model", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+        ("top_k", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+        ("type", ctypes.c_int32), ("score", ctypes.c_int32),
+        ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+        ("group_best", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("flags", ctypes.c_uint32),
     ]
 
 
@@ -123,6 +140,15 @@ def lib() -> ctypes.CDLL:
     L.moe_predict.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp]
     L.moe_predictor_destroy.argtypes = [vp]
     L.moe_rmsnorm.argtypes = [vp, vp, i32, i32, ctypes.c_float, vp]
+    L.moe_layernorm.argtypes = [vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, vp]
+    L.moe_layernorm_workspace.argtypes = [i32, i32, ctypes.POINTER(i64)]
+    L.moe_layernorm_backward.argtypes = [vp, i32, vp, vp, ctypes.c_float, i32, i32, vp, i32, vp,
+                                         vp, vp, vp]
+    L.moe_router_init.argtypes = [ctypes.POINTER(RouterDesc), vp, vp, ctypes.POINTER(vp)]
+    L.moe_route.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
+    L.moe_route_backward.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.moe_router_destroy.argtypes = [vp]
+    L.moe_layer_set_router.argtypes = [vp, vp]
     L.moe_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
         if name != "moe_last_error":
@@ -204,6 +230,133 @@ def rmsnorm(h, x, eps: float = 1e-5, stream=None):
     T, d = h.shape
     _check(lib().moe_rmsnorm(_addr(h, torch.float32, (T, d), "h"),
                              _addr(x, torch.float16, (T, d), "x"), T, d, eps, _stream(stream)))
+
+
+def _type16(dtype, name):
+    """MOE_F16 / MOE_BF16 of a torch dtype."""
+    torch = _th()
+    if dtype is torch.float16:
+        return MOE_F16
+    if dtype is torch.bfloat16:
+        return MOE_BF16
+    raise ValueError(f"{name} must be torch.float16 or torch.bfloat16, got {dtype}")
+
+
+def _rows(t, dtype, name):
+    """Shape (T, d) of a two-dimensional tensor argument."""
+    torch = _th()
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional device tensor")
+    return t.shape
+
+
+def layernorm(h, x, gain=None, bias=None, eps: float = 1e-5, stream=None):
+    """x = layer norm of h, row by row: h fp32 [T, d], x fp16 or bf16 [T, d],
+    gain / bias fp32 [d] or None."""
+    torch = _th()
+    T, d = _rows(h, torch.float32, "h")
+    _rows(x, None, "x")
+    _check(lib().moe_layernorm(
+        _addr(h, torch.float32, (T, d), "h"), _addr(gain, torch.float32, (d,), "gain"),
+        _addr(bias, torch.float32, (d,), "bias"), _addr(x, x.dtype, (T, d), "x"),
+        _type16(x.dtype, "x"), T, d, eps, _stream(stream)))
+
+
+def layernorm_workspace(n_tokens: int, d_model: int) -> int:
+    """Bytes of the workspace of layernorm_backward."""
+    n = ctypes.c_int64()
+    _check(lib().moe_layernorm_workspace(n_tokens, d_model, ctypes.byref(n)))
+    return n.value
+
+
+def layernorm_backward(d_x, h, d_h, gain=None, d_gain=None, d_bias=None, eps: float = 1e-5,
+                       accumulate: bool = False, workspace=None, stream=None):
+    """Gradients of layernorm from d_x (fp16 or bf16 [T, d]): d_h fp32 [T, d]
+    (with accumulate added to), d_gain / d_bias fp32 [d] or None.  workspace:
+    uint8 of layernorm_workspace(T, d) bytes; without one it is allocated on
+    the current stream, which `stream` then has to be (None)."""
+    torch = _th()
+    T, d = _rows(h, torch.float32, "h")
+    _rows(d_x, None, "d_x")
+    if workspace is None and (d_gain is not None or d_bias is not None):
+        if stream is not None:
+            raise ValueError("a call on a stream of its own needs a workspace")
+        workspace = torch.empty(layernorm_workspace(T, d), dtype=torch.uint8, device=h.device)
+    ws = None
+    if workspace is not None:
+        if workspace.numel() < layernorm_workspace(T, d):
+            raise ValueError(f"workspace must hold {layernorm_workspace(T, d)} bytes")
+        ws = _addr(workspace, torch.uint8, workspace.shape, "workspace")
+    _check(lib().moe_layernorm_backward(
+        _addr(d_x, d_x.dtype, (T, d), "d_x"), _type16(d_x.dtype, "d_x"),
+        _addr(h, torch.float32, (T, d), "h"), _addr(gain, torch.float32, (d,), "gain"), eps, T, d,
+        _addr(d_h, torch.float32, (T, d), "d_h"), 1 if accumulate else 0,
+        _addr(d_gain, torch.float32, (d,), "d_gain"), _addr(d_bias, torch.float32, (d,), "d_bias"),
+        ws, _stream(stream)))
+
+
+class MoeRouter:
+    """A routing rule over a borrowed gate w_router [E, d] (fp16 or bf16) and an
+    optional borrowed balance bias fp32 [E]; see moe_router_init.  Both may be
+    updated in place between calls.  backward: the handle can run backward()."""
+
+    def __init__(self, d_model, n_experts, top_k, max_tokens, w_router, bias=None, dtype=None,
+                 score=SCORE_SOFTMAX, n_groups=1, top_groups=1, group_best=1, renormalize=True,
+                 scale=1.0, backward=False):
+        torch = _th()
+        dtype = torch.float16 if dtype is None else dtype
+        self.d, self.E, self.K, self.max_tokens = d_model, n_experts, top_k, max_tokens
+        self.dtype = dtype
+        self._h = None
+        desc = RouterDesc(d_model, n_experts, top_k, max_tokens, _type16(dtype, "dtype"), score,
+                          n_groups, top_groups, group_best, 1 if renormalize else 0, scale,
+                          MOE_ROUTER_BACKWARD if backward else 0)
+        h = ctypes.c_void_p()
+        _check(lib().moe_router_init(
+            ctypes.byref(desc), _ptr(w_router, dtype, (n_experts, d_model), "w_router"),
+            _ptr(bias, torch.float32, (n_experts,), "bias"), ctypes.byref(h)))
+        self._keep = (w_router, bias)
+        self._h = h
+
+    def route(self, x, topk_idx, topk_w, logits=None, expert_count=None, stream=None):
+        """x [T, d]; topk_idx int32, topk_w fp32 [T, K]; logits fp32 [T, E] or
+        None; expert_count int32 [E] or None."""
+        torch = _th()
+        T, _ = _rows(x, self.dtype, "x")
+        _check(lib().moe_route(
+            self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
+            _addr(topk_idx, torch.int32, (T, self.K), "topk_idx"),
+            _addr(topk_w, torch.float32, (T, self.K), "topk_w"),
+            _addr(logits, torch.float32, (T, self.E), "logits"),
+            _addr(expert_count, torch.int32, (self.E,), "expert_count"), _stream(stream)))
+
+    def backward(self, x, logits, topk_idx, d_topk_w, d_x=None, d_w_router=None, d_logits=None,
+                 stream=None):
+        """From d_topk_w fp32 [T, K] (and d_logits fp32 [T, E] or None) to d_x
+        [T, d] of x's type and d_w_router fp32 [E, d] (each or None)."""
+        torch = _th()
+        T, _ = _rows(x, self.dtype, "x")
+        _check(lib().moe_route_backward(
+            self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
+            _addr(logits, torch.float32, (T, self.E), "logits"),
+            _addr(topk_idx, torch.int32, (T, self.K), "topk_idx"),
+            _addr(d_topk_w, torch.float32, (T, self.K), "d_topk_w"),
+            _addr(d_logits, torch.float32, (T, self.E), "d_logits"),
+            _addr(d_x, self.dtype, (T, self.d), "d_x"),
+            _addr(d_w_router, torch.float32, (self.E, self.d), "d_w_router"), _stream(stream)))
+
+    def destroy(self):
+        if self._h is not None and self._h.value:
+            _check(lib().moe_router_destroy(self._h))
+        self._h = None
+        self._keep = None
+
+    def __del__(self):
+        try:
+            if getattr(self, "_h", None) is not None and self._h.value:
+                lib().moe_router_destroy(self._h)
+        except Exception:
+            pass
 
 
 class MoeLayer:
@@ -327,6 +480,12 @@ class MoeLayer:
                                            arr(q, torch.uint8, "q"), arr(s, torch.float16, "s"),
                                            low_bits, _stream(stream)))
 
+    def set_router(self, router):
+        """Route this layer's steps by `router` (a MoeRouter, kept alive by the
+        layer), or by its own gate again (None)."""
+        _check(lib().moe_layer_set_router(self._h, None if router is None else router._h))
+        self._router = router
+
     def enable_timing(self, on: bool = True):
         _check(lib().moe_layer_enable_timing(self._h, 1 if on else 0))
 
@@ -350,6 +509,7 @@ class MoeLayer:
         self._h = None
         self._keep = None
         self._ws_owner = None
+        self._router = None
 
     def __del__(self):
         try:

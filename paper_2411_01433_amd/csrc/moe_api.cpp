@@ -81,6 +81,8 @@ struct moe_layer {
   // and how many layers run on this one's
   moe_layer* ws_owner = nullptr;
   int ws_sharers = 0;
+  // the router the layer's steps go by, or null: the layer's own gate
+  moe_router* router = nullptr;
   // stage timing (measurement only): 5 events per recorded call
   bool timing = false;
   std::vector<hipEvent_t> ev_pool;
@@ -178,6 +180,27 @@ hipError_t mark(moe_layer* l, int slot, hipStream_t s) {
   return hipEventRecord(l->ev_pool[at], s);
 }
 
+// Routing by the layer's router: its kernels write the workspace's routing
+// arrays with the Eq. 2 rule's precisions, then the work list is built.
+moe_status route_by_router(moe_layer* l, const RouteParams& rp, const RouteOut& o,
+                           const Workspace& ws, hipStream_t s) {
+  RouterUse u;
+  if (!router_use(l->router, &u)) return fail(MOE_ESTATE, "the layer's router was destroyed");
+  RouterOut ro;
+  ro.idx = o.idx;
+  ro.w = o.w;
+  ro.prec = o.prec;
+  ro.user_idx = o.user_idx;
+  ro.user_w = o.user_w;
+  ro.user_prec = o.user_prec;
+  ro.table = rp.table;
+  ro.t1 = rp.t1;
+  ro.t2 = rp.t2;
+  HIP_TRY(launch_router(u.p, rp.T, rp.x, ro, s), "router kernel launch");
+  HIP_TRY(launch_worklist(rp, o, ws.wl, ws.perm, ws.pos, s), "work list launch");
+  return MOE_OK;
+}
+
 // Which decode kernels a step takes.  The dot2 kernels stream each expert
 // copy once per two tokens of its group, the matrix-core kernels once per
 // 16; with at most about one token per expert copy (T*K <= E) the dot2
@@ -225,7 +248,7 @@ moe_status decode_launch(moe_layer* l, const Workspace& ws, int32_t T, const voi
   HIP_TRY(mark(l, 0, s), "timing event");
   RouteParams rp = route_params(l, T, x);
   if (prenorm) {
-    if (route_decode_fuses_norm(T, d)) {
+    if (!l->router && route_decode_fuses_norm(T, d)) {
       rp.h_res = h_res;
       rp.x_out = static_cast<f16*>(const_cast<void*>(x));
       rp.eps = l->desc.rms_eps;
@@ -234,8 +257,13 @@ moe_status decode_launch(moe_layer* l, const Workspace& ws, int32_t T, const voi
                              l->desc.rms_eps, s), "rmsnorm kernel launch");
     }
   }
-  HIP_TRY(launch_route_decode(rp, route_out(ws, idx, w, prec), ws.wl, ws.perm, ws.pos, s),
-          "route kernel launch");
+  const RouteOut ro = route_out(ws, idx, w, prec);
+  if (l->router) {
+    moe_status st = route_by_router(l, rp, ro, ws, s);
+    if (st != MOE_OK) return st;
+  } else {
+    HIP_TRY(launch_route_decode(rp, ro, ws.wl, ws.perm, ws.pos, s), "route kernel launch");
+  }
   HIP_TRY(mark(l, 1, s), "timing event");
   const int E = l->desc.n_experts;
   if (decode_on_matrix_cores(T, K, E)) {
@@ -296,8 +324,13 @@ moe_status prefill_impl(moe_layer* l, int32_t T, const void* x, float* y,
   const int mg = max_groups_of(l, T);
   HIP_TRY(mark(l, 0, s), "timing event");
   const Workspace& ws = l->ws;
-  HIP_TRY(launch_route_prefill(route_params(l, T, x), route_out(ws, idx, w, prec),
-                               ws.wl, ws.perm, ws.pos, s), "route kernel launch");
+  const RouteParams rp = route_params(l, T, x);
+  const RouteOut ro = route_out(ws, idx, w, prec);
+  if (l->router) {
+    if ((st = route_by_router(l, rp, ro, ws, s)) != MOE_OK) return st;
+  } else {
+    HIP_TRY(launch_route_prefill(rp, ro, ws.wl, ws.perm, ws.pos, s), "route kernel launch");
+  }
   HIP_TRY(mark(l, 1, s), "timing event");
   HIP_TRY(launch_prefill_up(l->d_table, ws.wl, ws.perm, static_cast<const f16*>(x), ws.h, T, d,
                             f, l->desc.n_experts, K, mg, s), "prefill up launch");
@@ -313,6 +346,7 @@ moe_status prefill_impl(moe_layer* l, int32_t T, const void* x, float* y,
 }
 
 void free_layer(moe_layer* l) {
+  if (l->router) (void)router_hold(l->router, -1);
   for (hipEvent_t e : l->ev_pool) (void)hipEventDestroy(e);
   for (void* p : l->owned) (void)hipFree(p);
   if (l->arena) (void)hipFree(l->arena);
@@ -805,6 +839,26 @@ moe_status moe_rmsnorm(const float* h, void* x, int32_t n_tokens, int32_t d_mode
   if (!aligned16(h) || !aligned16(x)) return fail(MOE_EINVAL, "h and x must be 16-byte aligned");
   HIP_TRY(launch_rmsnorm(h, static_cast<f16*>(x), n_tokens, d_model, eps,
                          static_cast<hipStream_t>(stream)), "rmsnorm kernel launch");
+  return MOE_OK;
+}
+
+moe_status moe_layer_set_router(moe_layer_t l, moe_router_t router) {
+  g_err.clear();
+  if (!l || !live(l)) return fail(MOE_ESTATE, "invalid or destroyed layer handle");
+  if (router) {
+    RouterUse u;
+    if (!router_use(router, &u)) return fail(MOE_ESTATE, "invalid or destroyed router handle");
+    const moe_layer_desc& a = l->desc;
+    if (u.p.type != TYPE_F16) return fail(MOE_EINVAL, "the layer needs a router of type MOE_F16");
+    if (u.p.d != a.d_model || u.p.E != a.n_experts || u.p.K != a.top_k)
+      return fail(MOE_EINVAL, "layer and router need equal d_model, n_experts and top_k");
+    if (u.max_tokens < a.max_tokens)
+      return fail(MOE_EINVAL, "the router takes %d tokens, the layer up to %d", u.max_tokens, a.max_tokens);
+    if (u.device != l->device) return fail(MOE_EINVAL, "layer and router live on different devices");
+    if (!router_hold(router, 1)) return fail(MOE_ESTATE, "invalid or destroyed router handle");
+  }
+  if (l->router) (void)router_hold(l->router, -1);
+  l->router = router;
   return MOE_OK;
 }
 

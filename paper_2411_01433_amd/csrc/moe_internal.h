@@ -5,9 +5,12 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+struct moe_router;
+
 namespace moe {
 
 typedef _Float16 f16;
+typedef __bf16 bf16;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -252,6 +255,49 @@ struct PredictParams {
   int32_t T, d, E, K, p;
 };
 
+// ---- routing rules and layer norm (router.hip, router_grad.hip, norm.hip) --
+constexpr int kRouterMaxExperts = 512;
+constexpr int kRouterMaxTopK = 16;
+constexpr int kRouterMaxGroups = 64;
+
+enum { TYPE_F16 = 0, TYPE_BF16 = 1 };
+enum { SCORE_SOFTMAX = 0, SCORE_SIGMOID = 1 };
+
+// A router's rule, its borrowed weights and its workspace.
+struct RouterParams {
+  const void* wg;          // [E, d] of `type`
+  const float* bias;       // [E] or null
+  int32_t d, E, K, type, score, n_groups, top_groups, group_best, renorm;
+  float scale;
+  // workspace, sized for max_tokens
+  double* logits;          // [T, E]
+  float* d_logits;         // [T, E], routers with a backward pass
+};
+
+// Outputs of one routing; what is null is not written.
+struct RouterOut {
+  int32_t* idx = nullptr;        // [T, K]
+  float* w = nullptr;            // [T, K]
+  float* logits = nullptr;       // [T, E]
+  int32_t* count = nullptr;      // [E]
+  // for a layer: the caller's copies and the Eq. 2 rule's precisions
+  int32_t* user_idx = nullptr;
+  float* user_w = nullptr;
+  int8_t* user_prec = nullptr;
+  int8_t* prec = nullptr;        // [T, K]
+  const ExpertEntry* table = nullptr;
+  float t1 = 0.0f, t2 = 0.0f;
+};
+
+// A live router as the layer takes it: its parameters, and the count of
+// layers that route by it (router.cpp).
+struct RouterUse {
+  RouterParams p;
+  int32_t max_tokens, device;
+};
+bool router_use(struct ::moe_router* r, RouterUse* out);
+bool router_hold(struct ::moe_router* r, int by);  // by: +1 or -1; false if not live
+
 // Static scratch of the allocation-free decode step (noalloc.hip): its size,
 // and its device address on `device` (looked up on the first call, which
 // must find `device` current; later calls return the kept address).
@@ -270,6 +316,19 @@ hipError_t launch_route_decode(const RouteParams& p, RouteOut o, WorkList* wl,
 bool route_decode_fuses_norm(int T, int d);
 hipError_t launch_route_prefill(const RouteParams& p, RouteOut o, WorkList* wl,
                                 int32_t* perm, int32_t* pos, hipStream_t s);
+hipError_t launch_worklist(const RouteParams& p, RouteOut o, WorkList* wl, int32_t* perm,
+                           int32_t* pos, hipStream_t s);
+hipError_t launch_router(const RouterParams& p, int T, const void* x, const RouterOut& o,
+                         hipStream_t s);
+hipError_t launch_router_backward(const RouterParams& p, int T, const void* x,
+                                  const float* logits, const int32_t* idx, const float* dw,
+                                  const float* dl, void* dx, float* dwg, hipStream_t s);
+hipError_t launch_layernorm(const float* h, const float* gain, const float* bias, void* x,
+                            int type, int T, int d, float eps, hipStream_t s);
+size_t layernorm_workspace(int T, int d);
+hipError_t launch_layernorm_backward(const void* dx, int type, const float* h, const float* gain,
+                                     float eps, int T, int d, float* dh, bool accumulate,
+                                     float* d_gain, float* d_bias, void* ws, hipStream_t s);
 hipError_t launch_decode_up(const ExpertEntry* table, const WorkList* wl,
                             const int32_t* perm, const f16* x, f16* h,
                             int T, int d, int f, int K, int max_groups,

@@ -1,0 +1,247 @@
+// Layer norm of the residual stream and its backward pass.
+//
+//   n = (h - mean h) r,  r = 1 / sqrt(mean (h - mean h)^2 + eps)
+//   x = n gain + bias
+//   a = d_x gain;  d_h = r (a - mean a - n mean(a n))
+//   d_gain = sum_t d_x n;  d_bias = sum_t d_x
+//
+// One block per row, which it holds in registers: h is read once.  The
+// variance is the mean square of the centred values (no difference of large
+// sums).  All of it in fp32; x and d_x are of 16 bits.
+#include "moe_internal.h"
+
+namespace moe {
+
+namespace {
+
+constexpr int kPieces = 4;  // float4 pieces of a row per thread
+
+// Threads of a row's block: d <= 16 columns per thread.
+__host__ __device__ inline int row_threads(int d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : 1024; }
+
+template <class T16>
+__device__ inline u32x2 pack4(f32x4 v) {
+  typedef T16 x2 __attribute__((ext_vector_type(2)));
+  const x2 lo = {(T16)v.x, (T16)v.y}, hi = {(T16)v.z, (T16)v.w};
+  return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+template <class T16>
+__device__ inline f32x4 unpack4(u32x2 u) {
+  typedef T16 x2 __attribute__((ext_vector_type(2)));
+  const uint32_t a = u.x, b = u.y;
+  const x2 lo = __builtin_bit_cast(x2, a), hi = __builtin_bit_cast(x2, b);
+  return f32x4{(float)lo.x, (float)lo.y, (float)hi.x, (float)hi.y};
+}
+
+// Sums of N values over the block's NT threads, in every thread, in a fixed
+// order.  `red`: N * NT / 64 floats; the caller alternates two of them.
+template <int NT, int N>
+__device__ inline void block_sums(float (&v)[N], float* red) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum_dpp(v[i]);
+  if constexpr (NT > 64) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[i * (NT / 64) + wave] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NT / 64; ++w) v[i] += red[i * (NT / 64) + w];
+    }
+  }
+}
+
+__device__ inline float sum4(f32x4 v) { return (v.x + v.y) + (v.z + v.w); }
+
+template <class T16, int NT>
+__global__ __launch_bounds__(NT) void layernorm_kernel(const float* __restrict__ h,
+                                                       const float* __restrict__ gain,
+                                                       const float* __restrict__ bias,
+                                                       T16* __restrict__ x, int d, float eps) {
+  __shared__ float red[2][NT / 64];
+  const int n4 = d >> 2;
+  const f32x4* hr = reinterpret_cast<const f32x4*>(h + (int64_t)blockIdx.x * d);
+  f32x4 v[kPieces];
+  float s[1] = {0.0f};
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int q = threadIdx.x + i * NT;
+    v[i] = q < n4 ? hr[q] : f32x4{0, 0, 0, 0};
+    s[0] += sum4(v[i]);
+  }
+  block_sums<NT, 1>(s, red[0]);
+  const float mean = s[0] / (float)d;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+    if (threadIdx.x + i * NT < n4) {
+      v[i] -= mean;
+      s[0] += sum4(v[i] * v[i]);
+    }
+  block_sums<NT, 1>(s, red[1]);
+  const float r = 1.0f / sqrtf(s[0] / (float)d + eps);
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int q = threadIdx.x + i * NT;
+    if (q < n4) {
+      f32x4 o = v[i] * r;
+      if (gain) o *= reinterpret_cast<const f32x4*>(gain)[q];
+      if (bias) o += reinterpret_cast<const f32x4*>(bias)[q];
+      *reinterpret_cast<u32x2*>(x + (int64_t)blockIdx.x * d + 4 * q) = pack4<T16>(o);
+    }
+  }
+}
+
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ...; the block's column sums of
+// d_x n and d_x go to part[block][2][d].
+template <class T16, int NT>
+__global__ __launch_bounds__(NT) void layernorm_backward_kernel(
+    const T16* __restrict__ dx, const float* __restrict__ h, const float* __restrict__ gain,
+    float* __restrict__ dh, float* __restrict__ part, int T, int d, float eps, int accumulate) {
+  __shared__ float red[2][3 * NT / 64];
+  const int n4 = d >> 2;
+  f32x4 dg[kPieces], db[kPieces], gn[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int q = threadIdx.x + i * NT;
+    dg[i] = db[i] = f32x4{0, 0, 0, 0};
+    gn[i] = gain && q < n4 ? reinterpret_cast<const f32x4*>(gain)[q] : f32x4{1, 1, 1, 1};
+  }
+  for (int t = blockIdx.x; t < T; t += gridDim.x) {
+    const f32x4* hr = reinterpret_cast<const f32x4*>(h + (int64_t)t * d);
+    const u32x2* xr = reinterpret_cast<const u32x2*>(dx + (int64_t)t * d);
+    f32x4 v[kPieces], a[kPieces];
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int q = threadIdx.x + i * NT;
+      v[i] = q < n4 ? hr[q] : f32x4{0, 0, 0, 0};
+      a[i] = q < n4 ? unpack4<T16>(xr[q]) : f32x4{0, 0, 0, 0};
+      s[0] += sum4(v[i]);
+    }
+    block_sums<NT, 1>(s, red[0]);
+    const float mean = s[0] / (float)d;
+    float m[3] = {0.0f, 0.0f, 0.0f};  // squares, a, a n (before the scale r)
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (threadIdx.x + i * NT < n4) {
+        v[i] -= mean;
+        const f32x4 g = a[i] * gn[i];
+        m[0] += sum4(v[i] * v[i]);
+        m[1] += sum4(g);
+        m[2] += sum4(g * v[i]);
+      }
+    block_sums<NT, 3>(m, red[1]);
+    const float r = 1.0f / sqrtf(m[0] / (float)d + eps);
+    const float ma = m[1] / (float)d, mn = m[2] * r / (float)d;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int q = threadIdx.x + i * NT;
+      if (q < n4) {
+        const f32x4 n = v[i] * r;
+        db[i] += a[i];
+        dg[i] += a[i] * n;
+        f32x4 o = r * (a[i] * gn[i] - ma - n * mn);
+        f32x4* to = reinterpret_cast<f32x4*>(dh + (int64_t)t * d) + q;
+        *to = accumulate ? *to + o : o;
+      }
+    }
+    if constexpr (NT > 64) __syncthreads();
+  }
+  if (part) {
+    f32x4* pr = reinterpret_cast<f32x4*>(part + (int64_t)blockIdx.x * 2 * d);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int q = threadIdx.x + i * NT;
+      if (q < n4) {
+        pr[q] = dg[i];
+        pr[n4 + q] = db[i];
+      }
+    }
+  }
+}
+
+// Column sums of part[n][2 d] into d_gain and d_bias: a block takes 16
+// pieces of four columns, 16 threads of it every 16th row.
+constexpr int kSumThreads = 256;
+__global__ __launch_bounds__(kSumThreads) void column_sums_kernel(const float* __restrict__ part,
+                                                                  int n, int d,
+                                                                  float* __restrict__ dg,
+                                                                  float* __restrict__ db) {
+  __shared__ f32x4 red[16][16];
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int q = blockIdx.x * 16 + c, n4 = d >> 2;
+  f32x4 s = {0, 0, 0, 0};
+  for (int b = g; b < n; b += 16) s += reinterpret_cast<const f32x4*>(part + (int64_t)b * 2 * d)[q];
+  red[g][c] = s;
+  __syncthreads();
+  if (g == 0) {
+    for (int i = 1; i < 16; ++i) s += red[i][c];
+    float* to = q < n4 ? dg : db;
+    if (to) reinterpret_cast<f32x4*>(to)[q < n4 ? q : q - n4] = s;
+  }
+}
+
+int backward_blocks(int T, int d) {
+  const int most = d <= 1024 ? 1024 : d <= 4096 ? 512 : 256;
+  return T < most ? T : most;
+}
+
+template <class T16>
+hipError_t norm_forward(const float* h, const float* gain, const float* bias, T16* x, int T, int d,
+                        float eps, hipStream_t s) {
+  switch (row_threads(d)) {
+    case 64: layernorm_kernel<T16, 64><<<T, 64, 0, s>>>(h, gain, bias, x, d, eps); break;
+    case 256: layernorm_kernel<T16, 256><<<T, 256, 0, s>>>(h, gain, bias, x, d, eps); break;
+    default: layernorm_kernel<T16, 1024><<<T, 1024, 0, s>>>(h, gain, bias, x, d, eps);
+  }
+  return hipGetLastError();
+}
+
+template <class T16>
+hipError_t norm_backward(const T16* dx, const float* h, const float* gain, float eps, int T, int d,
+                         float* dh, int acc, float* part, hipStream_t s) {
+  const int nb = backward_blocks(T, d);
+  switch (row_threads(d)) {
+    case 64:
+      layernorm_backward_kernel<T16, 64><<<nb, 64, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);
+      break;
+    case 256:
+      layernorm_backward_kernel<T16, 256><<<nb, 256, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);
+      break;
+    default:
+      layernorm_backward_kernel<T16, 1024><<<nb, 1024, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_layernorm(const float* h, const float* gain, const float* bias, void* x,
+                            int type, int T, int d, float eps, hipStream_t s) {
+  return type == TYPE_F16 ? norm_forward(h, gain, bias, static_cast<f16*>(x), T, d, eps, s)
+                          : norm_forward(h, gain, bias, static_cast<bf16*>(x), T, d, eps, s);
+}
+
+size_t layernorm_workspace(int T, int d) {
+  return ((size_t)backward_blocks(T, d) * 2 * d * sizeof(float) + 255) & ~(size_t)255;
+}
+
+hipError_t launch_layernorm_backward(const void* dx, int type, const float* h, const float* gain,
+                                     float eps, int T, int d, float* dh, bool accumulate,
+                                     float* d_gain, float* d_bias, void* ws, hipStream_t s) {
+  float* part = d_gain || d_bias ? static_cast<float*>(ws) : nullptr;
+  hipError_t e = type == TYPE_F16
+                     ? norm_backward(static_cast<const f16*>(dx), h, gain, eps, T, d, dh, accumulate, part, s)
+                     : norm_backward(static_cast<const bf16*>(dx), h, gain, eps, T, d, dh, accumulate, part, s);
+  if (e != hipSuccess || !part) return e;
+  column_sums_kernel<<<d / 32, kSumThreads, 0, s>>>(part, backward_blocks(T, d), d, d_gain, d_bias);
+  return hipGetLastError();
+}
+
+}  // namespace moe

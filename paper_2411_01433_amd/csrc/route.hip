@@ -505,13 +505,18 @@ hipError_t launch_route_tokens(const RouteParams& p, RouteOut o, WorkList* wl, i
   route_tokens_kernel<FIRST, TPB><<<(p.T + TPB - 1) / TPB, kRouteThreads, 0, s>>>(p, o);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  worklist_kernel<<<1, kRouteThreads, 0, s>>>(p, o, wl, perm, pos);
-  return hipGetLastError();
+  return launch_worklist(p, o, wl, perm, pos, s);
 }
 
 }  // namespace
 
 bool route_decode_fuses_norm(int T, int d) { return T <= kRouteSmallTokens && fast_gate(T, d); }
+
+hipError_t launch_worklist(const RouteParams& p, RouteOut o, WorkList* wl, int32_t* perm,
+                           int32_t* pos, hipStream_t s) {
+  worklist_kernel<<<1, kRouteThreads, 0, s>>>(p, o, wl, perm, pos);
+  return hipGetLastError();
+}
 
 hipError_t launch_route_decode(const RouteParams& p, RouteOut o, WorkList* wl,
                                int32_t* perm, int32_t* pos, hipStream_t s) {
