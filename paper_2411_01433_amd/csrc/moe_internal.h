@@ -270,7 +270,9 @@ struct RouterParams {
   int32_t d, E, K, type, score, n_groups, top_groups, group_best, renorm;
   float scale;
   // workspace, sized for max_tokens
-  double* logits;          // [T, E]
+  float* logits;           // [T, E], calls that do not ask for them
+  float* x_norm;           // [T] bounds of the rows' norms
+  float* w_norm;           // [E]
   float* d_logits;         // [T, E], routers with a backward pass
 };
 

@@ -150,7 +150,9 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
   auto al = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t rows = (size_t)desc->max_tokens * desc->n_experts;
   size_t off = 0;
-  const size_t o_lg = off; off += al(rows * sizeof(double));
+  const size_t o_lg = off; off += al(rows * sizeof(float));
+  const size_t o_xn = off; off += al(sizeof(float) * desc->max_tokens);
+  const size_t o_wn = off; off += al(sizeof(float) * desc->n_experts);
   const size_t o_dl = off; off += r->backward ? al(rows * sizeof(float)) : 0;
   he = hipMalloc(&r->arena, off);
   if (he != hipSuccess) {
@@ -158,7 +160,9 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
     return rfail(MOE_ENOMEM, "hipMalloc of %zu router bytes failed: %s", off, hipGetErrorString(he));
   }
   char* base = static_cast<char*>(r->arena);
-  p.logits = reinterpret_cast<double*>(base + o_lg);
+  p.logits = reinterpret_cast<float*>(base + o_lg);
+  p.x_norm = reinterpret_cast<float*>(base + o_xn);
+  p.w_norm = reinterpret_cast<float*>(base + o_wn);
   p.d_logits = r->backward ? reinterpret_cast<float*>(base + o_dl) : nullptr;
   {
     std::lock_guard<std::mutex> g(g_router_mu);

@@ -6,191 +6,709 @@
 //   top-k of the keys in the groups that count most, ties to the lower index
 //   w = scale s, or scale s / sum of the selected s
 //
-// Which of two near keys is larger decides what is selected, so logits, keys
-// and group scores are held in 64 bits.
+// Two kernels.  The logits are a matrix product on the matrix cores, in fp32
+// sums; a second kernel takes one wave per token for everything else.
+//
+// Which of two near keys is larger decides what is selected, and fp32 sums
+// differ in their last bits with the split of the sum.  So the first kernel
+// also gives the norms of the rows of x and Wg, whose product bounds the
+// error of a logit, and the second one carries a bound beside every key.
+// Where two keys (or groups) that decide something lie within their bounds -
+// a few tokens in a hundred - it sums the logits in question again in 64
+// bits and decides by those.
 #include "moe_internal.h"
 
 namespace moe {
 
 namespace {
 
+typedef f16 f16x8v __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Pointers that come in a struct would be loaded from as generic ones.
+template <class T>
+using Global = const __attribute__((address_space(1))) T*;
+template <class T>
+__device__ inline Global<T> global(const void* p) {
+  return (Global<T>)(const T*)p;
+}
+
+template <class T16> struct Vec;
+template <> struct Vec<f16> { typedef f16x8v x8; };
+template <> struct Vec<bf16> { typedef bf16x8 x8; };
+
+__device__ inline f32x4 mfma(f16x8v a, f16x8v b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// acc + the squares of a piece of a row
+__device__ inline float squares(f16x8v v, float acc) {
+  const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = u[i];
+    acc = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), __builtin_bit_cast(f16x2, w), acc, false);
+  }
+  return acc;
+}
+__device__ inline float squares(bf16x8 v, float acc) {
+  const u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = u[i];
+    acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, w), acc, false);
+  }
+  return acc;
+}
+__device__ inline uint32_t any_bits(u32x4 u) {
+  return (u.x | u.y) | (u.z | u.w);
+}
+
+// Bound of a row's norm from its sum of squares and the bits of its elements.
+// The squares of fp16 do not underflow in fp32; those of bf16 do below 1e-19,
+// and then count as the largest norm that can go with so small a sum.  A row
+// of zeros has norm 0, and its logits are exact.
+__device__ inline float norm_bound(float sq, uint32_t bits) {
+  if ((bits & 0x7FFF7FFFu) == 0) return 0.0f;
+  return fmaxf(sqrtf(sq) * 1.0001f, 4e-15f);
+}
+
+// A logit's error is at most this times the norms of its rows: the roundings
+// on a product's way.  A matrix product's step of 32 columns rounds its sum
+// once, to half a step of fp32: rows of one repeated number, whose roundings
+// all point the same way, come to 0.50 of 2^-23 per step (d 4096 and 16384)
+// and no input measured to more; counted are 0.75, and 0.5 for each join.
+__host__ __device__ inline float sum_error(int d, int waves) {
+  const int steps = 2 * ((d / 64 + waves - 1) / waves);
+  return (1.5f * steps + waves) * 0x1p-24f;
+}
+
+// Logits [T, E] of MT * 16 tokens and NT * 16 experts per block.  Every wave
+// takes its share of the columns for the whole tile, 64 columns (a line of
+// 128 bytes of each row) at a time, so that each byte is loaded once per
+// block and no wave waits for another; the waves' sums are joined in LDS in a
+// fixed order.  A piece is loaded into registers while the last one is
+// multiplied.
+//
+// What bounds it is the load path of a compute unit.  Loads in the layout
+// that the matrix products take put neighbouring lanes on different rows and
+// reach 15 bytes a cycle per unit, from L2 as from HBM; eight lanes along a
+// line reach 47 (256 units, 16-byte loads, 2 MiB that stay in L2).  So a
+// piece is loaded by lines, 8 rows an instruction, and turned through LDS of
+// the wave's own: 16-byte chunk k of a row r lies at slot k ^ (r & 7), where
+// neither the writes nor the products' reads conflict.
+// Rows past the end are read as the last one and not written.
+template <class T16, int MT, int NT, int NW>
+__global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, int T,
+                                                                const T16* __restrict__ x,
+                                                                float* __restrict__ lg,
+                                                                int32_t* __restrict__ count) {
+  typedef typename Vec<T16>::x8 x8;
+  constexpr int BM = MT * 16, BN = NT * 16, LD = BN + 4;
+  constexpr int LA = 2 * MT, LB = 2 * NT;           // loads of a piece: 8 rows each
+  constexpr int kPiece = (LA + LB) * 64;            // 16-byte slots of a piece
+  constexpr int kRed = NW * BM * LD / 4;            // ... of the waves' sums
+  __shared__ u32x4 lds[kRed > NW * kPiece ? kRed : NW * kPiece];
+  __shared__ float sq[NW][BM + BN];
+  __shared__ uint32_t nz[NW][BM + BN];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x * BM, e0 = blockIdx.y * BN;
+  const bool norm_x = blockIdx.y == 0, norm_w = blockIdx.x == 0;
+  if (count && blockIdx.x == 0 && blockIdx.y == 0)
+    for (int e = threadIdx.x; e < p.E; e += NW * 64) count[e] = 0;
+  // this lane's chunks as offsets in bytes from the block's first row (a tile
+  // has at most 128 rows of 32 KiB), so that loads take one uniform address
+  Global<char> xb = global<char>(x + (int64_t)t0 * p.d);
+  Global<char> wb = global<char>(static_cast<const T16*>(p.wg) + (int64_t)e0 * p.d);
+  uint32_t xo[LA], wo[LB];
+  const int r8 = lane >> 3, chunk = ((lane & 7) ^ r8) * 16;
+#pragma unroll
+  for (int j = 0; j < LA; ++j) xo[j] = (uint32_t)min(j * 8 + r8, T - 1 - t0) * (uint32_t)(p.d * 2) + chunk;
+#pragma unroll
+  for (int j = 0; j < LB; ++j) wo[j] = (uint32_t)min(j * 8 + r8, p.E - 1 - e0) * (uint32_t)(p.d * 2) + chunk;
+  f32x4 acc[MT][NT];
+  float sx[LA], sw[LB];
+  uint32_t zx[LA], zw[LB];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < LA; ++j) {
+    sx[j] = 0.0f;
+    zx[j] = 0;
+  }
+#pragma unroll
+  for (int j = 0; j < LB; ++j) {
+    sw[j] = 0.0f;
+    zw[j] = 0;
+  }
+  const int n = (p.d / 64 - wave + NW - 1) / NW;  // this wave's pieces
+  u32x4 a[LA], b[LB];
+  auto load = [&](int i) {
+    const int c = (wave + min(i, n - 1) * NW) * 128;  // (past the last: the last again)
+#pragma unroll
+    for (int j = 0; j < LA; ++j) a[j] = *(Global<u32x4>)(xb + c + xo[j]);
+#pragma unroll
+    for (int j = 0; j < LB; ++j) b[j] = *(Global<u32x4>)(wb + c + wo[j]);
+  };
+  u32x4* own = lds + wave * kPiece;
+  const int row = lane & 15, at0 = row * 8 + ((lane >> 4) ^ (row & 7)), at1 = at0 ^ 4;
+  if (n > 0) load(0);
+  for (int i = 0; i < n; ++i) {
+#pragma unroll
+    for (int j = 0; j < LA; ++j) own[j * 64 + lane] = a[j];
+#pragma unroll
+    for (int j = 0; j < LB; ++j) own[(LA + j) * 64 + lane] = b[j];
+    if (norm_x) {
+#pragma unroll
+      for (int j = 0; j < LA; ++j) {
+        sx[j] = squares(__builtin_bit_cast(x8, a[j]), sx[j]);
+        zx[j] |= any_bits(a[j]);
+      }
+    }
+    if (norm_w) {
+#pragma unroll
+      for (int j = 0; j < LB; ++j) {
+        sw[j] = squares(__builtin_bit_cast(x8, b[j]), sw[j]);
+        zw[j] |= any_bits(b[j]);
+      }
+    }
+    load(i + 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = h ? at1 : at0;
+      x8 af[MT], bf[NT];
+#pragma unroll
+      for (int k = 0; k < MT; ++k) af[k] = __builtin_bit_cast(x8, own[k * 128 + at]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) bf[j] = __builtin_bit_cast(x8, own[(MT + j) * 128 + at]);
+#pragma unroll
+      for (int k = 0; k < MT; ++k)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[k][j] = mfma(af[k], bf[j], acc[k][j]);
+    }
+  }
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        red[(wave * BM + i * 16 + (lane >> 4) * 4 + r) * LD + j * 16 + row] = acc[i][j][r];
+  // a row's squares lie in eight neighbouring lanes
+  auto put = [&](float s, uint32_t z, int at) {
+#pragma unroll
+    for (int m = 1; m < 8; m <<= 1) {
+      s += __shfl_xor(s, m, 64);
+      z |= __shfl_xor(z, m, 64);
+    }
+    if ((lane & 7) == 0) {
+      sq[wave][at + r8] = s;
+      nz[wave][at + r8] = z;
+    }
+  };
+  if (norm_x) {
+#pragma unroll
+    for (int j = 0; j < LA; ++j) put(sx[j], zx[j], j * 8);
+  }
+  if (norm_w) {
+#pragma unroll
+    for (int j = 0; j < LB; ++j) put(sw[j], zw[j], BM + j * 8);
+  }
+  __syncthreads();
+  for (int v = threadIdx.x; v < BM * BN; v += NW * 64) {
+    const int m = v / BN, c = v % BN;
+    float s = red[m * LD + c];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) s += red[(w * BM + m) * LD + c];
+    if (t0 + m < T && e0 + c < p.E) lg[(int64_t)(t0 + m) * p.E + e0 + c] = s;
+  }
+  for (int v = threadIdx.x; v < BM + BN; v += NW * 64) {
+    if (v < BM ? !norm_x : !norm_w) continue;
+    float s = 0.0f;
+    uint32_t z = 0;
+    for (int w = 0; w < NW; ++w) {
+      s += sq[w][v];
+      z |= nz[w][v];
+    }
+    const float bound = norm_bound(s, z);
+    if (v < BM && t0 + v < T) p.x_norm[t0 + v] = bound;
+    if (v >= BM && e0 + v - BM < p.E) p.w_norm[e0 + v - BM] = bound;
+  }
+}
+
+// ---- selection ------------------------------------------------------------
+
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
-__device__ inline double shfl_xor(double v, int m) { return __shfl_xor(v, m, 64); }
+__device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// Sum and maximum of doubles over a wave in registers (see wave_sum_dpp).
+template <int CTRL>
+__device__ inline double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double pair_d(uint32_t lo, uint32_t hi) {
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 __device__ inline double wave_sum(double v) {
-  for (int m = 1; m < 64; m <<= 1) v += shfl_xor(v, m);
-  return v;
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  uint64_t u = __builtin_bit_cast(uint64_t, v);
+  auto l = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
+  u = __builtin_bit_cast(uint64_t, v);
+  l = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  h = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
 }
 __device__ inline double wave_max(double v) {
-  for (int m = 1; m < 64; m <<= 1) v = fmax(v, shfl_xor(v, m));
-  return v;
+  // order-preserving key, its upper half first
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t k = u >> 63 ? ~u : u | 1ull << 63;
+  const uint32_t hi = wave_max_u32((uint32_t)(k >> 32));
+  const uint32_t lo = wave_max_u32((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+  const uint64_t m = (uint64_t)hi << 32 | lo;
+  return __builtin_bit_cast(double, m >> 63 ? m & ~(1ull << 63) : ~m);
 }
-__device__ inline bool finite(double v) { return fabs(v) <= 1.7976931348623157e308; }
+__device__ inline float key_float(uint32_t k) {
+  return __builtin_bit_cast(float, (k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ inline float wave_max(float v) { return key_float(wave_max_u32(float_key(v))); }
+
+// LDS of one wave is written and read by that wave alone.
+__device__ inline void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+}
 
 // x . w over d columns by one wave, in 64 bits (a product of two 16-bit
 // numbers is exact there).  Every lane gets the sum.
 template <class T16>
 __device__ inline double exact_dot(const T16* x, const T16* w, int d) {
-  typedef T16 x8 __attribute__((ext_vector_type(8)));
+  typedef typename Vec<T16>::x8 x8;
+  constexpr int B = 4;  // pieces whose loads are in flight together
   double s = 0.0;
-  for (int c = (threadIdx.x & 63) * 8; c < d; c += 512) {
-    const x8 a = *reinterpret_cast<const x8*>(x + c), b = *reinterpret_cast<const x8*>(w + c);
+  for (int c0 = (threadIdx.x & 63) * 8; c0 < d; c0 += 512 * B) {
+    x8 a[B], b[B];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fma((double)(float)a[j], (double)(float)b[j], s);
+    for (int i = 0; i < B; ++i) {
+      const int c = min(c0 + 512 * i, d - 8);
+      a[i] = *global<x8>(x + c);
+      b[i] = *global<x8>(w + c);
+    }
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+      if (c0 + 512 * i < d) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s = fma((double)(float)a[i][j], (double)(float)b[i][j], s);
+      }
   }
   return wave_sum(s);
 }
 
-// One wave per (token, expert).
-template <class T16>
-__global__ __launch_bounds__(kThreads) void router_logits_kernel(RouterParams p, int T,
-                                                                 const T16* __restrict__ x,
-                                                                 RouterOut o) {
-  const int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (o.count && blockIdx.x == 0)
-    for (int e = threadIdx.x; e < p.E; e += kThreads) o.count[e] = 0;
-  if (i >= (int64_t)T * p.E) return;
-  const int t = (int)(i / p.E), e = (int)(i - (int64_t)t * p.E);
-  const double l = exact_dot(x + (int64_t)t * p.d, static_cast<const T16*>(p.wg) + (int64_t)e * p.d, p.d);
-  if ((threadIdx.x & 63) == 0) {
-    p.logits[i] = l;
-    if (o.logits) o.logits[i] = (float)l;
+// Two best values of each group and what decides about it: 64 / G lanes per
+// group (G the groups rounded up to a power of two) scan its members and join.
+template <class F>
+struct GroupBest {
+  F sum;   // of the group's best one or two; -inf for a group without any
+  F low;   // the least value that counts in it
+};
+template <class F>
+__device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, int lane, int per, int g) {
+  const F none = -__builtin_inff();
+  const int size = p.E / p.n_groups;
+  F best = none, second = none;
+  if (g < p.n_groups)
+    for (int i = lane & (per - 1); i < size; i += per) {
+      const F v = row[g * size + i];
+      second = v > best ? best : v > second ? v : second;
+      best = v > best ? v : best;
+    }
+  for (int m = 1; m < per; m <<= 1) {
+    const F ob = __shfl_xor(best, m, 64), os = __shfl_xor(second, m, 64);
+    const F lo = ob > best ? best : ob;
+    second = os > second ? os : second;
+    second = lo > second ? lo : second;
+    best = ob > best ? ob : best;
+  }
+  const bool two = p.group_best == 2 && second > none;
+  return {two ? best + second : best, two ? second : best};
+}
+
+// What a token's selection has in LDS.
+template <int C>
+struct TokenLds {
+  double row[C * 64];
+  double sum[kRouterMaxGroups], low[kRouterMaxGroups];
+  float err[kRouterMaxGroups], more[2][kRouterMaxGroups];
+};
+
+// The selection by 64-bit sums where fp32 ones leave it open.  l: the token's
+// logits with their error bounds; experts whose order or group is open are
+// summed again (bound 0), those of `want` to begin with, until nothing is.
+// Lane k gets slot k.
+template <class T16, int C>
+__device__ void select_exact(const RouterParams& p, const T16* xr, const float (&lf)[C],
+                             const bool (&fit0)[C], const float (&bf)[C], bool (&want)[C], float xn,
+                             float rel,
+                             TokenLds<C>& lds, int& sel, float& sl) {
+  const int lane = threadIdx.x & 63;
+  const double none = -__builtin_inf();
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  double l[C];
+  float err[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int e = c * 64 + lane;
+    l[c] = lf[c];
+    err[c] = 0.0f;
+    if (e < p.E && finite(lf[c])) {
+      const float n = global<float>(p.w_norm)[e];
+      // (rounding to fp32 sums below the smallest numbers adds to the bound)
+      err[c] = n > 0.0f && xn > 0.0f ? fminf(rel * xn * n + 1e-33f, 1e30f) : 0.0f;
+    }
+    want[c] = want[c] && err[c] > 0.0f;
+  }
+  wave_lds_fence();  // the caller's use of lds ends here
+  int per = 64;
+  while (64 / per < p.n_groups) per >>= 1;
+  for (;;) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      uint64_t m = __ballot(want[c]);
+      while (m) {
+        const int at = __ffsll((unsigned long long)m) - 1;
+        m &= m - 1;
+        const double v = exact_dot(xr, static_cast<const T16*>(p.wg) + (int64_t)(c * 64 + at) * p.d, p.d);
+        if (lane == at) {
+          l[c] = v;
+          err[c] = 0.0f;
+        }
+      }
+    }
+    double key[C], sc[C], kerr[C];
+    bool fit[C];
+    double zrel = 0.0;
+    if (soft) {
+      double top = none, z = 0.0;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (finite(lf[c])) top = fmax(top, l[c]);
+      top = wave_max(top);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        sc[c] = finite(lf[c]) ? exp(l[c] - top) : 0.0;
+        z += sc[c];
+      }
+      z = wave_sum(z);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        sc[c] = finite(lf[c]) ? sc[c] / z : 0.0;
+        zrel += sc[c] * err[c];
+      }
+      zrel = biased ? 1.01 * wave_sum(zrel) : 0.0;  // (without a bias the sum is common to all)
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) sc[c] = finite(lf[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      fit[c] = fit0[c];
+      want[c] = false;
+      // slope of a score by its logit: s of the softmax's term, 1/4 at most of a sigmoid
+      const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
+      key[c] = biased ? sc[c] + bf[c] : l[c];
+      kerr[c] = biased ? serr : err[c];
+    }
+    bool open = false;
+    if (p.n_groups > 1) {
+      const int size = p.E / p.n_groups;
+#pragma unroll
+      for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
+      lds.more[0][lane] = lds.more[1][lane] = 0.0f;
+      wave_lds_fence();
+      const int g = lane / per;
+      const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
+      if ((lane & (per - 1)) == 0) {
+        lds.sum[g] = gb.sum;
+        lds.low[g] = gb.low;
+      }
+      // A group's error: that of its most uncertain member, once or twice,
+      // among those that may be one of its best - that reach, with their own
+      // bound, down to the least that counts less the bounds of what counts.
+#pragma unroll
+      for (int round = 0; round < 2; ++round) {
+        wave_lds_fence();
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int e = c * 64 + lane;
+          if (!fit[c]) continue;
+          const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
+          const double reach = round == 0 ? lds.row[e] : lds.row[e] + serr + lds.err[e / size];
+          const bool in = reach >= lds.low[e / size];
+          if (round == 1) want[c] = in && err[c] > 0.0f;
+          if (in && serr > 0.0)
+            atomicMax(reinterpret_cast<unsigned*>(&lds.more[round][e / size]),
+                      __float_as_uint((float)(serr * 1.0001)));
+        }
+        wave_lds_fence();
+        lds.err[lane] = lds.more[round][lane];
+      }
+      wave_lds_fence();
+      const bool is = lane < p.n_groups;
+      const double mine = is ? lds.sum[lane] : none;
+      int rank = 0;
+      for (int h = 0; h < p.n_groups; ++h) rank += lds.sum[h] > mine || (lds.sum[h] == mine && h < lane);
+      const uint64_t kept = __ballot(is && rank < p.top_groups);
+      bool unsure = false;
+      if (is && mine > none)
+        for (int h = 0; h < p.n_groups; ++h) {
+          const double v = lds.sum[h];
+          if (v > none && (kept >> lane & 1) != (kept >> h & 1))
+            unsure |= fabs(v - mine) <= p.group_best * ((double)lds.err[lane] + lds.err[h]) +
+                                            zrel * fmax(fabs(v), fabs(mine));
+        }
+      const uint64_t um = __ballot(unsure && (lds.err[lane] > 0.0f || zrel > 0.0));
+      open = um != 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] = want[c] && (um >> ((c * 64 + lane) / size) & 1);
+#pragma unroll
+      for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
+      wave_lds_fence();
+    }
+    if (!open) {
+      sel = -1;
+      for (int k = 0; k < p.K; ++k) {
+        double bk = none;
+        bool any = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (fit[c]) {
+            bk = any ? fmax(bk, key[c]) : key[c];
+            any = true;
+          }
+        bk = wave_max(bk);
+        int be = -1;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const uint64_t m = __ballot(fit[c] && key[c] == bk);
+          if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
+        }
+        if (be < 0) break;  // nobody left
+        double ml = 0.0, ms = 0.0, me = 0.0;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (c * 64 + lane == be) {
+            fit[c] = false;
+            ml = l[c];
+            ms = sc[c];
+            me = kerr[c];
+          }
+        ml = __shfl(ml, be & 63, 64);
+        ms = __shfl(ms, be & 63, 64);
+        me = __shfl(me, be & 63, 64);
+        if (lane == k) {
+          sel = be;
+          sl = (float)ml;
+        }
+        bool near = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const double room = me + kerr[c] + zrel * fabs(ms - sc[c]);
+          if (fit[c] && room > 0.0 && bk - key[c] <= room) {
+            near = true;
+            want[c] = want[c] || err[c] > 0.0f;
+          }
+        }
+        if (__ballot(near)) {
+          open = true;
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (c * 64 + lane == be) want[c] = want[c] || err[c] > 0.0f;
+        }
+      }
+    }
+    if (!open) return;
+    bool some = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) some |= want[c];
+    if (!__ballot(some)) {
+      // only the softmax's sum is uncertain: every logit that it adds
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] = err[c] > 0.0f;
+    }
   }
 }
 
 // log sigmoid(l) without overflow or loss far from 0
-__device__ inline double log_sigmoid(double l) { return fmin(l, 0.0) - log1p(exp(-fabs(l))); }
+__device__ inline float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
 
 // Selection and weights of one token by one wave; lane i holds the experts
-// i, i + 64, ... (C of them).
-template <int C>
-__global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p, int T, RouterOut o) {
-  __shared__ double rows[kWaves][C * 64];
-  __shared__ double groups[kWaves][kRouterMaxGroups];
+// i, i + 64, ... (C of them).  rel: the logits' error (sum_error).
+template <class T16, int C>
+__global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p, int T,
+                                                                 const T16* __restrict__ x,
+                                                                 const float* __restrict__ lg,
+                                                                 float rel, RouterOut o) {
+  __shared__ TokenLds<C> lds_all[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = blockIdx.x * kWaves + wave;
-  const bool on = t < T;
-  const double none = -__builtin_inf();
-  double l[C], key[C];
-  bool fit[C];   // can be selected
-  double top = none;
+  if (t >= T) return;  // (no barrier of the block follows)
+  TokenLds<C>& lds = lds_all[wave];
+  const float none = -__builtin_inff();
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  float l[C], b[C], wn[C];
+  const float xn = global<float>(p.x_norm)[t];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int e = c * 64 + lane;
-    l[c] = on && e < p.E ? p.logits[(int64_t)t * p.E + e] : none;
-    fit[c] = finite(l[c]);
-    if (fit[c]) top = fmax(top, l[c]);
+    const bool in = e < p.E;
+    l[c] = in ? lg[(int64_t)t * p.E + e] : none;
+    b[c] = in && biased ? global<float>(p.bias)[e] : 0.0f;
+    wn[c] = in ? global<float>(p.w_norm)[e] : 0.0f;
   }
-  double score[C];
-  if (p.score == SCORE_SIGMOID) {
+  bool fit[C];
+  float key[C], kerr[C], sc[C];
+  float top = none, z = 0.0f, far = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) score[c] = fit[c] ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
-  } else {
+  for (int c = 0; c < C; ++c) {
+    fit[c] = finite(l[c]);
+    if (fit[c]) top = fmaxf(top, l[c]);
+    kerr[c] = xn > 0.0f && wn[c] > 0.0f ? fminf(rel * xn * wn[c] + 1e-33f, 1e30f) : 0.0f;
+    far = fmaxf(far, fit[c] ? kerr[c] : 0.0f);
+  }
+  if (soft) {
     top = wave_max(top);
-    double z = 0.0;
+    far = wave_max(far);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      score[c] = fit[c] ? exp(l[c] - top) : 0.0;
-      z += score[c];
+      sc[c] = fit[c] ? expf(l[c] - top) : 0.0f;
+      z += sc[c];
     }
-    z = wave_sum(z);
-#pragma unroll
-    for (int c = 0; c < C; ++c) score[c] = fit[c] ? score[c] / z : 0.0;
+    z = wave_sum_dpp(z);
   }
+  // keys and their bounds; 1e-6 of a score covers its fp32 functions
+  float val[C], verr[C];  // what groups count
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int e = c * 64 + lane;
+    if (soft) {
+      sc[c] = fit[c] ? sc[c] / z : 0.0f;
+      verr[c] = sc[c] * 1.01f * (kerr[c] + far + 1e-6f * (2.0f + (top - l[c])));
+      if (!fit[c]) verr[c] = 0.0f;
+    } else {
+      sc[c] = fit[c] ? 1.0f / (1.0f + expf(-l[c])) : 0.0f;
+      verr[c] = 0.25f * kerr[c] + 1e-6f * sc[c];
+    }
+    val[c] = sc[c];
     key[c] = l[c];
-    if (p.bias && e < p.E) {
-      const float b = p.bias[e];
-      fit[c] = fit[c] && finite(b);
-      key[c] = score[c] + b;
+    if (biased) {
+      fit[c] = fit[c] && finite(b[c]);
+      val[c] = key[c] = sc[c] + b[c];
+      kerr[c] = verr[c] = verr[c] + 1e-7f * fabsf(key[c]);
     }
   }
-  if (p.n_groups > 1) {
-    // lane g scans the members of group g
-    const int size = p.E / p.n_groups;
+  bool fit0[C], open = false, groups_open = false;
 #pragma unroll
-    for (int c = 0; c < C; ++c) rows[wave][c * 64 + lane] = fit[c] ? (p.bias ? key[c] : score[c]) : none;
-    __syncthreads();
-    double best = none, second = none;
-    if (lane < p.n_groups)
-      for (int i = 0; i < size; ++i) {
-        const double v = rows[wave][lane * size + i];
-        if (v > best) {
-          second = best;
-          best = v;
-        } else {
-          second = fmax(second, v);
-        }
-      }
-    const double sum = p.group_best == 2 && second > none ? best + second : best;
-    groups[wave][lane] = sum;
-    __syncthreads();
-    int rank = 0;
-    for (int g = 0; g < p.n_groups; ++g) {
-      const double v = groups[wave][g];
-      rank += v > sum || (v == sum && g < lane);
+  for (int c = 0; c < C; ++c) fit0[c] = fit[c];
+  if (p.n_groups > 1) {
+    const int size = p.E / p.n_groups;
+    int per = 64;
+    while (64 / per < p.n_groups) per >>= 1;
+    float* row = reinterpret_cast<float*>(lds.row);
+    float worst = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      row[c * 64 + lane] = fit[c] ? val[c] : none;
+      worst = fmaxf(worst, fit[c] ? verr[c] : 0.0f);
     }
-    const uint64_t kept = __ballot(lane < p.n_groups && rank < p.top_groups);
+    wave_lds_fence();
+    worst = wave_max(worst);
+    const int g = lane / per;
+    const GroupBest<float> gb = group_best(p, row, lane, per, g);
+    float* sums = reinterpret_cast<float*>(lds.sum);
+    if ((lane & (per - 1)) == 0) sums[g] = gb.sum;
+    wave_lds_fence();
+    const bool is = lane < p.n_groups;
+    const float mine = is ? sums[lane] : none;
+    int rank = 0;
+    for (int h = 0; h < p.n_groups; ++h) rank += sums[h] > mine || (sums[h] == mine && h < lane);
+    const uint64_t kept = __ballot(is && rank < p.top_groups);
+    // the least kept group against the best of the others
+    const float in = wave_max(is && rank < p.top_groups ? -mine : none);
+    const float out = wave_max(is && rank >= p.top_groups ? mine : none);
+    if (out > none && -in - out <= 2.0f * p.group_best * worst + 1e-6f * fmaxf(fabsf(in), fabsf(out)))
+      open = groups_open = true;
 #pragma unroll
     for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
   }
   // top-k: lane k keeps slot k
   int sel = -1;
-  double sl = 0.0;
-  for (int k = 0; k < p.K; ++k) {
-    double bk = none;
-    int be = 1 << 30;
+  float sl = 0.0f;
+  bool want[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) want[c] = false;
+  for (int k = 0; k < p.K && !groups_open; ++k) {
+    float bk = none;
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (fit[c] && (be == 1 << 30 || key[c] > bk)) {
-        bk = key[c];
-        be = c * 64 + lane;
-      }
-    for (int m = 1; m < 64; m <<= 1) {
-      const double ok = shfl_xor(bk, m);
-      const int oe = __shfl_xor(be, m, 64);
-      if (ok > bk || (ok == bk && oe < be)) {
-        bk = ok;
-        be = oe;
-      }
+      if (fit[c]) bk = fmaxf(bk, key[c]);
+    bk = wave_max(bk);
+    int be = -1;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint64_t m = __ballot(fit[c] && key[c] == bk);
+      if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
     }
-    if (be == 1 << 30) break;  // nobody left (uniform)
-    double mine = 0.0;
+    if (be < 0) break;  // nobody left
+    float ml = 0.0f, me = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (c * 64 + lane == be) {
-        fit[c] = false;
-        mine = l[c];
+      if (be >> 6 == c) {
+        ml = __shfl(l[c], be & 63, 64);
+        me = __shfl(kerr[c], be & 63, 64);
+        if (lane == (be & 63)) fit[c] = false;
       }
-    mine = __shfl(mine, be & 63, 64);
+    bool near = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (fit[c] && bk - key[c] <= me + kerr[c]) near = want[c] = true;
+    if (__ballot(near)) {
+      open = true;
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] |= c * 64 + lane == be;
+    }
     if (lane == k) {
       sel = be;
-      sl = mine;
+      sl = ml;
     }
   }
+  if (open) select_exact<T16, C>(p, x + (int64_t)t * p.d, l, fit0, b, want, xn, rel, lds, sel, sl);
   // weights: the share of the selected scores by their logarithms, so that
   // scores that underflow still have their ratios
   const bool have = sel >= 0;
-  const double ls = !have ? none : p.score == SCORE_SIGMOID ? log_sigmoid(sl) : sl;
-  const double lm = wave_max(ls);
-  const double ex = have ? exp(ls - lm) : 0.0;
-  const double sum = wave_sum(ex);
-  const float share = have ? (float)(ex / sum) : 0.0f;
+  const float ls = !have ? none : soft ? sl : log_sigmoid(sl);
+  const float lm = wave_max(ls);  // (by every lane of the wave)
+  const float ex = have ? expf(ls - lm) : 0.0f;
+  const float sum = wave_sum_dpp(ex);
+  const float share = have ? ex / sum : 0.0f;
   float w = share;
-  if (!p.renorm) {
-    if (p.score == SCORE_SIGMOID) {
-      w = have ? (float)exp(ls) : 0.0f;
-    } else {
-      double z = 0.0;
-#pragma unroll
-      for (int c = 0; c < C; ++c) z += finite(l[c]) ? exp(l[c] - top) : 0.0;
-      z = wave_sum(z);
-      w = have ? (float)(exp(sl - top) / z) : 0.0f;
-    }
-  }
+  if (!p.renorm) w = !have ? 0.0f : soft ? expf(sl - top) / z : 1.0f / (1.0f + expf(-sl));
   w *= p.scale;
   // Eq. 2 over the shares: the score of a slot is the sum of those above it
   int prec = PREC_SKIP;
@@ -204,17 +722,17 @@ __global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p,
         first = false;
       }
     }
-    if (have && on && lane < p.K) {
+    if (have) {
       const int tag = o.table[sel].tag;
       if (tag == TAG_FP16 || tag == TAG_INT8) prec = PREC_HIGH;
       else if (tag == TAG_INT4 || tag == TAG_INT2) prec = PREC_LOW;
       else prec = first || above <= o.t1 ? PREC_HIGH : above <= o.t2 ? PREC_LOW : PREC_SKIP;
     }
   }
-  if (on && lane < p.K) {
+  if (lane < p.K) {
     const int64_t i = (int64_t)t * p.K + lane;
-    if (o.idx) o.idx[i] = sel;
-    if (o.w) o.w[i] = w;
+    o.idx[i] = sel;
+    o.w[i] = w;
     if (o.prec) o.prec[i] = (int8_t)prec;
     if (o.user_idx) o.user_idx[i] = sel;
     if (o.user_w) o.user_w[i] = w;
@@ -223,17 +741,44 @@ __global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p,
   }
 }
 
+template <class T16, int MT, int NT, int NW>
+hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, int32_t* count, float* rel,
+                  hipStream_t s) {
+  *rel = sum_error(p.d, NW);
+  const dim3 grid((T + MT * 16 - 1) / (MT * 16), (p.E + NT * 16 - 1) / (NT * 16));
+  router_logits_kernel<T16, MT, NT, NW><<<grid, NW * 64, 0, s>>>(p, T, x, lg, count);
+  return hipGetLastError();
+}
+
 template <class T16>
 hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, hipStream_t s) {
-  const int64_t items = (int64_t)T * p.E;
-  router_logits_kernel<T16><<<(unsigned)((items + kWaves - 1) / kWaves), kThreads, 0, s>>>(p, T, x, o);
-  hipError_t e = hipGetLastError();
+  float* lg = o.logits ? o.logits : p.logits;
+  float rel = 0.0f;
+  // The largest tile that still gives about every compute unit a block: a
+  // block loads (tokens + experts) rows for tokens * experts sums.  us at d
+  // 4096, 256 experts, tiles of 64x64 / 64x32 / 32x32 / 16x32 / 16x16 on eight
+  // waves: 4096 tokens 21.9 26.8 32.8 43.7 53.1, 2048 20.4 15.9 17.9 22.9 28.1,
+  // 1024 19.7 14.6 11.0 13.6 15.6, 512 19.5 14.5 9.9 8.4 9.3, 64 18.9 14.4 9.8
+  // 7.3 5.7.  Two blocks of 64x64 fit a unit on four waves each: 8192 tokens
+  // 35.0, on eight 42.0.  With at most 16 experts the tokens' rows are what is
+  // loaded, and small blocks spread them best: 8192 tokens, 16 experts 16x16
+  // on 16 waves 14.6, 32x16 on eight 18.9.
+  auto blocks = [&](int m, int n) { return (int64_t)((T + m - 1) / m) * ((p.E + n - 1) / n); };
+  constexpr int kEnough = 200;
+  hipError_t e;
+  if (p.E <= 16) e = logits<T16, 1, 1, 16>(p, T, x, lg, o.count, &rel, s);
+  else if (blocks(64, 64) >= 2 * kEnough) e = logits<T16, 4, 4, 4>(p, T, x, lg, o.count, &rel, s);
+  else if (blocks(64, 64) >= kEnough) e = logits<T16, 4, 4, 8>(p, T, x, lg, o.count, &rel, s);
+  else if (blocks(64, 32) >= kEnough) e = logits<T16, 4, 2, 8>(p, T, x, lg, o.count, &rel, s);
+  else if (blocks(32, 32) >= kEnough) e = logits<T16, 2, 2, 8>(p, T, x, lg, o.count, &rel, s);
+  else if (blocks(16, 32) >= kEnough) e = logits<T16, 1, 2, 8>(p, T, x, lg, o.count, &rel, s);
+  else e = logits<T16, 1, 1, 8>(p, T, x, lg, o.count, &rel, s);
   if (e != hipSuccess) return e;
   const int grid = (T + kWaves - 1) / kWaves;
-  if (p.E <= 64) router_select_kernel<1><<<grid, kThreads, 0, s>>>(p, T, o);
-  else if (p.E <= 128) router_select_kernel<2><<<grid, kThreads, 0, s>>>(p, T, o);
-  else if (p.E <= 256) router_select_kernel<4><<<grid, kThreads, 0, s>>>(p, T, o);
-  else router_select_kernel<8><<<grid, kThreads, 0, s>>>(p, T, o);
+  if (p.E <= 64) router_select_kernel<T16, 1><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
+  else if (p.E <= 128) router_select_kernel<T16, 2><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
+  else if (p.E <= 256) router_select_kernel<T16, 4><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
+  else router_select_kernel<T16, 8><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
   return hipGetLastError();
 }
 
