@@ -273,6 +273,7 @@ struct RouterParams {
   float* logits;           // [T, E], calls that do not ask for them
   float* x_norm;           // [T] bounds of the rows' norms
   float* w_norm;           // [E]
+  int32_t* open;           // [1 + T] number and list of tokens whose selection is open
   float* d_logits;         // [T, E], routers with a backward pass
 };
 

@@ -6,16 +6,16 @@
 //   top-k of the keys in the groups that count most, ties to the lower index
 //   w = scale s, or scale s / sum of the selected s
 //
-// Two kernels.  The logits are a matrix product on the matrix cores, in fp32
-// sums; a second kernel takes one wave per token for everything else.
+// The logits are a matrix product on the matrix cores, in fp32 sums; another
+// kernel takes a wave per token for everything else.
 //
 // Which of two near keys is larger decides what is selected, and fp32 sums
 // differ in their last bits with the split of the sum.  So the first kernel
 // also gives the norms of the rows of x and Wg, whose product bounds the
-// error of a logit, and the second one carries a bound beside every key.
-// Where two keys (or groups) that decide something lie within their bounds -
-// a few tokens in a hundred - it sums the logits in question again in 64
-// bits and decides by those.
+// error of a logit, and the selection knows how near two keys may be to be in
+// order for certain.  Where two keys (or groups) that decide something are
+// nearer - for a few tokens in a hundred - a block per token sums the logits
+// in question again in 64 bits and decides by those.
 #include "moe_internal.h"
 
 namespace moe {
@@ -118,8 +118,11 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t0 = blockIdx.x * BM, e0 = blockIdx.y * BN;
   const bool norm_x = blockIdx.y == 0, norm_w = blockIdx.x == 0;
-  if (count && blockIdx.x == 0 && blockIdx.y == 0)
-    for (int e = threadIdx.x; e < p.E; e += NW * 64) count[e] = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0) {  // what the selection adds to
+    if (threadIdx.x == 0) p.open[0] = 0;
+    if (count)
+      for (int e = threadIdx.x; e < p.E; e += NW * 64) count[e] = 0;
+  }
   // this lane's chunks as offsets in bytes from the block's first row (a tile
   // has at most 128 rows of 32 KiB), so that loads take one uniform address
   Global<char> xb = global<char>(x + (int64_t)t0 * p.d);
@@ -247,9 +250,6 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
 
 // ---- selection ------------------------------------------------------------
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-
 __device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 
 // Sum and maximum of doubles over a wave in registers (see wave_sum_dpp).
@@ -258,6 +258,20 @@ __device__ inline double dpp_d(double v) {
   const uint64_t u = __builtin_bit_cast(uint64_t, v);
   const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
   const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ inline double dpp_of(double v) { return dpp_d<CTRL>(v); }
+template <int CTRL>
+__device__ inline float dpp_of(float v) { return dpp_f<CTRL>(v); }
+// The value that lane `from` (the same for all) has.
+__device__ inline float lane_value(float v, int from) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), from));
+}
+__device__ inline double lane_value(double v, int from) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, from);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), from);
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 __device__ inline double pair_d(uint32_t lo, uint32_t hi) {
@@ -302,7 +316,7 @@ __device__ inline void wave_lds_fence() {
 template <class T16>
 __device__ inline double exact_dot(const T16* x, const T16* w, int d) {
   typedef typename Vec<T16>::x8 x8;
-  constexpr int B = 4;  // pieces whose loads are in flight together
+  constexpr int B = 8;  // pieces whose loads are in flight together
   double s = 0.0;
   for (int c0 = (threadIdx.x & 63) * 8; c0 < d; c0 += 512 * B) {
     x8 a[B], b[B];
@@ -340,68 +354,138 @@ __device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, i
       second = v > best ? best : v > second ? v : second;
       best = v > best ? v : best;
     }
-  for (int m = 1; m < per; m <<= 1) {
-    const F ob = __shfl_xor(best, m, 64), os = __shfl_xor(second, m, 64);
+  const auto join = [&](F ob, F os) {
     const F lo = ob > best ? best : ob;
     second = os > second ? os : second;
     second = lo > second ? lo : second;
     best = ob > best ? ob : best;
-  }
+  };
+  // lane ^ 1, lane ^ 2, mirrors in 8 and 16, then the other row of 16 and half
+  if (per > 1) join(dpp_of<0xB1>(best), dpp_of<0xB1>(second));
+  if (per > 2) join(dpp_of<0x4E>(best), dpp_of<0x4E>(second));
+  if (per > 4) join(dpp_of<0x141>(best), dpp_of<0x141>(second));
+  if (per > 8) join(dpp_of<0x140>(best), dpp_of<0x140>(second));
+  if (per > 16) join(__shfl_xor(best, 16, 64), __shfl_xor(second, 16, 64));
+  if (per > 32) join(__shfl_xor(best, 32, 64), __shfl_xor(second, 32, 64));
   const bool two = p.group_best == 2 && second > none;
   return {two ? best + second : best, two ? second : best};
 }
 
-// What a token's selection has in LDS.
+// One token's fp32 selection, by one wave: lane i has the experts i, i + 64,
+// ... (C of them), lane k slot k.
 template <int C>
-struct TokenLds {
-  double row[C * 64];
+struct Token {
+  float l[C], b[C], key[C];
+  float val[C];       // what groups count
+  bool exact[C];      // its row or the token's is all zeros: so is the sum
+  bool fit[C];        // can be selected at all
+  bool kept[C];       // ... and lies in a group that stays
+  // lanes of group g (lanes_per_group of them): its best members, whether it
+  // stays, the least sum that does and the largest that does not
+  GroupBest<float> group;
+  bool stays;
+  float in, out, group_err;
+  float top, z, zrel; // softmax: largest logit, denominator, its relative error
+  float margin;       // keys further apart are certainly in order
+  bool groups_open, slots_open;
+  int sel;
+  float sl;           // its logit
+};
+
+__device__ inline int lanes_per_group(const RouterParams& p) {
+  int per = 64;
+  while (64 / per < p.n_groups) per >>= 1;
+  return per;
+}
+
+// Error of a group's sum.
+template <int C>
+__device__ inline float group_margin(const Token<C>& tk) {
+  return tk.group_err + 5e-7f * fmaxf(fabsf(tk.in), fabsf(tk.out));
+}
+
+// The experts of the groups that stay.
+template <int C>
+__device__ inline void keep_groups(const RouterParams& p, Token<C>& tk) {
+  const int lane = threadIdx.x & 63, size = p.E / p.n_groups, per = lanes_per_group(p);
+  const uint64_t at = __ballot(tk.stays);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    tk.kept[c] = tk.fit[c] && (at >> min((c * 64 + lane) / size * per, 63) & 1);
+}
+
+// LDS of a block that works on one token whose selection is open.
+template <int C>
+struct OpenLds {
+  double row[C * 64];    // keys or scores for the groups' scan
+  double dots[C * 64];   // logits summed again
+  int32_t list[C * 64];  // ... and their experts
   double sum[kRouterMaxGroups], low[kRouterMaxGroups];
   float err[kRouterMaxGroups], more[2][kRouterMaxGroups];
 };
 
-// The selection by 64-bit sums where fp32 ones leave it open.  l: the token's
-// logits with their error bounds; experts whose order or group is open are
-// summed again (bound 0), those of `want` to begin with, until nothing is.
-// Lane k gets slot k.
+// Sums the logits of the experts of `want` again, in 64 bits, the block's
+// waves in turn; take(c, lane, value) gets each.  Every wave has the same
+// `want` and calls this.
+template <class T16, int C, class Take>
+__device__ inline void sum_again(const RouterParams& p, const T16* xr, const bool (&want)[C],
+                                 OpenLds<C>& lds, Take take) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint64_t m = __ballot(want[c]);
+    if (want[c] && threadIdx.x < 64)
+      lds.list[n + __popcll(m & ((1ull << lane) - 1ull))] = c * 64 + lane;
+    n += __popcll(m);
+  }
+  __syncthreads();
+  for (int i = wave; i < n; i += (int)(blockDim.x >> 6)) {
+    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    const double v = exact_dot(xr, static_cast<const T16*>(p.wg) + (int64_t)e * p.d, p.d);
+    if (lane == 0) lds.dots[i] = v;
+  }
+  __syncthreads();
+  for (int i = 0; i < n; ++i) {
+    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    take(e >> 6, e & 63, lds.dots[i]);
+  }
+  __syncthreads();
+}
+
+// The selection by 64-bit sums, whatever is open: experts whose order or group
+// is not certain are summed again (bound 0) until nothing is open.
 template <class T16, int C>
-__device__ void select_exact(const RouterParams& p, const T16* xr, const float (&lf)[C],
-                             const bool (&fit0)[C], const float (&bf)[C], bool (&want)[C], float xn,
-                             float rel,
-                             TokenLds<C>& lds, int& sel, float& sl) {
+__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, float xn, float rel,
+                             OpenLds<C>& lds) {
   const int lane = threadIdx.x & 63;
   const double none = -__builtin_inf();
   const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
   double l[C];
   float err[C];
+  bool want[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int e = c * 64 + lane;
-    l[c] = lf[c];
+    l[c] = tk.l[c];
     err[c] = 0.0f;
-    if (e < p.E && finite(lf[c])) {
+    if (e < p.E && finite(tk.l[c])) {
       const float n = global<float>(p.w_norm)[e];
       // (rounding to fp32 sums below the smallest numbers adds to the bound)
       err[c] = n > 0.0f && xn > 0.0f ? fminf(rel * xn * n + 1e-33f, 1e30f) : 0.0f;
     }
-    want[c] = want[c] && err[c] > 0.0f;
+    want[c] = false;
   }
-  wave_lds_fence();  // the caller's use of lds ends here
-  int per = 64;
-  while (64 / per < p.n_groups) per >>= 1;
+  const int per = lanes_per_group(p);
   for (;;) {
+    sum_again(p, xr, want, lds, [&](int c, int at, double v) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      uint64_t m = __ballot(want[c]);
-      while (m) {
-        const int at = __ffsll((unsigned long long)m) - 1;
-        m &= m - 1;
-        const double v = exact_dot(xr, static_cast<const T16*>(p.wg) + (int64_t)(c * 64 + at) * p.d, p.d);
-        if (lane == at) {
-          l[c] = v;
-          err[c] = 0.0f;
+      for (int i = 0; i < C; ++i)
+        if (i == c && lane == at) {
+          l[i] = v;
+          err[i] = 0.0f;
         }
-      }
-    }
+    });
     double key[C], sc[C], kerr[C];
     bool fit[C];
     double zrel = 0.0;
@@ -409,43 +493,45 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
       double top = none, z = 0.0;
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (finite(lf[c])) top = fmax(top, l[c]);
+        if (finite(tk.l[c])) top = fmax(top, l[c]);
       top = wave_max(top);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        sc[c] = finite(lf[c]) ? exp(l[c] - top) : 0.0;
+        sc[c] = finite(tk.l[c]) ? exp(l[c] - top) : 0.0;
         z += sc[c];
       }
       z = wave_sum(z);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        sc[c] = finite(lf[c]) ? sc[c] / z : 0.0;
+        sc[c] = finite(tk.l[c]) ? sc[c] / z : 0.0;
         zrel += sc[c] * err[c];
       }
       zrel = biased ? 1.01 * wave_sum(zrel) : 0.0;  // (without a bias the sum is common to all)
     } else {
 #pragma unroll
-      for (int c = 0; c < C; ++c) sc[c] = finite(lf[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
+      for (int c = 0; c < C; ++c) sc[c] = finite(tk.l[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      fit[c] = fit0[c];
+      fit[c] = tk.fit[c];
       want[c] = false;
       // slope of a score by its logit: s of the softmax's term, 1/4 at most of a sigmoid
       const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
-      key[c] = biased ? sc[c] + bf[c] : l[c];
+      key[c] = biased ? sc[c] + tk.b[c] : l[c];
       kerr[c] = biased ? serr : err[c];
     }
     bool open = false;
     if (p.n_groups > 1) {
       const int size = p.E / p.n_groups;
+      if (threadIdx.x < 64) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
-      lds.more[0][lane] = lds.more[1][lane] = 0.0f;
-      wave_lds_fence();
+        for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
+        lds.more[0][lane] = lds.more[1][lane] = 0.0f;
+      }
+      __syncthreads();
       const int g = lane / per;
       const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
-      if ((lane & (per - 1)) == 0) {
+      if (threadIdx.x < 64 && (lane & (per - 1)) == 0) {
         lds.sum[g] = gb.sum;
         lds.low[g] = gb.low;
       }
@@ -454,7 +540,7 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
       // bound, down to the least that counts less the bounds of what counts.
 #pragma unroll
       for (int round = 0; round < 2; ++round) {
-        wave_lds_fence();
+        __syncthreads();
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const int e = c * 64 + lane;
@@ -463,14 +549,14 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
           const double reach = round == 0 ? lds.row[e] : lds.row[e] + serr + lds.err[e / size];
           const bool in = reach >= lds.low[e / size];
           if (round == 1) want[c] = in && err[c] > 0.0f;
-          if (in && serr > 0.0)
+          if (in && serr > 0.0 && threadIdx.x < 64)
             atomicMax(reinterpret_cast<unsigned*>(&lds.more[round][e / size]),
                       __float_as_uint((float)(serr * 1.0001)));
         }
-        wave_lds_fence();
-        lds.err[lane] = lds.more[round][lane];
+        __syncthreads();
+        if (threadIdx.x < 64) lds.err[lane] = lds.more[round][lane];
       }
-      wave_lds_fence();
+      __syncthreads();
       const bool is = lane < p.n_groups;
       const double mine = is ? lds.sum[lane] : none;
       int rank = 0;
@@ -490,10 +576,10 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
       for (int c = 0; c < C; ++c) want[c] = want[c] && (um >> ((c * 64 + lane) / size) & 1);
 #pragma unroll
       for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
-      wave_lds_fence();
+      __syncthreads();
     }
     if (!open) {
-      sel = -1;
+      tk.sel = -1;
       for (int k = 0; k < p.K; ++k) {
         double bk = none;
         bool any = false;
@@ -510,6 +596,7 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
           const uint64_t m = __ballot(fit[c] && key[c] == bk);
           if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
         }
+        be = __builtin_amdgcn_readfirstlane(be);
         if (be < 0) break;  // nobody left
         double ml = 0.0, ms = 0.0, me = 0.0;
 #pragma unroll
@@ -520,12 +607,12 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
             ms = sc[c];
             me = kerr[c];
           }
-        ml = __shfl(ml, be & 63, 64);
-        ms = __shfl(ms, be & 63, 64);
-        me = __shfl(me, be & 63, 64);
+        ml = lane_value(ml, be & 63);
+        ms = lane_value(ms, be & 63);
+        me = lane_value(me, be & 63);
         if (lane == k) {
-          sel = be;
-          sl = (float)ml;
+          tk.sel = be;
+          tk.sl = (float)ml;
         }
         bool near = false;
 #pragma unroll
@@ -549,7 +636,7 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
 #pragma unroll
     for (int c = 0; c < C; ++c) some |= want[c];
     if (!__ballot(some)) {
-      // only the softmax's sum is uncertain: every logit that it adds
+      // only the softmax's denominator is uncertain: every logit that it adds
 #pragma unroll
       for (int c = 0; c < C; ++c) want[c] = err[c] > 0.0f;
     }
@@ -559,156 +646,326 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, const float (
 // log sigmoid(l) without overflow or loss far from 0
 __device__ inline float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
 
-// Selection and weights of one token by one wave; lane i holds the experts
-// i, i + 64, ... (C of them).  rel: the logits' error (sum_error).
-template <class T16, int C>
-__global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p, int T,
-                                                                 const T16* __restrict__ x,
-                                                                 const float* __restrict__ lg,
-                                                                 float rel, RouterOut o) {
-  __shared__ TokenLds<C> lds_all[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int t = blockIdx.x * kWaves + wave;
-  if (t >= T) return;  // (no barrier of the block follows)
-  TokenLds<C>& lds = lds_all[wave];
+// Descending order of a lane's C keys, each with its number c.
+template <int C>
+__device__ inline void sort_lane(uint32_t (&k)[C], int (&e)[C]) {
+  const auto step = [&](int i, int j) {
+    const bool swap = k[j] > k[i];
+    const uint32_t kt = swap ? k[j] : k[i];
+    k[j] = swap ? k[i] : k[j];
+    k[i] = kt;
+    const int et = swap ? e[j] : e[i];
+    e[j] = swap ? e[i] : e[j];
+    e[i] = et;
+  };
+  // odd-even merging: pairs, fours, eights
+#pragma unroll
+  for (int n = 1; n < C; n *= 2)
+#pragma unroll
+    for (int m = n; m >= 1; m /= 2)
+#pragma unroll
+      for (int j = m % n; j + m < C; j += 2 * m)
+#pragma unroll
+        for (int i = 0; i < m; ++i)
+          if (i + j + m < C && (i + j) / (2 * n) == (i + j + m) / (2 * n)) step(i + j, i + j + m);
+}
+
+// Scores, keys and groups of token t in fp32.  Keys are compared with one
+// margin, twice the largest bound of their errors.  For the slots each lane
+// sorts its keys, and a slot takes the largest of the lanes' first ones
+// (take_slots).  row: C * 64 floats of LDS of the wave's own.
+template <int C>
+__device__ inline void score_token(const RouterParams& p, int t, const float* lg, float xn, float rel,
+                                   float* row, Token<C>& tk) {
+  const int lane = threadIdx.x & 63;
   const float none = -__builtin_inff();
   const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  float l[C], b[C], wn[C];
-  const float xn = global<float>(p.x_norm)[t];
+  float err[C], sc[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int e = c * 64 + lane;
     const bool in = e < p.E;
-    l[c] = in ? lg[(int64_t)t * p.E + e] : none;
-    b[c] = in && biased ? global<float>(p.bias)[e] : 0.0f;
-    wn[c] = in ? global<float>(p.w_norm)[e] : 0.0f;
+    tk.l[c] = in ? lg[(int64_t)t * p.E + e] : none;
+    tk.b[c] = in && biased ? global<float>(p.bias)[e] : 0.0f;
+    err[c] = in ? global<float>(p.w_norm)[e] : 0.0f;
   }
-  bool fit[C];
-  float key[C], kerr[C], sc[C];
-  float top = none, z = 0.0f, far = 0.0f;
+  float worst = 0.0f;
+  tk.top = none;
+  tk.z = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    fit[c] = finite(l[c]);
-    if (fit[c]) top = fmaxf(top, l[c]);
-    kerr[c] = xn > 0.0f && wn[c] > 0.0f ? fminf(rel * xn * wn[c] + 1e-33f, 1e30f) : 0.0f;
-    far = fmaxf(far, fit[c] ? kerr[c] : 0.0f);
+    tk.fit[c] = finite(tk.l[c]);
+    if (tk.fit[c]) tk.top = fmaxf(tk.top, tk.l[c]);
+    // (rounding to fp32 of the smallest numbers adds to a bound)
+    err[c] = xn > 0.0f && err[c] > 0.0f ? fminf(rel * xn * err[c] + 1e-33f, 1e30f) : 0.0f;
+    tk.exact[c] = err[c] == 0.0f;
+    worst = fmaxf(worst, tk.fit[c] ? err[c] : 0.0f);
   }
+  // The scores by the fast exponential and reciprocal: within 1e-6 of a
+  // score, and of a softmax's term 1e-6 for each unit below the largest.
+  tk.zrel = soft ? wave_max(worst) + 4e-6f : 0.0f;
   if (soft) {
-    top = wave_max(top);
-    far = wave_max(far);
+    tk.top = wave_max(tk.top);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      sc[c] = fit[c] ? expf(l[c] - top) : 0.0f;
-      z += sc[c];
+      sc[c] = tk.fit[c] ? __expf(tk.l[c] - tk.top) : 0.0f;
+      tk.z += sc[c];
     }
-    z = wave_sum_dpp(z);
+    tk.z = wave_sum_dpp(tk.z);
   }
-  // keys and their bounds; 1e-6 of a score covers its fp32 functions
-  float val[C], verr[C];  // what groups count
+  float verr = 0.0f;  // largest error of what groups count
+  worst = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
+    float e1;
     if (soft) {
-      sc[c] = fit[c] ? sc[c] / z : 0.0f;
-      verr[c] = sc[c] * 1.01f * (kerr[c] + far + 1e-6f * (2.0f + (top - l[c])));
-      if (!fit[c]) verr[c] = 0.0f;
+      sc[c] = tk.fit[c] ? sc[c] * __frcp_rn(tk.z) : 0.0f;
+      e1 = tk.fit[c] ? sc[c] * 1.01f * (err[c] + tk.zrel + 1e-6f * (tk.top - tk.l[c])) : 0.0f;
     } else {
-      sc[c] = fit[c] ? 1.0f / (1.0f + expf(-l[c])) : 0.0f;
-      verr[c] = 0.25f * kerr[c] + 1e-6f * sc[c];
+      sc[c] = tk.fit[c] ? __frcp_rn(1.0f + __expf(-tk.l[c])) : 0.0f;
+      e1 = 0.25f * err[c] + 1e-6f * sc[c];
     }
-    val[c] = sc[c];
-    key[c] = l[c];
+    tk.key[c] = tk.l[c];
     if (biased) {
-      fit[c] = fit[c] && finite(b[c]);
-      val[c] = key[c] = sc[c] + b[c];
-      kerr[c] = verr[c] = verr[c] + 1e-7f * fabsf(key[c]);
+      tk.fit[c] = tk.fit[c] && finite(tk.b[c]);
+      tk.key[c] = sc[c] + tk.b[c];
+      e1 += 1e-7f * fabsf(tk.key[c]);
     }
+    verr = fmaxf(verr, tk.fit[c] ? e1 : 0.0f);
+    worst = fmaxf(worst, tk.fit[c] ? (biased ? e1 : err[c]) : 0.0f);
+    tk.kept[c] = tk.fit[c];
   }
-  bool fit0[C], open = false, groups_open = false;
-#pragma unroll
-  for (int c = 0; c < C; ++c) fit0[c] = fit[c];
+  tk.margin = 2.0f * wave_max(worst);
+  tk.group_err = p.group_best * wave_max(verr);
+  tk.groups_open = false;
   if (p.n_groups > 1) {
     const int size = p.E / p.n_groups;
-    int per = 64;
-    while (64 / per < p.n_groups) per >>= 1;
-    float* row = reinterpret_cast<float*>(lds.row);
-    float worst = 0.0f;
+    const int per = lanes_per_group(p);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      row[c * 64 + lane] = fit[c] ? val[c] : none;
-      worst = fmaxf(worst, fit[c] ? verr[c] : 0.0f);
+      tk.val[c] = tk.fit[c] ? (biased ? tk.key[c] : sc[c]) : none;
+      row[c * 64 + lane] = tk.val[c];
     }
     wave_lds_fence();
-    worst = wave_max(worst);
     const int g = lane / per;
-    const GroupBest<float> gb = group_best(p, row, lane, per, g);
-    float* sums = reinterpret_cast<float*>(lds.sum);
-    if ((lane & (per - 1)) == 0) sums[g] = gb.sum;
-    wave_lds_fence();
-    const bool is = lane < p.n_groups;
-    const float mine = is ? sums[lane] : none;
+    tk.group = group_best(p, row, lane, per, g);
+    // a group's rank, in all of its lanes
     int rank = 0;
-    for (int h = 0; h < p.n_groups; ++h) rank += sums[h] > mine || (sums[h] == mine && h < lane);
-    const uint64_t kept = __ballot(is && rank < p.top_groups);
+    for (int h = 0; h < p.n_groups; ++h) {
+      const float v = lane_value(tk.group.sum, h * per);
+      rank += v > tk.group.sum || (v == tk.group.sum && h < g);
+    }
+    const bool is = g < p.n_groups;
+    tk.stays = is && rank < p.top_groups;
     // the least kept group against the best of the others
-    const float in = wave_max(is && rank < p.top_groups ? -mine : none);
-    const float out = wave_max(is && rank >= p.top_groups ? mine : none);
-    if (out > none && -in - out <= 2.0f * p.group_best * worst + 1e-6f * fmaxf(fabsf(in), fabsf(out)))
-      open = groups_open = true;
-#pragma unroll
-    for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
+    tk.in = -wave_max(tk.stays ? -tk.group.sum : none);
+    tk.out = wave_max(is && !tk.stays ? tk.group.sum : none);
+    tk.groups_open = tk.out > none && tk.in - tk.out <= 2.0f * group_margin(tk);
+    keep_groups(p, tk);
+    wave_lds_fence();
   }
-  // top-k: lane k keeps slot k
-  int sel = -1;
-  float sl = 0.0f;
-  bool want[C];
+}
+
+// Slots of the kept experts by their fp32 keys.
+template <int C>
+__device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& tk) {
+  const int lane = threadIdx.x & 63;
+  uint32_t hk[C];
+  int he[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) want[c] = false;
-  for (int k = 0; k < p.K && !groups_open; ++k) {
-    float bk = none;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (fit[c]) bk = fmaxf(bk, key[c]);
-    bk = wave_max(bk);
-    int be = -1;
+  for (int c = 0; c < C; ++c) {
+    row[c * 64 + lane] = tk.l[c];
+    hk[c] = tk.kept[c] ? float_key(tk.key[c] + 0.0f) : 0u;  // (one zero)
+    he[c] = c * 64 + lane;
+  }
+  sort_lane(hk, he);
+  tk.sel = -1;
+  uint64_t near = 0;
+  for (int k = 0; k < p.K; ++k) {
+    const uint32_t m = __builtin_amdgcn_readfirstlane(wave_max_u32(hk[0]));
+    if (m == 0) break;  // nobody left
+    const int from = __ffsll((unsigned long long)__ballot(hk[0] == m)) - 1;
+    const int e = __builtin_amdgcn_readlane(he[0], from);
+    if (lane == k) tk.sel = e;
+    const bool mine = lane == from;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint64_t m = __ballot(fit[c] && key[c] == bk);
-      if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
+      hk[c] = mine ? (c + 1 < C ? hk[c + 1] : 0u) : hk[c];
+      he[c] = mine ? (c + 1 < C ? he[c + 1] : 0) : he[c];
     }
-    if (be < 0) break;  // nobody left
-    float ml = 0.0f, me = 0.0f;
+    near |= __ballot(hk[0] >= float_key(key_float(m) - tk.margin));
+  }
+  tk.slots_open = near != 0;
+  wave_lds_fence();
+  tk.sl = tk.sel >= 0 ? row[tk.sel] : 0.0f;
+  wave_lds_fence();
+}
+
+// The groups that stay where fp32 sums leave it open: those certainly in or
+// out keep their place (for each, all of the others or enough of them are
+// certainly on the other side of it), and the rest are ranked by the sums of
+// their members that may count, in 64 bits.
+template <class T16, int C>
+__device__ void settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+  const int lane = threadIdx.x & 63;
+  const int size = p.E / p.n_groups, per = lanes_per_group(p), g = lane / per;
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  const double none = -__builtin_inf();
+  const float room = 2.0f * group_margin(tk);
+  const bool contested = g < p.n_groups && tk.group.sum > -__builtin_inff() &&
+                         (tk.stays ? tk.group.sum - tk.out <= room : tk.in - tk.group.sum <= room);
+  const uint64_t cm = __ballot(contested), sure = __ballot(tk.stays && !contested);
+  const int left = p.top_groups - __popcll(sure) / per;
+  bool want[C], again[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (be >> 6 == c) {
-        ml = __shfl(l[c], be & 63, 64);
-        me = __shfl(kerr[c], be & 63, 64);
-        if (lane == (be & 63)) fit[c] = false;
-      }
-    bool near = false;
+  for (int c = 0; c < C; ++c) {
+    const int at = min((c * 64 + lane) / size * per, 63);
+    const float low = __shfl(tk.group.low, at, 64);
+    want[c] = tk.fit[c] && (cm >> at & 1) && tk.val[c] >= low - room;
+    again[c] = want[c] && !tk.exact[c];
+  }
+  double l[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (fit[c] && bk - key[c] <= me + kerr[c]) near = want[c] = true;
-    if (__ballot(near)) {
-      open = true;
+  for (int c = 0; c < C; ++c) l[c] = tk.l[c];
+  sum_again(p, xr, again, lds, [&](int c, int at, double v) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) want[c] |= c * 64 + lane == be;
-    }
-    if (lane == k) {
-      sel = be;
-      sl = ml;
+    for (int i = 0; i < C; ++i)
+      if (i == c && lane == at) l[i] = v;
+  });
+  if (threadIdx.x < 64) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      // (a softmax's denominator is common to all groups without a bias)
+      const double sc = soft ? exp(l[c] - tk.top) : 1.0 / (1.0 + exp(-l[c]));
+      lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
     }
   }
-  if (open) select_exact<T16, C>(p, x + (int64_t)t * p.d, l, fit0, b, want, xn, rel, lds, sel, sl);
-  // weights: the share of the selected scores by their logarithms, so that
-  // scores that underflow still have their ratios
+  __syncthreads();
+  const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
+  int rank = 0;
+  for (int h = 0; h < p.n_groups; ++h) {
+    if (!(cm >> (h * per) & 1)) continue;
+    const double v = lane_value(gb.sum, h * per);
+    rank += v > gb.sum || (v == gb.sum && h < g);
+  }
+  tk.stays = (sure >> lane & 1) || (contested && rank < left);
+  keep_groups(p, tk);
+  __syncthreads();
+}
+
+// The order of the slots where only neighbours of it are open: the experts
+// within the margin of a slot's key are summed again, and those and the other
+// slots ranked anew, a lane each.  Every expert outside is certainly below
+// all slots.  False where this does not decide: too many experts, or a
+// softmax's denominator that is not known well enough.
+template <class T16, int C>
+__device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+  const int lane = threadIdx.x & 63;
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  bool want[C], slot[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) want[c] = slot[c] = false;
+  for (int k = 0; k < p.K; ++k) {
+    const int e = __builtin_amdgcn_readlane(tk.sel, k);
+    if (e < 0) break;
+    float ke = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
+    uint64_t near = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const bool self = c * 64 + lane == e;
+      const bool n = tk.kept[c] && !self && fabsf(tk.key[c] - ke) <= tk.margin;
+      want[c] |= n;
+      slot[c] |= self;
+      near |= __ballot(n);
+    }
+    if (near) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] |= c * 64 + lane == e;
+    }
+  }
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) n += __popcll(__ballot(want[c] || slot[c]));
+  if (n > 32) return false;
+  bool again[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) again[c] = want[c] && !tk.exact[c];
+  // lane u: member u, its logit and bias
+  int me = -1, at = 0;
+  double ml = 0.0;
+  float mb = 0.0f;
+  const auto add = [&](int c, int j, double v) {
+    float bj = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (i == c) bj = lane_value(tk.b[i], j);
+    if (lane == at) {
+      me = c * 64 + j;
+      ml = v;
+      mb = bj;
+    }
+    ++at;
+  };
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    uint64_t m = __ballot((slot[c] || want[c]) && !again[c]);
+    for (; m; m &= m - 1) {
+      const int j = __ffsll((unsigned long long)m) - 1;
+      add(c, j, lane_value(tk.l[c], j));
+    }
+  }
+  sum_again(p, xr, again, lds, add);
+  double s = 0.0, k = ml;
+  if (biased) {
+    s = soft ? exp(ml - tk.top) / tk.z : 1.0 / (1.0 + exp(-ml));
+    k = s + mb;
+  }
+  const bool in = lane < n;
+  int rank = 0;
+  bool unsure = false;
+  for (int u = 0; u < n; ++u) {
+    const double ku = lane_value(k, u), su = lane_value(s, u);
+    const int eu = __builtin_amdgcn_readlane(me, u);
+    rank += ku > k || (ku == k && eu < me);
+    unsure |= soft && biased && u != lane && fabs(ku - k) <= 1.01 * tk.zrel * fabs(su - s);
+  }
+  if (__ballot(in && unsure)) return false;
+  const int K = min(p.K, n);
+  tk.sel = -1;
+  for (int r = 0; r < K; ++r) {
+    const int u = __ffsll((unsigned long long)__ballot(in && rank == r)) - 1;
+    const int e = __builtin_amdgcn_readlane(me, u);
+    const float v = (float)lane_value(ml, u);
+    if (lane == r) {
+      tk.sel = e;
+      tk.sl = v;
+    }
+  }
+  return true;
+}
+
+// Weights and outputs of token t from its selection, by one wave.  counts: the
+// block's, in LDS.
+template <int C>
+__device__ inline void finish(const RouterParams& p, int t, const Token<C>& tk, const RouterOut& o,
+                              int32_t* counts) {
+  const int lane = threadIdx.x & 63;
+  const float none = -__builtin_inff();
+  const bool soft = p.score == SCORE_SOFTMAX;
+  // the share of the selected scores by their logarithms, so that scores that
+  // underflow still have their ratios
+  const int sel = tk.sel;
   const bool have = sel >= 0;
-  const float ls = !have ? none : soft ? sl : log_sigmoid(sl);
+  const float ls = !have ? none : soft ? tk.sl : log_sigmoid(tk.sl);
   const float lm = wave_max(ls);  // (by every lane of the wave)
   const float ex = have ? expf(ls - lm) : 0.0f;
   const float sum = wave_sum_dpp(ex);
   const float share = have ? ex / sum : 0.0f;
   float w = share;
-  if (!p.renorm) w = !have ? 0.0f : soft ? expf(sl - top) / z : 1.0f / (1.0f + expf(-sl));
+  if (!p.renorm) w = !have ? 0.0f : soft ? expf(tk.sl - tk.top) / tk.z : 1.0f / (1.0f + expf(-tk.sl));
   w *= p.scale;
   // Eq. 2 over the shares: the score of a slot is the sum of those above it
   int prec = PREC_SKIP;
@@ -716,7 +973,7 @@ __global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p,
     float above = 0.0f;
     bool first = true;
     for (int j = 0; j < p.K; ++j) {
-      const float sj = __shfl(share, j, 64);
+      const float sj = lane_value(share, j);
       if (sj > share || (sj == share && j < lane)) {
         above += sj;
         first = false;
@@ -737,8 +994,88 @@ __global__ __launch_bounds__(kThreads) void router_select_kernel(RouterParams p,
     if (o.user_idx) o.user_idx[i] = sel;
     if (o.user_w) o.user_w[i] = w;
     if (o.user_prec) o.user_prec[i] = (int8_t)prec;
-    if (o.count && have) atomicAdd(o.count + sel, 1);
+    if (o.count && have) atomicAdd(&counts[sel], 1);
   }
+}
+
+// The block's counts into the call's, by neighbouring lanes: one request per
+// line.  (An atomic per slot on these few lines took 21 us for 1337 tokens of
+// 4 slots.)
+__device__ inline void add_counts(const RouterParams& p, const RouterOut& o, const int32_t* counts) {
+  if (!o.count) return;
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x)
+    if (counts[e]) atomicAdd(o.count + e, counts[e]);
+}
+
+// A token per wave in turn; tokens whose selection fp32 leaves open go on a
+// list.  Few blocks of many waves, so that few of them add to the counts.
+constexpr int kManyThreads = 1024;
+constexpr int kManyWaves = kManyThreads / 64;
+constexpr int kManyBlocks = 256;
+template <int C>
+__global__ __launch_bounds__(kManyThreads) void router_select_kernel(RouterParams p, int T,
+                                                                     const float* __restrict__ lg,
+                                                                     float rel, RouterOut o) {
+  __shared__ float rows[kManyWaves][C * 64];
+  __shared__ int32_t counts[C * 64];
+  __shared__ int32_t n_open, first_open, opens[kManyThreads];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (threadIdx.x == 0) n_open = 0;
+  if (o.count)
+    for (int e = threadIdx.x; e < C * 64; e += kManyThreads) counts[e] = 0;
+  __syncthreads();
+  // (at most 65536 / (16 * 256) = 16 tokens a wave, one slot of opens each)
+  for (int t = blockIdx.x * kManyWaves + wave; t < T; t += gridDim.x * kManyWaves) {
+    Token<C> tk;
+    score_token(p, t, lg, global<float>(p.x_norm)[t], rel, rows[wave], tk);
+    take_slots(p, rows[wave], tk);
+    if (!tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
+    else if ((threadIdx.x & 63) == 0) opens[atomicAdd(&n_open, 1)] = t;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && n_open) first_open = atomicAdd(p.open, n_open);
+  __syncthreads();
+  if ((int)threadIdx.x < n_open) p.open[1 + first_open + threadIdx.x] = opens[threadIdx.x];
+  add_counts(p, o, counts);
+}
+
+// A token per block: the call's, or those of the list.  Every wave makes the
+// same selection; where it is open they share the sums in 64 bits.
+constexpr int kOneThreads = 256;
+constexpr int kListBlocks = 768;
+template <class T16, int C>
+__global__ __launch_bounds__(kOneThreads) void router_select_open_kernel(RouterParams p, int T, int listed,
+                                                                         const T16* __restrict__ x,
+                                                                         const float* __restrict__ lg,
+                                                                         float rel, RouterOut o) {
+  __shared__ float rows[kOneThreads / 64][C * 64];
+  __shared__ OpenLds<C> lds;
+  __shared__ int32_t counts[C * 64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[0]) : T;
+  if ((int)blockIdx.x >= n) return;
+  if (o.count) {
+    for (int e = threadIdx.x; e < C * 64; e += kOneThreads) counts[e] = 0;
+    __syncthreads();
+  }
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int t = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[1 + i]) : i;
+    const float xn = global<float>(p.x_norm)[t];
+    const T16* xr = x + (int64_t)t * p.d;
+    Token<C> tk;
+    score_token(p, t, lg, xn, rel, rows[wave], tk);
+    // (scores that share an uncertain denominator beside biases that do not)
+    bool open = tk.groups_open && p.bias && p.score == SCORE_SOFTMAX;
+    if (!open) {
+      if (tk.groups_open) settle_groups(p, xr, tk, lds);
+      take_slots(p, rows[wave], tk);
+      if (tk.slots_open) open = !select_slots(p, xr, tk, lds);
+    }
+    if (open) select_exact(p, xr, tk, xn, rel, lds);
+    if (wave == 0) finish(p, t, tk, o, counts);
+  }
+  add_counts(p, o, counts);
 }
 
 template <class T16, int MT, int NT, int NW>
@@ -774,11 +1111,23 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, h
   else if (blocks(16, 32) >= kEnough) e = logits<T16, 1, 2, 8>(p, T, x, lg, o.count, &rel, s);
   else e = logits<T16, 1, 1, 8>(p, T, x, lg, o.count, &rel, s);
   if (e != hipSuccess) return e;
-  const int grid = (T + kWaves - 1) / kWaves;
-  if (p.E <= 64) router_select_kernel<T16, 1><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
-  else if (p.E <= 128) router_select_kernel<T16, 2><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
-  else if (p.E <= 256) router_select_kernel<T16, 4><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
-  else router_select_kernel<T16, 8><<<grid, kThreads, 0, s>>>(p, T, x, lg, rel, o);
+  // Up to kFew tokens a block each, in one launch; more a wave each, and the
+  // open ones a block each in another.
+  constexpr int kFew = 256;
+  const int C = p.E <= 64 ? 1 : p.E <= 128 ? 2 : p.E <= 256 ? 4 : 8;
+  if (T > kFew) {
+    const int blocks = (T + kManyWaves - 1) / kManyWaves, grid = blocks < kManyBlocks ? blocks : kManyBlocks;
+    if (C == 1) router_select_kernel<1><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
+    else if (C == 2) router_select_kernel<2><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
+    else if (C == 4) router_select_kernel<4><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
+    else router_select_kernel<8><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const int listed = T > kFew, grid = listed ? kListBlocks : T;
+  if (C == 1) router_select_open_kernel<T16, 1><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
+  else if (C == 2) router_select_open_kernel<T16, 2><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
+  else if (C == 4) router_select_open_kernel<T16, 4><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
+  else router_select_open_kernel<T16, 8><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
   return hipGetLastError();
 }
 
