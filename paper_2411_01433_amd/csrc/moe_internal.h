@@ -274,7 +274,7 @@ struct RouterParams {
   float* x_norm;           // [T] bounds of the rows' norms
   float* w_norm;           // [E]
   int32_t* open;           // [1 + T] number and list of tokens whose selection is open
-  float* d_logits;         // [T, E], routers with a backward pass
+  void* grad_ws;           // router_backward_bytes, routers with a backward pass
 };
 
 // Outputs of one routing; what is null is not written.
@@ -323,6 +323,7 @@ hipError_t launch_worklist(const RouteParams& p, RouteOut o, WorkList* wl, int32
                            int32_t* pos, hipStream_t s);
 hipError_t launch_router(const RouterParams& p, int T, const void* x, const RouterOut& o,
                          hipStream_t s);
+size_t router_backward_bytes(int type, int T, int d, int E);
 hipError_t launch_router_backward(const RouterParams& p, int T, const void* x,
                                   const float* logits, const int32_t* idx, const float* dw,
                                   const float* dl, void* dx, float* dwg, hipStream_t s);

@@ -154,7 +154,8 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
   const size_t o_xn = off; off += al(sizeof(float) * desc->max_tokens);
   const size_t o_wn = off; off += al(sizeof(float) * desc->n_experts);
   const size_t o_open = off; off += al(sizeof(int32_t) * (1 + (size_t)desc->max_tokens));
-  const size_t o_dl = off; off += r->backward ? al(rows * sizeof(float)) : 0;
+  const size_t o_grad = off;
+  if (r->backward) off += router_backward_bytes(p.type, desc->max_tokens, p.d, p.E);
   he = hipMalloc(&r->arena, off);
   if (he != hipSuccess) {
     delete r;
@@ -165,7 +166,7 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
   p.x_norm = reinterpret_cast<float*>(base + o_xn);
   p.w_norm = reinterpret_cast<float*>(base + o_wn);
   p.open = reinterpret_cast<int32_t*>(base + o_open);
-  p.d_logits = r->backward ? reinterpret_cast<float*>(base + o_dl) : nullptr;
+  p.grad_ws = r->backward ? base + o_grad : nullptr;
   {
     std::lock_guard<std::mutex> g(g_router_mu);
     g_router_live.insert(r);
