@@ -48,11 +48,6 @@ __device__ inline const __attribute__((address_space(1))) T* global(const void* 
 
 __device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 
-__device__ inline float wave_max_f(float v) {
-  for (int m = 1; m < 64; m <<= 1) v = fmaxf(v, __shfl_xor(v, m, 64));
-  return v;
-}
-
 // Fragments.  A product of 32 terms takes 8 numbers from each of 64 lanes:
 // lane l has row (or column) l & 15 and the terms 4 g .. 4 g + 3 and 16 + 4 g
 // .. 16 + 4 g + 3 of its group g = l >> 4, which is what two transposing reads
@@ -73,9 +68,37 @@ __device__ inline T16 next_part(float& left) {
   return h;
 }
 
-// Gradient of the logits of 64 tokens, and its fragments.  A wave per token in
-// turn: lane k has slot k, lane i the experts i, i + 64, ...
+// Sum and maximum over the 16 lanes of a row, in each of them.
+__device__ inline float row_sum(float v) {
+  v += dpp_f<0xB1>(v);
+  v += dpp_f<0x4E>(v);
+  v += dpp_f<0x141>(v);
+  return v + dpp_f<0x140>(v);
+}
+__device__ inline float row_max(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  return fmaxf(v, dpp_f<0x140>(v));
+}
+__device__ inline float wave_max_f(float v) {
+  v = row_max(v);
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ inline float lane_value(float v, int from) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), from));
+}
+__device__ inline void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Gradient of the logits of 64 tokens, and its fragments.  A wave has four
+// tokens: 16 lanes each for their slots, all lanes for their rows of experts.
 constexpr int kLogitThreads = 1024;
+constexpr int kWaveTokens = kGroupTokens / (kLogitThreads / 64);
+static_assert(kWaveTokens * 16 == 64 && kRouterMaxTopK <= 16, "a lane per slot");
 template <class T16, int C>
 __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     RouterParams p, int T, const float* __restrict__ logits, const int32_t* __restrict__ idx,
@@ -89,72 +112,99 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
   const int Ep = (p.E + 31) & ~31;
   const bool sig = p.score == SCORE_SIGMOID, full = !p.renorm && !sig;
   const float none = -__builtin_inff();
-  float most = 0.0f;
-  for (int i = wave; i < kGroupTokens; i += kLogitThreads / 64) {
-    const int t = blockIdx.x * kGroupTokens + i;
-    float row[C];
-    int e = -1;
-    float slot = 0.0f, mean = 0.0f, all = 1.0f;
-    if (t < T) {
-      const float* lr = logits + (int64_t)t * p.E;
-      float g = 0.0f, l = none;
-      if (lane < p.K) {
-        e = idx[(int64_t)t * p.K + lane];
-        if (e >= 0 && e < p.E) l = lr[e];
-        if (finite(l)) g = p.scale * dw[(int64_t)t * p.K + lane];
-        else e = -1;
+  const int t0 = blockIdx.x * kGroupTokens + wave * kWaveTokens;   // the wave's first token
+  const int mi = lane >> 4, k = lane & 15;                         // this lane's token and slot
+  // slots
+  int e = -1;
+  float up = 0.0f, l = none;
+  if (t0 + mi < T && k < p.K) {
+    const int64_t at = (int64_t)(t0 + mi) * p.K + k;
+    e = idx[at];
+    if (e >= 0 && e < p.E) l = logits[(int64_t)(t0 + mi) * p.E + e];
+    if (finite(l)) up = p.scale * dw[at];
+    else e = -1;
+  }
+  const bool have = e >= 0;
+  // softmax of all experts: the rows' exponentials and sums
+  float ex[kWaveTokens][C], top = 0.0f, all = 1.0f;
+  if (full) {
+#pragma unroll
+    for (int i = 0; i < kWaveTokens; ++i) {
+      float most = none, sum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int ee = c * 64 + lane;
+        ex[i][c] = t0 + i < T && ee < p.E ? logits[(int64_t)(t0 + i) * p.E + ee] : none;
+        if (finite(ex[i][c])) most = fmaxf(most, ex[i][c]);
       }
-      const bool have = e >= 0;
-      // z = exp(-|l|): s and 1 - s without loss on either side
-      const float z = expf(-fabsf(l));
-      const float not_s = have ? (l >= 0.0f ? z : 1.0f) / (1.0f + z) : 0.0f;
-      const float s = have ? (l >= 0.0f ? 1.0f : z) / (1.0f + z) : 0.0f;
-      if (p.renorm) {
-        const float ls = !have ? none : sig ? fminf(l, 0.0f) - log1pf(z) : l;
-        const float lm = wave_max_f(ls);
-        const float ex = have ? expf(ls - lm) : 0.0f;
-        const float sum = wave_sum_dpp(ex);
-        const float share = have ? ex / sum : 0.0f;
-        mean = wave_sum_dpp(g * share);
-        slot = share * (g - mean) * (sig ? not_s : 1.0f);
-      } else if (sig) {
-        slot = g * s * not_s;
-      } else {
-        float top = none;
-        all = 0.0f;
+      most = wave_max_f(most);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int ee = c * 64 + lane;
-          row[c] = ee < p.E ? lr[ee] : none;
-          if (finite(row[c])) top = fmaxf(top, row[c]);
-        }
-        top = wave_max_f(top);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          row[c] = finite(row[c]) ? expf(row[c] - top) : 0.0f;
-          all += row[c];
-        }
-        all = wave_sum_dpp(all);
-        const float pk = have ? expf(l - top) / all : 0.0f;
-        mean = wave_sum_dpp(g * pk);
-        slot = g * pk;
+      for (int c = 0; c < C; ++c) {
+        ex[i][c] = finite(ex[i][c]) ? expf(ex[i][c] - most) : 0.0f;
+        sum += ex[i][c];
+      }
+      sum = wave_sum_dpp(sum);
+      if (mi == i) {
+        top = most;
+        all = sum;
       }
     }
+  }
+  // z = exp(-|l|): s and 1 - s without loss on either side
+  const float z = expf(-fabsf(l));
+  const float not_s = have ? (l >= 0.0f ? z : 1.0f) / (1.0f + z) : 0.0f;
+  const float sc = have ? (l >= 0.0f ? 1.0f : z) / (1.0f + z) : 0.0f;
+  float slot, mean = 0.0f;
+  if (p.renorm) {
+    const float ls = !have ? none : sig ? fminf(l, 0.0f) - log1pf(z) : l;
+    const float lm = row_max(ls);
+    const float v = have ? expf(ls - lm) : 0.0f;
+    const float sum = row_sum(v);
+    const float share = have ? v / sum : 0.0f;
+    mean = row_sum(up * share);
+    slot = share * (up - mean) * (sig ? not_s : 1.0f);
+  } else if (sig) {
+    slot = up * sc * not_s;
+  } else {
+    slot = have ? up * (expf(l - top) / all) : 0.0f;
+    mean = row_sum(slot);
+  }
+  // rows: what every expert gets, then the slots on top
+#pragma unroll
+  for (int i = 0; i < kWaveTokens; ++i) {
+    const float by = full ? -lane_value(mean, 16 * i) / lane_value(all, 16 * i) : 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int ee = c * 64 + lane;
-      float v = t < T && full && row[c] > 0.0f ? -mean * (row[c] / all) : 0.0f;
-      for (int k = 0; k < p.K; ++k) {
-        const int ek = __builtin_amdgcn_readlane(e, k);
-        const float gk = __builtin_bit_cast(
-            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, slot), k));
-        if (ek == ee) v += gk;
-      }
-      if (dl && t < T && ee < p.E) v += dl[(int64_t)t * p.E + ee];
-      if (finite(v)) most = fmaxf(most, fabsf(v));
-      rows[i][ee] = v;
+      float v = full && ex[i][c] > 0.0f ? by * ex[i][c] : 0.0f;
+      if (dl && t0 + i < T && ee < p.E) v += dl[(int64_t)(t0 + i) * p.E + ee];
+      rows[wave * kWaveTokens + i][ee] = v;
     }
   }
+  wave_lds_fence();
+  float* row = rows[wave * kWaveTokens + mi];
+  bool twice = false;  // an expert in two slots of a token: these in their order
+  for (int j = 0; j < p.K; ++j) {
+    const int ej = __shfl(e, (lane & 48) + j, 64);
+    twice |= j < k && have && ej == e;
+  }
+  if (!__ballot(twice)) {
+    if (have) row[e] += slot;
+  } else {
+    for (int j = 0; j < p.K; ++j) {
+      if (have && k == j) row[e] += slot;
+      wave_lds_fence();
+    }
+  }
+  wave_lds_fence();
+  float most = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWaveTokens; ++i)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const float v = rows[wave * kWaveTokens + i][c * 64 + lane];
+      if (finite(v)) most = fmaxf(most, fabsf(v));
+    }
   most = wave_max_f(most);
   if (lane == 0) tops[wave] = most;
   __syncthreads();
@@ -202,10 +252,18 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
 
 constexpr int kCols = 128;   // columns of d per block of the products
 
-// LDS tile of 16-bit rows of kCols columns, 256 bytes each: 64-byte block b of
-// a row r lies at block b ^ (r & 3), so that the four rows that 16 lanes of a
-// transposing read touch lie in different banks.
-__device__ inline int tile_at(int row, int byte) { return row * 256 + (byte ^ ((row & 3) << 6)); }
+// LDS tile of 16-bit rows of kCols columns, 256 bytes each.  A transposing
+// read takes 8 bytes of four rows for each 16 lanes: 64-byte block b of a row
+// r lies at block b ^ (r & 3), so that the four rows are in different banks,
+// and the halves of 16 bytes are exchanged where r & 4, so that the next 16
+// lanes, four rows on, are in the others.
+__device__ inline int tile_at(int row, int byte) {
+  return row * 256 + (byte ^ ((row & 3) << 6) ^ ((row & 4) << 1));
+}
+__device__ inline void tile_put(unsigned char* tile, int row, int byte, u32x4 v) {
+  const u32x4 w = row & 4 ? u32x4{v.z, v.w, v.x, v.y} : v;
+  *reinterpret_cast<u32x4*>(tile + row * 256 + (byte ^ ((row & 3) << 6))) = w;
+}
 
 typedef __attribute__((address_space(3))) s16x4* LdsRead;
 
@@ -225,12 +283,14 @@ __device__ inline typename Split<T16>::x8 read_columns(const unsigned char* tile
 
 // d_x of kCols columns: the block keeps Wg's columns in LDS (EB * 32 rows) and
 // its waves take 32 tokens each in turn.  A wave's fragment of dl is loaded
-// once and multiplied with 128 columns.  Rows of the result are columns of
+// once and multiplied with 128 columns.  Blocks that follow one another, which
+// the eight dies take in turn, have different tokens, so that a die's L2 holds
+// its tokens' dl for all columns.  Rows of the result are columns of
 // d, ordered so that a lane has 8 neighbouring ones of a token: tile 2 s + h,
 // row 4 q + r is column 32 s + 8 q + 4 h + r.
 constexpr int kDxThreads = 256;
 template <class T16, int EB>
-__global__ __launch_bounds__(kDxThreads) void router_dx_kernel(RouterParams p, int T,
+__global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p, int T,
                                                                const T16* __restrict__ fx,
                                                                const float* __restrict__ scales,
                                                                T16* __restrict__ dx) {
@@ -238,55 +298,58 @@ __global__ __launch_bounds__(kDxThreads) void router_dx_kernel(RouterParams p, i
   constexpr int kX = Split<T16>::kX;
   __shared__ __attribute__((aligned(16))) unsigned char tile[EB * 32 * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = blockIdx.x * kCols, eb_n = (p.E + 31) / 32;
-  for (int v = threadIdx.x; v < eb_n * 32 * 16; v += kDxThreads) {
-    const int e = v >> 4, c = v & 15;
-    u32x4 w = {0, 0, 0, 0};
-    if (e < p.E && n0 + c * 8 < p.d)
-      w = *global<u32x4>(static_cast<const T16*>(p.wg) + (int64_t)e * p.d + n0 + c * 8);
-    *reinterpret_cast<u32x4*>(tile + tile_at(e, c * 16)) = w;
+  const int n0 = blockIdx.y * kCols, eb_n = (p.E + 31) / 32;
+  constexpr int kAhead = EB < 4 ? EB * 2 : 8;   // rows of a thread on their way
+  const int c16 = threadIdx.x & 15;
+  for (int e0 = threadIdx.x >> 4; e0 < eb_n * 32; e0 += kAhead * 16) {
+    u32x4 w[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int e = e0 + i * 16;
+      const bool in = e < p.E && n0 + c16 * 8 < p.d;
+      w[i] = in ? *global<u32x4>(static_cast<const T16*>(p.wg) + (int64_t)e * p.d + n0 + c16 * 8)
+                : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (e0 + i * 16 < eb_n * 32) tile_put(tile, e0 + i * 16, c16 * 16, w[i]);
   }
   __syncthreads();
   const int q = lane & 3, g = lane >> 4;
-  for (int w32 = blockIdx.y * 4 + wave; w32 * 32 < T; w32 += gridDim.y * 4) {
-    f32x4 acc[2][8];
+  // steps of 32 experts through the wave's tiles of 32 tokens, one after
+  // another; dl's fragments three steps ahead, Wg's one
+  const int first = blockIdx.x * 4 + wave, every = gridDim.x * 4, all = (T + 31) / 32;
+  const int steps = first < all ? ((all - first + every - 1) / every) * eb_n : 0;
+  f32x4 acc[2][8];
+  x8 a[2][8], b[4][2][kX];
+  const auto zero = [&]() {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    const auto frag = [&](int i, int eb, int part) {
-      return global<x8>(fx)[(((int64_t)(w32 * 2 + i) * eb_n + eb) * kX + part) * 64 + lane];
-    };
-    x8 b[2][kX];
+  };
+  int load_at = first, load_eb = 0;
+  const auto load_dl = [&](x8 (&bv)[2][kX]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int part = 0; part < kX; ++part) b[i][part] = frag(i, 0, part);
-    for (int eb = 0; eb < eb_n; ++eb) {
-      x8 next[2][kX];
-      const int en = min(eb + 1, eb_n - 1);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int part = 0; part < kX; ++part) next[i][part] = frag(i, en, part);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const x8 a = read_columns<T16>(tile, eb * 32, (j >> 1) * 64 + q * 16 + (j & 1) * 8);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int part = 0; part < kX; ++part) acc[i][j] = mfma(a, b[i][part], acc[i][j]);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int part = 0; part < kX; ++part) b[i][part] = next[i][part];
+      for (int part = 0; part < kX; ++part)
+        bv[i][part] = global<x8>(fx)[(((int64_t)(load_at * 2 + i) * eb_n + load_eb) * kX + part) * 64 + lane];
+    if (++load_eb == eb_n) {
+      load_eb = 0;
+      if (load_at + every < all) load_at += every;  // (past the last tile: that one again)
     }
+  };
+  const auto load_wg = [&](int eb, x8 (&av)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      av[j] = read_columns<T16>(tile, eb * 32, (j >> 1) * 64 + q * 16 + (j & 1) * 8);
+  };
+  const auto write = [&](int w32) {
     const float s = global<float>(scales)[w32 * 32 / kGroupTokens];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int t = w32 * 32 + i * 16 + (lane & 15);
-      if (t >= T) continue;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = n0 + k * 32 + g * 8;
@@ -296,7 +359,36 @@ __global__ __launch_bounds__(kDxThreads) void router_dx_kernel(RouterParams p, i
           o[r] = (T16)(acc[i][2 * k][r] * s);
           o[r + 4] = (T16)(acc[i][2 * k + 1][r] * s);
         }
-        if (c < p.d) *reinterpret_cast<x8*>(dx + (int64_t)t * p.d + c) = o;
+        if (t < T && c < p.d) *reinterpret_cast<x8*>(dx + (int64_t)t * p.d + c) = o;
+      }
+    }
+  };
+  if (steps == 0) return;
+#pragma unroll
+  for (int u = 0; u < 3; ++u) load_dl(b[u]);
+  load_wg(0, a[0]);
+  zero();
+  int w32 = first, eb = 0;
+  for (int s0 = 0; s0 < steps; s0 += 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (s0 + u < steps) {
+        const int next = eb + 1 < eb_n ? eb + 1 : 0;
+        load_dl(b[(u + 3) & 3]);
+        load_wg(next, a[(u + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int part = 0; part < kX; ++part)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[i][j] = mfma(a[u & 1][j], b[u][i][part], acc[i][j]);
+        if (next == 0) {
+          write(w32);
+          zero();
+          w32 += every;
+        }
+        eb = next;
       }
     }
   }
@@ -317,21 +409,25 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
   typedef typename Split<T16>::x8 x8;
   constexpr int WT = 8 / WE, kW = Split<T16>::kW;
   constexpr int kLoads = 16 / WE;   // 16-byte chunks of 64 rows per thread of a set
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[WT][kGroupTokens * 256];
+  // a turn's fragments of dl during the turn before, where registers allow
+  constexpr bool kDlAhead = WE >= 4;
+  constexpr int kTiles = WT <= 4 ? 2 : 1;  // two tiles in turn where LDS holds them
+  __shared__ __attribute__((aligned(16))) unsigned char tiles[kTiles][WT][kGroupTokens * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int we = wave % WE, wt = wave / WE, set = blockIdx.z * WT + wt, sets = gridDim.z * WT;
-  const int n0 = blockIdx.x * kCols;
-  const int ET = ((p.E + 31) & ~31) / 16, et = blockIdx.y * 16 + we * 2;
+  const int we = wave % WE, wt = wave / WE, set = blockIdx.x * WT + wt, sets = gridDim.x * WT;
+  const int n0 = blockIdx.y * kCols;
+  const int ET = ((p.E + 31) & ~31) / 16, et = blockIdx.z * 16 + we * 2;
   const int groups = (T + kGroupTokens - 1) / kGroupTokens, turns = (groups + sets - 1) / sets;
   const bool mine = et < ET;
-  unsigned char* tile = tiles[wt];
   f32x4 acc[2][8];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   u32x4 ahead[kLoads];
-  const auto load = [&](int turn) {
+  x8 b[2][2][kW];   // [32 tokens][16 experts][part]
+  float s = 0.0f;
+  const auto load_x = [&](int turn) {
     const int t0 = (turn * sets + set) * kGroupTokens;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -340,40 +436,76 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
       ahead[i] = t < T && c < p.d ? *global<u32x4>(x + (int64_t)t * p.d + c) : u32x4{0, 0, 0, 0};
     }
   };
-  load(0);
-  for (int turn = 0; turn < turns; ++turn) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int v = (i * WE + we) * 64 + lane;
-      *reinterpret_cast<u32x4*>(tile + tile_at(v >> 4, (v & 15) * 16)) = ahead[i];
-    }
-    __syncthreads();
-    if (turn + 1 < turns) load(turn + 1);
-    const int group = turn * sets + set;
-    if (!mine || group >= groups) continue;
-    const float s = global<float>(scales)[group];
-    x8 b[2][2][kW];   // [32 tokens][16 experts][part]
+  const auto load_dl = [&](int turn) {
+    const int group = min(turn * sets + set, groups - 1), tile_e = min(et, ET - 2);
+    s = global<float>(scales)[group];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int part = 0; part < kW; ++part)
-          b[k][i][part] = global<x8>(fw)[(((int64_t)(group * 2 + k) * ET + et + i) * kW + part) * 64 + lane];
+          b[k][i][part] = global<x8>(fw)[(((int64_t)(group * 2 + k) * ET + tile_e + i) * kW + part) * 64 + lane];
+  };
+  load_x(0);
+  if (kDlAhead) load_dl(0);
+  for (int turn = 0; turn < turns; ++turn) {
+    unsigned char* tile = tiles[turn % kTiles][wt];
+    if (kTiles == 1) __syncthreads();   // (the last turn's reads)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      f32x4 sum[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (int i = 0; i < kLoads; ++i) {
+      const int v = (i * WE + we) * 64 + lane;
+      tile_put(tile, v >> 4, (v & 15) * 16, ahead[i]);
+    }
+    load_x(turn + 1);
+    if (!kDlAhead) load_dl(turn);
+    __syncthreads();
+    x8 now[2][2][kW];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const x8 a = read_columns<T16>(tile, k * 32, j * 32 + (lane & 3) * 8);
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int part = 0; part < kW; ++part)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) sum[i] = mfma(a, b[k][i][part], sum[i]);
+        for (int part = 0; part < kW; ++part) now[k][i][part] = b[k][i][part];
+    const float by = s;
+    if (kDlAhead) load_dl(turn + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if (!mine || turn * sets + set >= groups) continue;
+    // two tiles of 16 columns at a time, four sums that do not wait for one
+    // another; the next two's fragments of x are read meanwhile, and the last
+    // two's sums added
+    x8 a[2][2][2];   // [turn][tile][32 tokens]
+    f32x4 sum[2][2][2];
+    const auto read = [&](int j, x8 (&av)[2][2]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          av[h][k] = read_columns<T16>(tile, k * 32, (j * 2 + h) * 32 + (lane & 3) * 8);
+    };
+    read(0, a[0]);
+#pragma unroll
+    for (int j = 0; j < 5; ++j) {
+      if (j < 3) read(j + 1, a[(j + 1) & 1]);
+      if (j < 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int part = 0; part < kW; ++part)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                sum[j & 1][h][i] = mfma(a[j & 1][h][k], now[k][i][part],
+                                        k == 0 && part == 0 ? f32x4{0, 0, 0, 0} : sum[j & 1][h][i]);
       }
+      if (j > 0) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i][j] += s * sum[i];
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[i][(j - 1) * 2 + h] += by * sum[(j - 1) & 1][h][i];
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   if (!mine) return;
@@ -389,16 +521,24 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
   }
 }
 
-// Sum of n partial sums in their order.
+// Sum of n partial sums: a wave each for every fourth of them, then theirs in
+// order.
 constexpr int kJoinThreads = 256;
 __global__ __launch_bounds__(kJoinThreads) void router_join_kernel(const float* __restrict__ part,
                                                                    int n, int64_t size,
                                                                    float* __restrict__ out) {
-  const int64_t i = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) * 4;
-  if (i >= size) return;
-  f32x4 s = *reinterpret_cast<const f32x4*>(part + i);
-  for (int k = 1; k < n; ++k) s += *reinterpret_cast<const f32x4*>(part + k * size + i);
-  *reinterpret_cast<f32x4*>(out + i) = s;
+  __shared__ f32x4 sums[3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t i = ((int64_t)blockIdx.x * 64 + lane) * 4;
+  f32x4 s = {0, 0, 0, 0};
+  if (i < size) {
+#pragma unroll 4
+    for (int k = wave; k < n; k += 4) s += *reinterpret_cast<const f32x4*>(part + k * size + i);
+  }
+  if (wave) sums[wave - 1][lane] = s;
+  __syncthreads();
+  if (wave == 0 && i < size)
+    *reinterpret_cast<f32x4*>(out + i) = s + sums[0][lane] + sums[1][lane] + sums[2][lane];
 }
 
 // Waves over the experts of a block of d_Wg, and the blocks over the tokens:
@@ -434,7 +574,7 @@ template <class T16, int EB>
 void dx_launch(const RouterParams& p, int T, const T16* fx, const float* scales, T16* dx, hipStream_t s) {
   // about two blocks per compute unit, 128 tokens a block and turn
   const int cols = (p.d + kCols - 1) / kCols, turns = (T + 127) / 128, want = (512 + cols - 1) / cols;
-  router_dx_kernel<T16, EB><<<dim3(cols, want < turns ? want : turns), kDxThreads, 0, s>>>(p, T, fx, scales, dx);
+  router_dx_kernel<T16, EB><<<dim3(want < turns ? want : turns, cols), kDxThreads, 0, s>>>(p, T, fx, scales, dx);
 }
 
 template <class T16>
@@ -463,7 +603,7 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
   }
   if (!dwg) return hipSuccess;
   const int we = dw_waves(p.E), splits = dw_splits(T, p.d, p.E), sets = splits * (8 / we);
-  const dim3 grid_w((p.d + kCols - 1) / kCols, (p.E + 255) / 256, splits);
+  const dim3 grid_w(splits, (p.d + kCols - 1) / kCols, (p.E + 255) / 256);
   float* to = sets == 1 ? dwg : part;
   if (we == 1) router_dw_kernel<T16, 1><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
   else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
@@ -471,7 +611,7 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
   else router_dw_kernel<T16, 8><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
   if ((e = hipGetLastError()) != hipSuccess || sets == 1) return e;
   const int64_t size = (int64_t)p.E * p.d;
-  router_join_kernel<<<(unsigned)((size / 4 + kJoinThreads - 1) / kJoinThreads), kJoinThreads, 0, s>>>(part, sets, size, dwg);
+  router_join_kernel<<<(unsigned)((size / 4 + 63) / 64), kJoinThreads, 0, s>>>(part, sets, size, dwg);
   return hipGetLastError();
 }
 
