@@ -17,7 +17,7 @@ namespace {
 constexpr int kPieces = 4;  // float4 pieces of a row per thread
 
 // Threads of a row's block: d <= 16 columns per thread.
-__host__ __device__ inline int row_threads(int d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : 1024; }
+inline int row_threads(int d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
 
 template <class T16>
 __device__ inline u32x2 pack4(f32x4 v) {
@@ -56,6 +56,12 @@ __device__ inline void block_sums(float (&v)[N], float* red) {
   }
 }
 
+// Rows are read and written once: they pass the caches by.
+template <class V>
+__device__ inline V stream_in(const V* p) { return __builtin_nontemporal_load(p); }
+template <class V>
+__device__ inline void stream_out(V* p, V v) { __builtin_nontemporal_store(v, p); }
+
 __device__ inline float sum4(f32x4 v) { return (v.x + v.y) + (v.z + v.w); }
 
 template <class T16, int NT>
@@ -71,7 +77,7 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(const float* __restrict__
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) {
     const int q = threadIdx.x + i * NT;
-    v[i] = q < n4 ? hr[q] : f32x4{0, 0, 0, 0};
+    v[i] = q < n4 ? stream_in(hr + q) : f32x4{0, 0, 0, 0};
     s[0] += sum4(v[i]);
   }
   block_sums<NT, 1>(s, red[0]);
@@ -92,7 +98,7 @@ __global__ __launch_bounds__(NT) void layernorm_kernel(const float* __restrict__
       f32x4 o = v[i] * r;
       if (gain) o *= reinterpret_cast<const f32x4*>(gain)[q];
       if (bias) o += reinterpret_cast<const f32x4*>(bias)[q];
-      *reinterpret_cast<u32x2*>(x + (int64_t)blockIdx.x * d + 4 * q) = pack4<T16>(o);
+      stream_out(reinterpret_cast<u32x2*>(x + (int64_t)blockIdx.x * d + 4 * q), pack4<T16>(o));
     }
   }
 }
@@ -112,18 +118,32 @@ __global__ __launch_bounds__(NT) void layernorm_backward_kernel(
     dg[i] = db[i] = f32x4{0, 0, 0, 0};
     gn[i] = gain && q < n4 ? reinterpret_cast<const f32x4*>(gain)[q] : f32x4{1, 1, 1, 1};
   }
-  for (int t = blockIdx.x; t < T; t += gridDim.x) {
+  // a row's loads are on their way during the row before
+  f32x4 vn[kPieces];
+  u32x2 an[kPieces];
+  const auto load = [&](int t) {
     const f32x4* hr = reinterpret_cast<const f32x4*>(h + (int64_t)t * d);
     const u32x2* xr = reinterpret_cast<const u32x2*>(dx + (int64_t)t * d);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int q = threadIdx.x + i * NT;
+      vn[i] = q < n4 ? stream_in(hr + q) : f32x4{0, 0, 0, 0};
+      an[i] = q < n4 ? stream_in(xr + q) : u32x2{0, 0};
+    }
+  };
+  constexpr bool kAhead = NT < 1024;   // (where registers allow)
+  if (kAhead) load(blockIdx.x);
+  for (int t = blockIdx.x; t < T; t += gridDim.x) {
+    if (!kAhead) load(t);
     f32x4 v[kPieces], a[kPieces];
     float s[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int q = threadIdx.x + i * NT;
-      v[i] = q < n4 ? hr[q] : f32x4{0, 0, 0, 0};
-      a[i] = q < n4 ? unpack4<T16>(xr[q]) : f32x4{0, 0, 0, 0};
+      v[i] = vn[i];
+      a[i] = unpack4<T16>(an[i]);
       s[0] += sum4(v[i]);
     }
+    if (kAhead && t + (int)gridDim.x < T) load(t + gridDim.x);
     block_sums<NT, 1>(s, red[0]);
     const float mean = s[0] / (float)d;
     float m[3] = {0.0f, 0.0f, 0.0f};  // squares, a, a n (before the scale r)
@@ -148,7 +168,8 @@ __global__ __launch_bounds__(NT) void layernorm_backward_kernel(
         dg[i] += a[i] * n;
         f32x4 o = r * (a[i] * gn[i] - ma - n * mn);
         f32x4* to = reinterpret_cast<f32x4*>(dh + (int64_t)t * d) + q;
-        *to = accumulate ? *to + o : o;
+        if (accumulate) o += *to;
+        stream_out(to, o);
       }
     }
     if constexpr (NT > 64) __syncthreads();
@@ -166,22 +187,33 @@ __global__ __launch_bounds__(NT) void layernorm_backward_kernel(
   }
 }
 
-// Column sums of part[n][2 d] into d_gain and d_bias: a block takes 16
-// pieces of four columns, 16 threads of it every 16th row.
-constexpr int kSumThreads = 256;
+// Column sums of part[n][2 d] into d_gain and d_bias: a block takes 16 pieces
+// of four columns, 16 threads of it every 64th row; the 64 sums
+// are added in a fixed order.
+constexpr int kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void column_sums_kernel(const float* __restrict__ part,
                                                                   int n, int d,
                                                                   float* __restrict__ dg,
                                                                   float* __restrict__ db) {
-  __shared__ f32x4 red[16][16];
+  __shared__ f32x4 red[64][17];
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
   const int q = blockIdx.x * 16 + c, n4 = d >> 2;
   f32x4 s = {0, 0, 0, 0};
-  for (int b = g; b < n; b += 16) s += reinterpret_cast<const f32x4*>(part + (int64_t)b * 2 * d)[q];
+#pragma unroll 8
+  for (int b = g; b < n; b += 64) s += reinterpret_cast<const f32x4*>(part + (int64_t)b * 2 * d)[q];
   red[g][c] = s;
   __syncthreads();
+  // 64 sums in two steps of eight
+  if (g < 8) {
+    s = red[g * 8][c];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += red[g * 8 + i][c];
+    red[g * 8][c] = s;
+  }
+  __syncthreads();
   if (g == 0) {
-    for (int i = 1; i < 16; ++i) s += red[i][c];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += red[i * 8][c];
     float* to = q < n4 ? dg : db;
     if (to) reinterpret_cast<f32x4*>(to)[q < n4 ? q : q - n4] = s;
   }
@@ -198,6 +230,7 @@ hipError_t norm_forward(const float* h, const float* gain, const float* bias, T1
   switch (row_threads(d)) {
     case 64: layernorm_kernel<T16, 64><<<T, 64, 0, s>>>(h, gain, bias, x, d, eps); break;
     case 256: layernorm_kernel<T16, 256><<<T, 256, 0, s>>>(h, gain, bias, x, d, eps); break;
+    case 512: layernorm_kernel<T16, 512><<<T, 512, 0, s>>>(h, gain, bias, x, d, eps); break;
     default: layernorm_kernel<T16, 1024><<<T, 1024, 0, s>>>(h, gain, bias, x, d, eps);
   }
   return hipGetLastError();
@@ -213,6 +246,9 @@ hipError_t norm_backward(const T16* dx, const float* h, const float* gain, float
       break;
     case 256:
       layernorm_backward_kernel<T16, 256><<<nb, 256, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);
+      break;
+    case 512:
+      layernorm_backward_kernel<T16, 512><<<nb, 512, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);
       break;
     default:
       layernorm_backward_kernel<T16, 1024><<<nb, 1024, 0, s>>>(dx, h, gain, dh, part, T, d, eps, acc);

@@ -68,24 +68,23 @@ __device__ inline uint32_t any_bits(u32x4 u) {
   return (u.x | u.y) | (u.z | u.w);
 }
 
-// Bound of a row's norm from its sum of squares and the bits of its elements.
+// Error of a logit.  A matrix product's step of 32 columns rounds its sum once,
+// to half a step of fp32: rows of one repeated number, whose roundings all
+// point the same way, come to 0.50 of 2^-23 per step (d 4096 and 16384) and no
+// input measured to more; counted is 0.55, and 0.5 for each join of a wave's
+// sum.  The sum S_j that the j-th step rounds is at most |x_j| |w_j|, the norms
+// of the columns up to it, so with P(x) the sum of |x_j|^2 over the steps the
+// roundings come to at most
+//   2^-24 (1.1 sum_j |x_j| |w_j| + waves |x| |w|) <= 2^-24 q(x) q(w),
+//   q(x)^2 = 1.1 P(x) + waves |x|^2.
 // The squares of fp16 do not underflow in fp32; those of bf16 do below 1e-19,
 // and then count as the largest norm that can go with so small a sum.  A row
-// of zeros has norm 0, and its logits are exact.
-__device__ inline float norm_bound(float sq, uint32_t bits) {
+// of zeros has q 0, and its logits are exact.
+__device__ inline float error_norm(float q2, uint32_t bits) {
   if ((bits & 0x7FFF7FFFu) == 0) return 0.0f;
-  return fmaxf(sqrtf(sq) * 1.0001f, 4e-15f);
+  return fmaxf(sqrtf(q2) * 1.0001f, 1e-13f);
 }
-
-// A logit's error is at most this times the norms of its rows: the roundings
-// on a product's way.  A matrix product's step of 32 columns rounds its sum
-// once, to half a step of fp32: rows of one repeated number, whose roundings
-// all point the same way, come to 0.50 of 2^-23 per step (d 4096 and 16384)
-// and no input measured to more; counted are 0.75, and 0.5 for each join.
-__host__ __device__ inline float sum_error(int d, int waves) {
-  const int steps = 2 * ((d / 64 + waves - 1) / waves);
-  return (1.5f * steps + waves) * 0x1p-24f;
-}
+constexpr float kSumError = 0x1p-24f;
 
 // Logits [T, E] of MT * 16 tokens and NT * 16 experts per block.  Every wave
 // takes its share of the columns for the whole tile, 64 columns (a line of
@@ -134,7 +133,7 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
 #pragma unroll
   for (int j = 0; j < LB; ++j) wo[j] = (uint32_t)min(j * 8 + r8, p.E - 1 - e0) * (uint32_t)(p.d * 2) + chunk;
   f32x4 acc[MT][NT];
-  float sx[LA], sw[LB];
+  float sx[LA], sw[LB], px[LA], pw[LB];   // squares so far, and their sum over the steps
   uint32_t zx[LA], zw[LB];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -142,12 +141,12 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < LA; ++j) {
-    sx[j] = 0.0f;
+    sx[j] = px[j] = 0.0f;
     zx[j] = 0;
   }
 #pragma unroll
   for (int j = 0; j < LB; ++j) {
-    sw[j] = 0.0f;
+    sw[j] = pw[j] = 0.0f;
     zw[j] = 0;
   }
   const int n = (p.d / 64 - wave + NW - 1) / NW;  // this wave's pieces
@@ -170,7 +169,9 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
     if (norm_x) {
 #pragma unroll
       for (int j = 0; j < LA; ++j) {
+        // (a row's squares lie in eight lanes: the sums of both are joined below)
         sx[j] = squares(__builtin_bit_cast(x8, a[j]), sx[j]);
+        px[j] += sx[j];
         zx[j] |= any_bits(a[j]);
       }
     }
@@ -178,6 +179,7 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
 #pragma unroll
       for (int j = 0; j < LB; ++j) {
         sw[j] = squares(__builtin_bit_cast(x8, b[j]), sw[j]);
+        pw[j] += sw[j];
         zw[j] |= any_bits(b[j]);
       }
     }
@@ -220,11 +222,11 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
   };
   if (norm_x) {
 #pragma unroll
-    for (int j = 0; j < LA; ++j) put(sx[j], zx[j], j * 8);
+    for (int j = 0; j < LA; ++j) put(2.2f * px[j] + NW * sx[j], zx[j], j * 8);
   }
   if (norm_w) {
 #pragma unroll
-    for (int j = 0; j < LB; ++j) put(sw[j], zw[j], BM + j * 8);
+    for (int j = 0; j < LB; ++j) put(2.2f * pw[j] + NW * sw[j], zw[j], BM + j * 8);
   }
   __syncthreads();
   for (int v = threadIdx.x; v < BM * BN; v += NW * 64) {
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
       s += sq[w][v];
       z |= nz[w][v];
     }
-    const float bound = norm_bound(s, z);
+    const float bound = error_norm(s, z);
     if (v < BM && t0 + v < T) p.x_norm[t0 + v] = bound;
     if (v >= BM && e0 + v - BM < p.E) p.w_norm[e0 + v - BM] = bound;
   }
@@ -375,7 +377,7 @@ __device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, i
 // ... (C of them), lane k slot k.
 template <int C>
 struct Token {
-  float l[C], b[C], key[C];
+  float l[C], b[C], key[C], kerr[C];
   float val[C];       // what groups count
   bool exact[C];      // its row or the token's is all zeros: so is the sum
   bool fit[C];        // can be selected at all
@@ -456,7 +458,7 @@ __device__ inline void sum_again(const RouterParams& p, const T16* xr, const boo
 // The selection by 64-bit sums, whatever is open: experts whose order or group
 // is not certain are summed again (bound 0) until nothing is open.
 template <class T16, int C>
-__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, float xn, float rel,
+__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, float xn,
                              OpenLds<C>& lds) {
   const int lane = threadIdx.x & 63;
   const double none = -__builtin_inf();
@@ -472,7 +474,7 @@ __device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk,
     if (e < p.E && finite(tk.l[c])) {
       const float n = global<float>(p.w_norm)[e];
       // (rounding to fp32 sums below the smallest numbers adds to the bound)
-      err[c] = n > 0.0f && xn > 0.0f ? fminf(rel * xn * n + 1e-33f, 1e30f) : 0.0f;
+      err[c] = n > 0.0f && xn > 0.0f ? fminf(kSumError * xn * n + 1e-33f, 1e30f) : 0.0f;
     }
     want[c] = false;
   }
@@ -675,7 +677,7 @@ __device__ inline void sort_lane(uint32_t (&k)[C], int (&e)[C]) {
 // sorts its keys, and a slot takes the largest of the lanes' first ones
 // (take_slots).  row: C * 64 floats of LDS of the wave's own.
 template <int C>
-__device__ inline void score_token(const RouterParams& p, int t, const float* lg, float xn, float rel,
+__device__ inline void score_token(const RouterParams& p, int t, const float* lg, float xn,
                                    float* row, Token<C>& tk) {
   const int lane = threadIdx.x & 63;
   const float none = -__builtin_inff();
@@ -697,7 +699,7 @@ __device__ inline void score_token(const RouterParams& p, int t, const float* lg
     tk.fit[c] = finite(tk.l[c]);
     if (tk.fit[c]) tk.top = fmaxf(tk.top, tk.l[c]);
     // (rounding to fp32 of the smallest numbers adds to a bound)
-    err[c] = xn > 0.0f && err[c] > 0.0f ? fminf(rel * xn * err[c] + 1e-33f, 1e30f) : 0.0f;
+    err[c] = xn > 0.0f && err[c] > 0.0f ? fminf(kSumError * xn * err[c] + 1e-33f, 1e30f) : 0.0f;
     tk.exact[c] = err[c] == 0.0f;
     worst = fmaxf(worst, tk.fit[c] ? err[c] : 0.0f);
   }
@@ -723,7 +725,8 @@ __device__ inline void score_token(const RouterParams& p, int t, const float* lg
       e1 = tk.fit[c] ? sc[c] * 1.01f * (err[c] + tk.zrel + 1e-6f * (tk.top - tk.l[c])) : 0.0f;
     } else {
       sc[c] = tk.fit[c] ? __frcp_rn(1.0f + __expf(-tk.l[c])) : 0.0f;
-      e1 = 0.25f * err[c] + 1e-6f * sc[c];
+      // (the sigmoid's slope here, and what it may change by within the bound)
+      e1 = err[c] * (1.001f * sc[c] * (1.0f - sc[c]) + 0.1f * err[c]) + 1e-6f * sc[c];
     }
     tk.key[c] = tk.l[c];
     if (biased) {
@@ -732,7 +735,8 @@ __device__ inline void score_token(const RouterParams& p, int t, const float* lg
       e1 += 1e-7f * fabsf(tk.key[c]);
     }
     verr = fmaxf(verr, tk.fit[c] ? e1 : 0.0f);
-    worst = fmaxf(worst, tk.fit[c] ? (biased ? e1 : err[c]) : 0.0f);
+    tk.kerr[c] = biased ? e1 : err[c];
+    worst = fmaxf(worst, tk.fit[c] ? tk.kerr[c] : 0.0f);
     tk.kept[c] = tk.fit[c];
   }
   tk.margin = 2.0f * wave_max(worst);
@@ -781,9 +785,11 @@ __device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& t
   sort_lane(hk, he);
   tk.sel = -1;
   uint64_t near = 0;
+  float last = 0.0f;
   for (int k = 0; k < p.K; ++k) {
     const uint32_t m = __builtin_amdgcn_readfirstlane(wave_max_u32(hk[0]));
     if (m == 0) break;  // nobody left
+    last = key_float(m);
     const int from = __ffsll((unsigned long long)__ballot(hk[0] == m)) - 1;
     const int e = __builtin_amdgcn_readlane(he[0], from);
     if (lane == k) tk.sel = e;
@@ -793,7 +799,27 @@ __device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& t
       hk[c] = mine ? (c + 1 < C ? hk[c + 1] : 0u) : hk[c];
       he[c] = mine ? (c + 1 < C ? he[c + 1] : 0) : he[c];
     }
-    near |= __ballot(hk[0] >= float_key(key_float(m) - tk.margin));
+    near |= __ballot(hk[0] >= float_key(last - tk.margin));
+  }
+  if (near) {
+    // again by the margin of those that count: the slots and what comes near
+    float worst = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      worst = fmaxf(worst, tk.kept[c] && tk.key[c] >= last - tk.margin ? tk.kerr[c] : 0.0f);
+    tk.margin = 2.0f * wave_max(worst);
+    near = 0;
+    for (int k = 0; k < p.K; ++k) {
+      const int e = __builtin_amdgcn_readlane(tk.sel, k);
+      if (e < 0) break;
+      float ke = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        near |= __ballot(tk.kept[c] && c * 64 + lane != e && fabsf(tk.key[c] - ke) <= tk.margin);
+    }
   }
   tk.slots_open = near != 0;
   wave_lds_fence();
@@ -1016,7 +1042,7 @@ constexpr int kManyBlocks = 256;
 template <int C>
 __global__ __launch_bounds__(kManyThreads) void router_select_kernel(RouterParams p, int T,
                                                                      const float* __restrict__ lg,
-                                                                     float rel, RouterOut o) {
+                                                                     RouterOut o) {
   __shared__ float rows[kManyWaves][C * 64];
   __shared__ int32_t counts[C * 64];
   __shared__ int32_t n_open, first_open, opens[kManyThreads];
@@ -1028,7 +1054,7 @@ __global__ __launch_bounds__(kManyThreads) void router_select_kernel(RouterParam
   // (at most 65536 / (16 * 256) = 16 tokens a wave, one slot of opens each)
   for (int t = blockIdx.x * kManyWaves + wave; t < T; t += gridDim.x * kManyWaves) {
     Token<C> tk;
-    score_token(p, t, lg, global<float>(p.x_norm)[t], rel, rows[wave], tk);
+    score_token(p, t, lg, global<float>(p.x_norm)[t], rows[wave], tk);
     take_slots(p, rows[wave], tk);
     if (!tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
     else if ((threadIdx.x & 63) == 0) opens[atomicAdd(&n_open, 1)] = t;
@@ -1048,7 +1074,7 @@ template <class T16, int C>
 __global__ __launch_bounds__(kOneThreads) void router_select_open_kernel(RouterParams p, int T, int listed,
                                                                          const T16* __restrict__ x,
                                                                          const float* __restrict__ lg,
-                                                                         float rel, RouterOut o) {
+                                                                         RouterOut o) {
   __shared__ float rows[kOneThreads / 64][C * 64];
   __shared__ OpenLds<C> lds;
   __shared__ int32_t counts[C * 64];
@@ -1064,7 +1090,7 @@ __global__ __launch_bounds__(kOneThreads) void router_select_open_kernel(RouterP
     const float xn = global<float>(p.x_norm)[t];
     const T16* xr = x + (int64_t)t * p.d;
     Token<C> tk;
-    score_token(p, t, lg, xn, rel, rows[wave], tk);
+    score_token(p, t, lg, xn, rows[wave], tk);
     // (scores that share an uncertain denominator beside biases that do not)
     bool open = tk.groups_open && p.bias && p.score == SCORE_SOFTMAX;
     if (!open) {
@@ -1072,16 +1098,14 @@ __global__ __launch_bounds__(kOneThreads) void router_select_open_kernel(RouterP
       take_slots(p, rows[wave], tk);
       if (tk.slots_open) open = !select_slots(p, xr, tk, lds);
     }
-    if (open) select_exact(p, xr, tk, xn, rel, lds);
+    if (open) select_exact(p, xr, tk, xn, lds);
     if (wave == 0) finish(p, t, tk, o, counts);
   }
   add_counts(p, o, counts);
 }
 
 template <class T16, int MT, int NT, int NW>
-hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, int32_t* count, float* rel,
-                  hipStream_t s) {
-  *rel = sum_error(p.d, NW);
+hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, int32_t* count, hipStream_t s) {
   const dim3 grid((T + MT * 16 - 1) / (MT * 16), (p.E + NT * 16 - 1) / (NT * 16));
   router_logits_kernel<T16, MT, NT, NW><<<grid, NW * 64, 0, s>>>(p, T, x, lg, count);
   return hipGetLastError();
@@ -1090,7 +1114,6 @@ hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, int32_t
 template <class T16>
 hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, hipStream_t s) {
   float* lg = o.logits ? o.logits : p.logits;
-  float rel = 0.0f;
   // The largest tile that still gives about every compute unit a block: a
   // block loads (tokens + experts) rows for tokens * experts sums.  us at d
   // 4096, 256 experts, tiles of 64x64 / 64x32 / 32x32 / 16x32 / 16x16 on eight
@@ -1103,13 +1126,13 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, h
   auto blocks = [&](int m, int n) { return (int64_t)((T + m - 1) / m) * ((p.E + n - 1) / n); };
   constexpr int kEnough = 200;
   hipError_t e;
-  if (p.E <= 16) e = logits<T16, 1, 1, 16>(p, T, x, lg, o.count, &rel, s);
-  else if (blocks(64, 64) >= 2 * kEnough) e = logits<T16, 4, 4, 4>(p, T, x, lg, o.count, &rel, s);
-  else if (blocks(64, 64) >= kEnough) e = logits<T16, 4, 4, 8>(p, T, x, lg, o.count, &rel, s);
-  else if (blocks(64, 32) >= kEnough) e = logits<T16, 4, 2, 8>(p, T, x, lg, o.count, &rel, s);
-  else if (blocks(32, 32) >= kEnough) e = logits<T16, 2, 2, 8>(p, T, x, lg, o.count, &rel, s);
-  else if (blocks(16, 32) >= kEnough) e = logits<T16, 1, 2, 8>(p, T, x, lg, o.count, &rel, s);
-  else e = logits<T16, 1, 1, 8>(p, T, x, lg, o.count, &rel, s);
+  if (p.E <= 16) e = logits<T16, 1, 1, 16>(p, T, x, lg, o.count, s);
+  else if (blocks(64, 64) >= 2 * kEnough) e = logits<T16, 4, 4, 4>(p, T, x, lg, o.count, s);
+  else if (blocks(64, 64) >= kEnough) e = logits<T16, 4, 4, 8>(p, T, x, lg, o.count, s);
+  else if (blocks(64, 32) >= kEnough) e = logits<T16, 4, 2, 8>(p, T, x, lg, o.count, s);
+  else if (blocks(32, 32) >= kEnough) e = logits<T16, 2, 2, 8>(p, T, x, lg, o.count, s);
+  else if (blocks(16, 32) >= kEnough) e = logits<T16, 1, 2, 8>(p, T, x, lg, o.count, s);
+  else e = logits<T16, 1, 1, 8>(p, T, x, lg, o.count, s);
   if (e != hipSuccess) return e;
   // Up to kFew tokens a block each, in one launch; more a wave each, and the
   // open ones a block each in another.
@@ -1117,17 +1140,17 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, h
   const int C = p.E <= 64 ? 1 : p.E <= 128 ? 2 : p.E <= 256 ? 4 : 8;
   if (T > kFew) {
     const int blocks = (T + kManyWaves - 1) / kManyWaves, grid = blocks < kManyBlocks ? blocks : kManyBlocks;
-    if (C == 1) router_select_kernel<1><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
-    else if (C == 2) router_select_kernel<2><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
-    else if (C == 4) router_select_kernel<4><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
-    else router_select_kernel<8><<<grid, kManyThreads, 0, s>>>(p, T, lg, rel, o);
+    if (C == 1) router_select_kernel<1><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
+    else if (C == 2) router_select_kernel<2><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
+    else if (C == 4) router_select_kernel<4><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
+    else router_select_kernel<8><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   const int listed = T > kFew, grid = listed ? kListBlocks : T;
-  if (C == 1) router_select_open_kernel<T16, 1><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
-  else if (C == 2) router_select_open_kernel<T16, 2><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
-  else if (C == 4) router_select_open_kernel<T16, 4><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
-  else router_select_open_kernel<T16, 8><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, rel, o);
+  if (C == 1) router_select_open_kernel<T16, 1><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
+  else if (C == 2) router_select_open_kernel<T16, 2><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
+  else if (C == 4) router_select_open_kernel<T16, 4><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
+  else router_select_open_kernel<T16, 8><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
   return hipGetLastError();
 }
 
