@@ -253,16 +253,19 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
 constexpr int kCols = 128;   // columns of d per block of the products
 
 // LDS tile of 16-bit rows of kCols columns, 256 bytes each.  A transposing
-// read takes 8 bytes of four rows for each 16 lanes: 64-byte block b of a row
-// r lies at block b ^ (r & 3), so that the four rows are in different banks,
-// and the halves of 16 bytes are exchanged where r & 4, so that the next 16
-// lanes, four rows on, are in the others.
+// read takes 8 bytes of four rows in each of 16 lanes.  64-byte block b of a
+// row r lies at block b ^ (r & 3), so that the four rows are in different
+// banks; and so that the next 16 lanes, four rows on, are in others again,
+// where r & 4 the halves of `kHalf` bytes are exchanged: of 16 bytes for
+// columns read 8 bytes in 16, of 64 for columns in a row.
+template <int kHalf>
 __device__ inline int tile_at(int row, int byte) {
-  return row * 256 + (byte ^ ((row & 3) << 6) ^ ((row & 4) << 1));
+  return row * 256 + (byte ^ ((row & 3) << 6) ^ (row & 4 ? kHalf : 0));
 }
+template <int kHalf>
 __device__ inline void tile_put(unsigned char* tile, int row, int byte, u32x4 v) {
-  const u32x4 w = row & 4 ? u32x4{v.z, v.w, v.x, v.y} : v;
-  *reinterpret_cast<u32x4*>(tile + row * 256 + (byte ^ ((row & 3) << 6))) = w;
+  if (kHalf == 8 && (row & 4)) v = u32x4{v.z, v.w, v.x, v.y};
+  *reinterpret_cast<u32x4*>(tile + tile_at<kHalf == 8 ? 0 : kHalf>(row, byte)) = v;
 }
 
 typedef __attribute__((address_space(3))) s16x4* LdsRead;
@@ -270,12 +273,12 @@ typedef __attribute__((address_space(3))) s16x4* LdsRead;
 // 8 terms for one of 16 columns per lane from rows `row` + term(g, .) of a
 // tile; lanes q = l & 3 read the columns at byte col(q) (8 bytes each), and
 // lane l gets column l & 3 of the ones that q = (l & 15) >> 2 points at.
-template <class T16>
+template <class T16, int kHalf>
 __device__ inline typename Split<T16>::x8 read_columns(const unsigned char* tile, int row, int byte) {
   const int lane = threadIdx.x & 63;
   const int r = row + 4 * (lane >> 4) + ((lane & 15) >> 2);
-  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRead)(tile + tile_at(r, byte)));
-  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRead)(tile + tile_at(r + 16, byte)));
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRead)(tile + tile_at<kHalf>(r, byte)));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsRead)(tile + tile_at<kHalf>(r + 16, byte)));
   typedef short s16x8 __attribute__((ext_vector_type(8)));
   const s16x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   return __builtin_bit_cast(typename Split<T16>::x8, v);
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (e0 + i * 16 < eb_n * 32) tile_put(tile, e0 + i * 16, c16 * 16, w[i]);
+      if (e0 + i * 16 < eb_n * 32) tile_put<8>(tile, e0 + i * 16, c16 * 16, w[i]);
   }
   __syncthreads();
   const int q = lane & 3, g = lane >> 4;
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
   const auto load_wg = [&](int eb, x8 (&av)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      av[j] = read_columns<T16>(tile, eb * 32, (j >> 1) * 64 + q * 16 + (j & 1) * 8);
+      av[j] = read_columns<T16, 8>(tile, eb * 32, (j >> 1) * 64 + q * 16 + (j & 1) * 8);
   };
   const auto write = [&](int w32) {
     const float s = global<float>(scales)[w32 * 32 / kGroupTokens];
@@ -409,8 +412,8 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
   typedef typename Split<T16>::x8 x8;
   constexpr int WT = 8 / WE, kW = Split<T16>::kW;
   constexpr int kLoads = 16 / WE;   // 16-byte chunks of 64 rows per thread of a set
-  // a turn's fragments of dl during the turn before, where registers allow
-  constexpr bool kDlAhead = WE >= 4;
+  // a turn's loads during the turn before, where registers allow
+  constexpr bool kDlAhead = WE >= 4, kXAhead = WE >= 2;
   constexpr int kTiles = WT <= 4 ? 2 : 1;  // two tiles in turn where LDS holds them
   __shared__ __attribute__((aligned(16))) unsigned char tiles[kTiles][WT][kGroupTokens * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -447,17 +450,18 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
         for (int part = 0; part < kW; ++part)
           b[k][i][part] = global<x8>(fw)[(((int64_t)(group * 2 + k) * ET + tile_e + i) * kW + part) * 64 + lane];
   };
-  load_x(0);
+  if (kXAhead) load_x(0);
   if (kDlAhead) load_dl(0);
   for (int turn = 0; turn < turns; ++turn) {
     unsigned char* tile = tiles[turn % kTiles][wt];
+    if (!kXAhead) load_x(turn);
     if (kTiles == 1) __syncthreads();   // (the last turn's reads)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int v = (i * WE + we) * 64 + lane;
-      tile_put(tile, v >> 4, (v & 15) * 16, ahead[i]);
+      tile_put<32>(tile, v >> 4, (v & 15) * 16, ahead[i]);
     }
-    load_x(turn + 1);
+    if (kXAhead) load_x(turn + 1);
     if (!kDlAhead) load_dl(turn);
     __syncthreads();
     x8 now[2][2][kW];
@@ -481,7 +485,7 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          av[h][k] = read_columns<T16>(tile, k * 32, (j * 2 + h) * 32 + (lane & 3) * 8);
+          av[h][k] = read_columns<T16, 32>(tile, k * 32, (j * 2 + h) * 32 + (lane & 3) * 8);
     };
     read(0, a[0]);
 #pragma unroll
