@@ -268,6 +268,7 @@ struct RouterParams {
   const void* wg;          // [E, d] of `type`
   const float* bias;       // [E] or null
   int32_t d, E, K, type, score, n_groups, top_groups, group_best, renorm;
+  int32_t size_inv;        // 2^20 / (E / n_groups), rounded up
   float scale;
   // workspace, sized for max_tokens
   float* logits;           // [T, E], calls that do not ask for them

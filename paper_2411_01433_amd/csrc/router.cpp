@@ -143,6 +143,8 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
   p.type = desc->type;
   p.score = desc->score;
   p.n_groups = desc->n_groups;
+  const int32_t size = desc->n_experts / desc->n_groups;
+  p.size_inv = ((1 << 20) + size - 1) / size;
   p.top_groups = desc->top_groups;
   p.group_best = desc->group_best;
   p.renorm = desc->renormalize;

@@ -85,6 +85,902 @@ __device__ inline float error_norm(float q2, uint32_t bits) {
   return fmaxf(sqrtf(q2) * 1.0001f, 1e-13f);
 }
 constexpr float kSumError = 0x1p-24f;
+__device__ inline float logit_error(float qx, float qw) {
+  // (rounding to fp32 of the smallest numbers adds to a bound)
+  return qx > 0.0f && qw > 0.0f ? fminf(kSumError * qx * qw + 1e-33f, 1e30f) : 0.0f;
+}
+
+// ---- selection ------------------------------------------------------------
+
+__device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// Sum and maximum of doubles over a wave in registers (see wave_sum_dpp).
+template <int CTRL>
+__device__ inline double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ inline double dpp_of(double v) { return dpp_d<CTRL>(v); }
+template <int CTRL>
+__device__ inline float dpp_of(float v) { return dpp_f<CTRL>(v); }
+// The value that lane `from` (the same for all) has.
+__device__ inline float lane_value(float v, int from) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), from));
+}
+__device__ inline double lane_value(double v, int from) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, from);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), from);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double pair_d(uint32_t lo, uint32_t hi) {
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline double wave_sum(double v) {
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  uint64_t u = __builtin_bit_cast(uint64_t, v);
+  auto l = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  v = pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
+  u = __builtin_bit_cast(uint64_t, v);
+  l = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  h = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
+}
+__device__ inline double wave_max(double v) {
+  // order-preserving key, its upper half first
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t k = u >> 63 ? ~u : u | 1ull << 63;
+  const uint32_t hi = wave_max_u32((uint32_t)(k >> 32));
+  const uint32_t lo = wave_max_u32((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+  const uint64_t m = (uint64_t)hi << 32 | lo;
+  return __builtin_bit_cast(double, m >> 63 ? m & ~(1ull << 63) : ~m);
+}
+__device__ inline float key_float(uint32_t k) {
+  return __builtin_bit_cast(float, (k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ inline float wave_max(float v) { return key_float(wave_max_u32(float_key(v))); }
+
+// LDS of one wave is written and read by that wave alone.
+__device__ inline void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// x . w for two rows w over d columns by one wave, in 64 bits (a product of two
+// 16-bit numbers is exact there).  Every lane gets the sums.
+template <class T16>
+__device__ inline void exact_dots(const T16* x, const T16* w0, const T16* w1, int d, double& s0,
+                                  double& s1) {
+  typedef typename Vec<T16>::x8 x8;
+  constexpr int B = 4;  // pieces whose loads are in flight together
+  s0 = s1 = 0.0;
+  for (int c0 = (threadIdx.x & 63) * 8; c0 < d; c0 += 512 * B) {
+    x8 a[B], b[B], e[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const int c = min(c0 + 512 * i, d - 8);
+      a[i] = *global<x8>(x + c);
+      b[i] = *global<x8>(w0 + c);
+      e[i] = *global<x8>(w1 + c);
+    }
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+      if (c0 + 512 * i < d) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const double v = (double)(float)a[i][j];
+          s0 = fma(v, (double)(float)b[i][j], s0);
+          s1 = fma(v, (double)(float)e[i][j], s1);
+        }
+      }
+  }
+  s0 = wave_sum(s0);
+  s1 = wave_sum(s1);
+}
+
+// Two best values of each group and what decides about it: 64 / G lanes per
+// group (G the groups rounded up to a power of two) scan its members and join.
+template <class F>
+struct GroupBest {
+  F sum;   // of the group's best one or two; -inf for a group without any
+  F low;   // the least value that counts in it
+};
+template <class F>
+__device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, int lane, int per, int g) {
+  const F none = -__builtin_inff();
+  const int size = p.E / p.n_groups;
+  F best = none, second = none;
+  if (g < p.n_groups)
+    for (int i = lane & (per - 1); i < size; i += per) {
+      const F v = row[g * size + i];
+      second = v > best ? best : v > second ? v : second;
+      best = v > best ? v : best;
+    }
+  const auto join = [&](F ob, F os) {
+    const F lo = ob > best ? best : ob;
+    second = os > second ? os : second;
+    second = lo > second ? lo : second;
+    best = ob > best ? ob : best;
+  };
+  // lane ^ 1, lane ^ 2, mirrors in 8 and 16, then the other row of 16 and half
+  if (per > 1) join(dpp_of<0xB1>(best), dpp_of<0xB1>(second));
+  if (per > 2) join(dpp_of<0x4E>(best), dpp_of<0x4E>(second));
+  if (per > 4) join(dpp_of<0x141>(best), dpp_of<0x141>(second));
+  if (per > 8) join(dpp_of<0x140>(best), dpp_of<0x140>(second));
+  if (per > 16) join(__shfl_xor(best, 16, 64), __shfl_xor(second, 16, 64));
+  if (per > 32) join(__shfl_xor(best, 32, 64), __shfl_xor(second, 32, 64));
+  const bool two = p.group_best == 2 && second > none;
+  return {two ? best + second : best, two ? second : best};
+}
+
+// One token's fp32 selection, by one wave: lane i has the experts i, i + 64,
+// ... (C of them), lane k slot k.
+template <int C>
+struct Token {
+  float l[C], b[C], key[C], kerr[C];
+  float val[C];       // what groups count
+  float err[C];       // bound of l's error; 0 where a row is all zeros
+  bool fit[C];        // can be selected at all
+  bool kept[C];       // ... and lies in a group that stays
+  // lanes of group g (lanes_per_group of them): its best members, whether it
+  // stays, the least sum that does and the largest that does not
+  GroupBest<float> group;
+  bool stays;
+  float in, out, group_err;
+  float top, z, zrel; // softmax: largest logit, denominator, its relative error
+  float margin;       // keys further apart are certainly in order
+  bool groups_open, slots_open;
+  int sel;
+  float sl;           // its logit
+};
+
+__device__ inline int lanes_per_group(const RouterParams& p) {
+  int per = 64;
+  while (64 / per < p.n_groups) per >>= 1;
+  return per;
+}
+
+// Group of expert e < 512: size_inv is 2^20 / size rounded up, which is off by
+// less than 2^-11 for such e, below the 1/size by which e / size can miss a
+// whole number.
+__device__ inline int group_of(const RouterParams& p, int e) { return (int)((uint32_t)(e * p.size_inv) >> 20); }
+
+// Error of a group's sum.
+template <int C>
+__device__ inline float group_margin(const Token<C>& tk) {
+  return tk.group_err + 5e-7f * fmaxf(fabsf(tk.in), fabsf(tk.out));
+}
+
+// The experts of the groups that stay.
+template <int C>
+__device__ inline void keep_groups(const RouterParams& p, Token<C>& tk) {
+  const int lane = threadIdx.x & 63, per = lanes_per_group(p);
+  const uint64_t at = __ballot(tk.stays);
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    tk.kept[c] = tk.fit[c] && (at >> min(group_of(p, c * 64 + lane) * per, 63) & 1);
+}
+
+// The waves that work on one open token: a block of TW, or one wave by itself.
+// All of a team make the same selection and share the sums in 64 bits.
+template <int TW>
+struct Team {
+  static __device__ void sync() {
+    if constexpr (TW == 1) wave_lds_fence();
+    else __syncthreads();
+  }
+  static __device__ bool lead() { return TW == 1 || threadIdx.x < 64; }
+  static __device__ int wave() { return TW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+};
+
+// LDS of a team that works on a token whose selection is open.
+template <int C>
+struct OpenLds {
+  double row[C * 64];    // keys or scores for the groups' scan
+  double dots[C * 64];   // logits summed again
+  int32_t list[C * 64];  // ... and their experts
+  double sum[kRouterMaxGroups], low[kRouterMaxGroups];
+  float err[kRouterMaxGroups], more[2][kRouterMaxGroups];
+};
+
+// Sums the logits of the experts of `want` again, in 64 bits, the team's
+// waves in turn; take(c, lane, value) gets each.  Every wave has the same
+// `want` and calls this.
+template <class T16, int C, int TW, class Take>
+__device__ inline void sum_again(const RouterParams& p, const T16* xr, const bool (&want)[C],
+                                 OpenLds<C>& lds, Take take) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint64_t m = __ballot(want[c]);
+    if (want[c] && Team<TW>::lead())
+      lds.list[n + __popcll(m & ((1ull << lane) - 1ull))] = c * 64 + lane;
+    n += __popcll(m);
+  }
+  Team<TW>::sync();
+  // two of them at a time, unless the team has a wave for each
+  const int step = n > TW ? 2 : 1;
+  for (int i = Team<TW>::wave() * step; i < n; i += TW * step) {
+    const int last = min(i + step, n) - 1;
+    const int e0 = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    const int e1 = __builtin_amdgcn_readfirstlane(lds.list[last]);
+    const T16* wg = static_cast<const T16*>(p.wg);
+    double s0, s1;
+    exact_dots(xr, wg + (int64_t)e0 * p.d, wg + (int64_t)e1 * p.d, p.d, s0, s1);
+    if (lane == 0) {
+      lds.dots[last] = s1;
+      lds.dots[i] = s0;
+    }
+  }
+  Team<TW>::sync();
+  for (int i = 0; i < n; ++i) {
+    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    take(e >> 6, e & 63, lds.dots[i]);
+  }
+  Team<TW>::sync();
+}
+
+// The selection by 64-bit sums, whatever is open: experts whose order or group
+// is not certain are summed again (bound 0) until nothing is open.
+template <class T16, int C, int TW>
+__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+  const int lane = threadIdx.x & 63;
+  const double none = -__builtin_inf();
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  double l[C];
+  float err[C];
+  bool want[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    l[c] = tk.l[c];
+    err[c] = finite(tk.l[c]) ? tk.err[c] : 0.0f;
+    want[c] = false;
+  }
+  const int per = lanes_per_group(p);
+  for (;;) {
+    sum_again<T16, C, TW>(p, xr, want, lds, [&](int c, int at, double v) {
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+        if (i == c && lane == at) {
+          l[i] = v;
+          err[i] = 0.0f;
+        }
+    });
+    double key[C], sc[C], kerr[C];
+    bool fit[C];
+    double zrel = 0.0;
+    if (soft) {
+      double top = none, z = 0.0;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (finite(tk.l[c])) top = fmax(top, l[c]);
+      top = wave_max(top);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        sc[c] = finite(tk.l[c]) ? exp(l[c] - top) : 0.0;
+        z += sc[c];
+      }
+      z = wave_sum(z);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        sc[c] = finite(tk.l[c]) ? sc[c] / z : 0.0;
+        zrel += sc[c] * err[c];
+      }
+      zrel = biased ? 1.01 * wave_sum(zrel) : 0.0;  // (without a bias the sum is common to all)
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) sc[c] = finite(tk.l[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      fit[c] = tk.fit[c];
+      want[c] = false;
+      // slope of a score by its logit: s of the softmax's term, 1/4 at most of a sigmoid
+      const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
+      key[c] = biased ? sc[c] + tk.b[c] : l[c];
+      kerr[c] = biased ? serr : err[c];
+    }
+    bool open = false;
+    if (p.n_groups > 1) {
+      const int size = p.E / p.n_groups;
+      if (Team<TW>::lead()) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
+        lds.more[0][lane] = lds.more[1][lane] = 0.0f;
+      }
+      Team<TW>::sync();
+      const int g = lane / per;
+      const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
+      if (Team<TW>::lead() && (lane & (per - 1)) == 0) {
+        lds.sum[g] = gb.sum;
+        lds.low[g] = gb.low;
+      }
+      // A group's error: that of its most uncertain member, once or twice,
+      // among those that may be one of its best - that reach, with their own
+      // bound, down to the least that counts less the bounds of what counts.
+#pragma unroll
+      for (int round = 0; round < 2; ++round) {
+        Team<TW>::sync();
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int e = c * 64 + lane;
+          if (!fit[c]) continue;
+          const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
+          const double reach = round == 0 ? lds.row[e] : lds.row[e] + serr + lds.err[e / size];
+          const bool in = reach >= lds.low[e / size];
+          if (round == 1) want[c] = in && err[c] > 0.0f;
+          if (in && serr > 0.0 && Team<TW>::lead())
+            atomicMax(reinterpret_cast<unsigned*>(&lds.more[round][e / size]),
+                      __float_as_uint((float)(serr * 1.0001)));
+        }
+        Team<TW>::sync();
+        if (Team<TW>::lead()) lds.err[lane] = lds.more[round][lane];
+      }
+      Team<TW>::sync();
+      const bool is = lane < p.n_groups;
+      const double mine = is ? lds.sum[lane] : none;
+      int rank = 0;
+      for (int h = 0; h < p.n_groups; ++h) rank += lds.sum[h] > mine || (lds.sum[h] == mine && h < lane);
+      const uint64_t kept = __ballot(is && rank < p.top_groups);
+      bool unsure = false;
+      if (is && mine > none)
+        for (int h = 0; h < p.n_groups; ++h) {
+          const double v = lds.sum[h];
+          if (v > none && (kept >> lane & 1) != (kept >> h & 1))
+            unsure |= fabs(v - mine) <= p.group_best * ((double)lds.err[lane] + lds.err[h]) +
+                                            zrel * fmax(fabs(v), fabs(mine));
+        }
+      const uint64_t um = __ballot(unsure && (lds.err[lane] > 0.0f || zrel > 0.0));
+      open = um != 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] = want[c] && (um >> ((c * 64 + lane) / size) & 1);
+#pragma unroll
+      for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
+      Team<TW>::sync();
+    }
+    if (!open) {
+      tk.sel = -1;
+      for (int k = 0; k < p.K; ++k) {
+        double bk = none;
+        bool any = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (fit[c]) {
+            bk = any ? fmax(bk, key[c]) : key[c];
+            any = true;
+          }
+        bk = wave_max(bk);
+        int be = -1;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const uint64_t m = __ballot(fit[c] && key[c] == bk);
+          if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
+        }
+        be = __builtin_amdgcn_readfirstlane(be);
+        if (be < 0) break;  // nobody left
+        double ml = 0.0, ms = 0.0, me = 0.0;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (c * 64 + lane == be) {
+            fit[c] = false;
+            ml = l[c];
+            ms = sc[c];
+            me = kerr[c];
+          }
+        ml = lane_value(ml, be & 63);
+        ms = lane_value(ms, be & 63);
+        me = lane_value(me, be & 63);
+        if (lane == k) {
+          tk.sel = be;
+          tk.sl = (float)ml;
+        }
+        bool near = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const double room = me + kerr[c] + zrel * fabs(ms - sc[c]);
+          if (fit[c] && room > 0.0 && bk - key[c] <= room) {
+            near = true;
+            want[c] = want[c] || err[c] > 0.0f;
+          }
+        }
+        if (__ballot(near)) {
+          open = true;
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (c * 64 + lane == be) want[c] = want[c] || err[c] > 0.0f;
+        }
+      }
+    }
+    if (!open) return;
+    bool some = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) some |= want[c];
+    if (!__ballot(some)) {
+      // only the softmax's denominator is uncertain: every logit that it adds
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] = err[c] > 0.0f;
+    }
+  }
+}
+
+// Descending order of a lane's C keys, each with its number c.
+template <int C>
+__device__ inline void sort_lane(uint32_t (&k)[C], int (&e)[C]) {
+  const auto step = [&](int i, int j) {
+    const bool swap = k[j] > k[i];
+    const uint32_t kt = swap ? k[j] : k[i];
+    k[j] = swap ? k[i] : k[j];
+    k[i] = kt;
+    const int et = swap ? e[j] : e[i];
+    e[j] = swap ? e[i] : e[j];
+    e[i] = et;
+  };
+  // odd-even merging: pairs, fours, eights
+#pragma unroll
+  for (int n = 1; n < C; n *= 2)
+#pragma unroll
+    for (int m = n; m >= 1; m /= 2)
+#pragma unroll
+      for (int j = m % n; j + m < C; j += 2 * m)
+#pragma unroll
+        for (int i = 0; i < m; ++i)
+          if (i + j + m < C && (i + j) / (2 * n) == (i + j + m) / (2 * n)) step(i + j, i + j + m);
+}
+
+// Logits of one token and the bounds of their errors.
+template <int C>
+__device__ inline void load_token(const RouterParams& p, Global<float> lg, Global<float> wn, float xn,
+                                  Token<C>& tk) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int e = c * 64 + lane;
+    const bool in = e < p.E;
+    tk.l[c] = in ? lg[e] : -__builtin_inff();
+    tk.b[c] = in && p.bias ? global<float>(p.bias)[e] : 0.0f;
+    tk.err[c] = in ? logit_error(xn, wn[e]) : 0.0f;
+  }
+}
+
+// Scores, keys and groups of a token in fp32.  Keys are compared with one
+// margin, twice the largest bound of their errors.  For the slots each lane
+// sorts its keys, and a slot takes the largest of the lanes' first ones
+// (take_slots).  row: C * 64 floats of LDS of the wave's own.
+template <int C>
+__device__ inline void score_token(const RouterParams& p, float* row, Token<C>& tk) {
+  const int lane = threadIdx.x & 63;
+  const float none = -__builtin_inff();
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  float sc[C];
+  float worst = 0.0f;
+  tk.top = none;
+  tk.z = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    tk.fit[c] = finite(tk.l[c]);
+    if (tk.fit[c]) tk.top = fmaxf(tk.top, tk.l[c]);
+    worst = fmaxf(worst, tk.fit[c] ? tk.err[c] : 0.0f);
+  }
+  // The scores by the fast exponential and reciprocal: within 1e-6 of a
+  // score, and of a softmax's term 1e-6 for each unit below the largest.
+  tk.zrel = soft ? wave_max(worst) + 4e-6f : 0.0f;
+  if (soft) {
+    tk.top = wave_max(tk.top);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sc[c] = tk.fit[c] ? __expf(tk.l[c] - tk.top) : 0.0f;
+      tk.z += sc[c];
+    }
+    tk.z = wave_sum_dpp(tk.z);
+  }
+  float verr = 0.0f;  // largest error of what groups count
+  worst = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    float e1;
+    if (soft) {
+      sc[c] = tk.fit[c] ? sc[c] * __builtin_amdgcn_rcpf(tk.z) : 0.0f;
+      e1 = tk.fit[c] ? sc[c] * 1.01f * (tk.err[c] + tk.zrel + 1e-6f * (tk.top - tk.l[c])) : 0.0f;
+    } else {
+      sc[c] = tk.fit[c] ? __builtin_amdgcn_rcpf(1.0f + __expf(-tk.l[c])) : 0.0f;
+      // (the sigmoid's slope here, and what it may change by within the bound)
+      e1 = tk.err[c] * (1.001f * sc[c] * (1.0f - sc[c]) + 0.1f * tk.err[c]) + 1e-6f * sc[c];
+    }
+    tk.key[c] = tk.l[c];
+    if (biased) {
+      tk.fit[c] = tk.fit[c] && finite(tk.b[c]);
+      tk.key[c] = sc[c] + tk.b[c];
+      e1 += 1e-7f * fabsf(tk.key[c]);
+    }
+    verr = fmaxf(verr, tk.fit[c] ? e1 : 0.0f);
+    tk.kerr[c] = biased ? e1 : tk.err[c];
+    worst = fmaxf(worst, tk.fit[c] ? tk.kerr[c] : 0.0f);
+    tk.kept[c] = tk.fit[c];
+  }
+  tk.margin = 2.0f * wave_max(worst);
+  tk.group_err = p.group_best * wave_max(verr);
+  tk.groups_open = false;
+  if (p.n_groups > 1) {
+    const int per = lanes_per_group(p);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      tk.val[c] = tk.fit[c] ? (biased ? tk.key[c] : sc[c]) : none;
+      row[c * 64 + lane] = tk.val[c];
+    }
+    wave_lds_fence();
+    const int g = lane / per;
+    tk.group = group_best(p, row, lane, per, g);
+    // a group's rank, in all of its lanes
+    int rank = 0;
+    for (int h = 0; h < p.n_groups; ++h) {
+      const float v = lane_value(tk.group.sum, h * per);
+      rank += v > tk.group.sum || (v == tk.group.sum && h < g);
+    }
+    const bool is = g < p.n_groups;
+    tk.stays = is && rank < p.top_groups;
+    // the least kept group against the best of the others
+    tk.in = -wave_max(tk.stays ? -tk.group.sum : none);
+    tk.out = wave_max(is && !tk.stays ? tk.group.sum : none);
+    tk.groups_open = tk.out > none && tk.in - tk.out <= 2.0f * group_margin(tk);
+    keep_groups(p, tk);
+    wave_lds_fence();
+  }
+}
+
+// Slots of the kept experts by their fp32 keys.
+template <int C>
+__device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& tk) {
+  const int lane = threadIdx.x & 63;
+  uint32_t hk[C];
+  int he[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    row[c * 64 + lane] = tk.l[c];
+    hk[c] = tk.kept[c] ? float_key(tk.key[c] + 0.0f) : 0u;  // (one zero)
+    he[c] = c * 64 + lane;
+  }
+  sort_lane(hk, he);
+  tk.sel = -1;
+  uint64_t near = 0;
+  float last = 0.0f;
+  for (int k = 0; k < p.K; ++k) {
+    const uint32_t m = __builtin_amdgcn_readfirstlane(wave_max_u32(hk[0]));
+    if (m == 0) break;  // nobody left
+    last = key_float(m);
+    const int from = __ffsll((unsigned long long)__ballot(hk[0] == m)) - 1;
+    const int e = __builtin_amdgcn_readlane(he[0], from);
+    if (lane == k) tk.sel = e;
+    const bool mine = lane == from;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      hk[c] = mine ? (c + 1 < C ? hk[c + 1] : 0u) : hk[c];
+      he[c] = mine ? (c + 1 < C ? he[c + 1] : 0) : he[c];
+    }
+    near |= __ballot(hk[0] >= float_key(last - tk.margin));
+  }
+  if (near) {
+    // again by the margin of those that count: the slots and what comes near
+    float worst = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      worst = fmaxf(worst, tk.kept[c] && tk.key[c] >= last - tk.margin ? tk.kerr[c] : 0.0f);
+    tk.margin = 2.0f * wave_max(worst);
+    near = 0;
+    for (int k = 0; k < p.K; ++k) {
+      const int e = __builtin_amdgcn_readlane(tk.sel, k);
+      if (e < 0) break;
+      float ke = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        near |= __ballot(tk.kept[c] && c * 64 + lane != e && fabsf(tk.key[c] - ke) <= tk.margin);
+    }
+  }
+  tk.slots_open = near != 0;
+  wave_lds_fence();
+  tk.sl = tk.sel >= 0 ? row[tk.sel] : 0.0f;
+  wave_lds_fence();
+}
+
+// The groups that stay where fp32 sums leave it open: those certainly in or
+// out keep their place (for each, all of the others or enough of them are
+// certainly on the other side of it), and the rest are ranked by the sums of
+// their members that may count, in 64 bits.
+template <class T16, int C, int TW>
+__device__ void settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+  const int lane = threadIdx.x & 63;
+  const int per = lanes_per_group(p), g = lane / per;
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  const double none = -__builtin_inf();
+  const float room = 2.0f * group_margin(tk);
+  const bool contested = g < p.n_groups && tk.group.sum > -__builtin_inff() &&
+                         (tk.stays ? tk.group.sum - tk.out <= room : tk.in - tk.group.sum <= room);
+  const uint64_t cm = __ballot(contested), sure = __ballot(tk.stays && !contested);
+  const int left = p.top_groups - __popcll(sure) / per;
+  bool want[C], again[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = min(group_of(p, c * 64 + lane) * per, 63);
+    const float low = __shfl(tk.group.low, at, 64);
+    want[c] = tk.fit[c] && (cm >> at & 1) && tk.val[c] >= low - room;
+    again[c] = want[c] && tk.err[c] > 0.0f;
+  }
+  double l[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) l[c] = tk.l[c];
+  sum_again<T16, C, TW>(p, xr, again, lds, [&](int c, int at, double v) {
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (i == c && lane == at) l[i] = v;
+  });
+  if (Team<TW>::lead()) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      // (a softmax's denominator is common to all groups without a bias)
+      const double sc = soft ? exp(l[c] - tk.top) : 1.0 / (1.0 + exp(-l[c]));
+      lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
+    }
+  }
+  Team<TW>::sync();
+  const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
+  int rank = 0;
+  for (int h = 0; h < p.n_groups; ++h) {
+    if (!(cm >> (h * per) & 1)) continue;
+    const double v = lane_value(gb.sum, h * per);
+    rank += v > gb.sum || (v == gb.sum && h < g);
+  }
+  tk.stays = (sure >> lane & 1) || (contested && rank < left);
+  keep_groups(p, tk);
+  Team<TW>::sync();
+}
+
+// The order of the slots where only neighbours of it are open: the experts
+// within the margin of a slot's key are summed again, and those and the other
+// slots ranked anew, a lane each.  Every expert outside is certainly below
+// all slots.  False where this does not decide: too many experts, or a
+// softmax's denominator that is not known well enough.
+template <class T16, int C, int TW>
+__device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+  const int lane = threadIdx.x & 63;
+  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
+  bool want[C], slot[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) want[c] = slot[c] = false;
+  for (int k = 0; k < p.K; ++k) {
+    const int e = __builtin_amdgcn_readlane(tk.sel, k);
+    if (e < 0) break;
+    float ke = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
+    uint64_t near = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const bool self = c * 64 + lane == e;
+      const bool n = tk.kept[c] && !self && fabsf(tk.key[c] - ke) <= tk.margin;
+      want[c] |= n;
+      slot[c] |= self;
+      near |= __ballot(n);
+    }
+    if (near) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) want[c] |= c * 64 + lane == e;
+    }
+  }
+  int n = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) n += __popcll(__ballot(want[c] || slot[c]));
+  if (n > 32) return false;
+  bool again[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) again[c] = want[c] && tk.err[c] > 0.0f;
+  // lane u: member u, its logit and bias
+  int me = -1, at = 0;
+  double ml = 0.0;
+  float mb = 0.0f;
+  const auto add = [&](int c, int j, double v) {
+    float bj = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (i == c) bj = lane_value(tk.b[i], j);
+    if (lane == at) {
+      me = c * 64 + j;
+      ml = v;
+      mb = bj;
+    }
+    ++at;
+  };
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    uint64_t m = __ballot((slot[c] || want[c]) && !again[c]);
+    for (; m; m &= m - 1) {
+      const int j = __ffsll((unsigned long long)m) - 1;
+      add(c, j, lane_value(tk.l[c], j));
+    }
+  }
+  sum_again<T16, C, TW>(p, xr, again, lds, add);
+  double s = 0.0, k = ml;
+  if (biased) {
+    s = soft ? exp(ml - tk.top) / tk.z : 1.0 / (1.0 + exp(-ml));
+    k = s + mb;
+  }
+  const bool in = lane < n;
+  int rank = 0;
+  bool unsure = false;
+  for (int u = 0; u < n; ++u) {
+    const double ku = lane_value(k, u), su = lane_value(s, u);
+    const int eu = __builtin_amdgcn_readlane(me, u);
+    rank += ku > k || (ku == k && eu < me);
+    unsure |= soft && biased && u != lane && fabs(ku - k) <= 1.01 * tk.zrel * fabs(su - s);
+  }
+  if (__ballot(in && unsure)) return false;
+  const int K = min(p.K, n);
+  tk.sel = -1;
+  for (int r = 0; r < K; ++r) {
+    const int u = __ffsll((unsigned long long)__ballot(in && rank == r)) - 1;
+    const int e = __builtin_amdgcn_readlane(me, u);
+    const float v = (float)lane_value(ml, u);
+    if (lane == r) {
+      tk.sel = e;
+      tk.sl = v;
+    }
+  }
+  return true;
+}
+
+// Weights and outputs of token t from its selection, by one wave.  counts: the
+// block's, in LDS.
+template <int C>
+__device__ inline void finish(const RouterParams& p, int t, const Token<C>& tk, const RouterOut& o,
+                              int32_t* counts) {
+  const int lane = threadIdx.x & 63;
+  const float none = -__builtin_inff();
+  const bool soft = p.score == SCORE_SOFTMAX;
+  // shares of the selected scores, so that scores that underflow still have
+  // their ratios
+  const int sel = tk.sel;
+  const bool have = sel >= 0;
+  const float lm = wave_max(have ? tk.sl : none);  // (by every lane of the wave)
+  float ex = 0.0f;
+  if (soft || lm < -60.0f) {
+    // (the logarithm of a sigmoid that far out is its logit to all bits)
+    ex = have ? expf(tk.sl - lm) : 0.0f;
+  } else {
+    ex = have ? 1.0f / (1.0f + expf(-tk.sl)) : 0.0f;
+  }
+  const float sum = wave_sum_dpp(ex);
+  const float share = have ? ex / sum : 0.0f;
+  float w = share;
+  if (!p.renorm) w = !have ? 0.0f : soft ? ex * expf(lm - tk.top) / tk.z : 1.0f / (1.0f + expf(-tk.sl));
+  w *= p.scale;
+  // Eq. 2 over the shares: the score of a slot is the sum of those above it
+  int prec = PREC_SKIP;
+  if (o.table) {
+    float above = 0.0f;
+    bool first = true;
+    for (int j = 0; j < p.K; ++j) {
+      const float sj = lane_value(share, j);
+      if (sj > share || (sj == share && j < lane)) {
+        above += sj;
+        first = false;
+      }
+    }
+    if (have) {
+      const int tag = o.table[sel].tag;
+      if (tag == TAG_FP16 || tag == TAG_INT8) prec = PREC_HIGH;
+      else if (tag == TAG_INT4 || tag == TAG_INT2) prec = PREC_LOW;
+      else prec = first || above <= o.t1 ? PREC_HIGH : above <= o.t2 ? PREC_LOW : PREC_SKIP;
+    }
+  }
+  if (lane < p.K) {
+    const int64_t i = (int64_t)t * p.K + lane;
+    o.idx[i] = sel;
+    o.w[i] = w;
+    if (o.prec) o.prec[i] = (int8_t)prec;
+    if (o.user_idx) o.user_idx[i] = sel;
+    if (o.user_w) o.user_w[i] = w;
+    if (o.user_prec) o.user_prec[i] = (int8_t)prec;
+    if (o.count && have) atomicAdd(&counts[sel], 1);
+  }
+}
+
+// Selection of a token whose logits are loaded.
+template <class T16, int C, int TW>
+__device__ inline void select_token(const RouterParams& p, const T16* xr, float* row, Token<C>& tk,
+                                    OpenLds<C>& lds) {
+  score_token(p, row, tk);
+  // (scores that share an uncertain denominator beside biases that do not)
+  bool open = tk.groups_open && p.bias && p.score == SCORE_SOFTMAX;
+  if (!open) {
+    if (tk.groups_open) settle_groups<T16, C, TW>(p, xr, tk, lds);
+    take_slots(p, row, tk);
+    if (tk.slots_open) open = !select_slots<T16, C, TW>(p, xr, tk, lds);
+  }
+  if (open) select_exact<T16, C, TW>(p, xr, tk, lds);
+}
+
+// The block's counts into the call's, by neighbouring lanes: one request per
+// line.  (An atomic per slot on these few lines took 21 us for 1337 tokens of
+// 4 slots.)
+__device__ inline void add_counts(const RouterParams& p, const RouterOut& o, const int32_t* counts) {
+  if (!o.count) return;
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x)
+    if (counts[e]) atomicAdd(o.count + e, counts[e]);
+}
+
+// Many tokens: one per wave in turn; those that fp32 leaves open go on a list.
+// Few blocks of many waves, so that few of them add to the counts.
+constexpr int kManyThreads = 1024;
+constexpr int kManyWaves = kManyThreads / 64;
+constexpr int kManyBlocks = 256;
+template <int C>
+__global__ __launch_bounds__(kManyThreads) void router_select_many_kernel(RouterParams p, int T,
+                                                                          const float* __restrict__ lg,
+                                                                          RouterOut o) {
+  __shared__ float rows[kManyWaves][C * 64];
+  __shared__ int32_t counts[C * 64];
+  __shared__ int32_t n_open, first_open, opens[kManyThreads];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (threadIdx.x == 0) n_open = 0;
+  if (o.count)
+    for (int e = threadIdx.x; e < C * 64; e += kManyThreads) counts[e] = 0;
+  __syncthreads();
+  // (at most 65536 / (16 * 256) = 16 tokens a wave, one slot of opens each)
+  for (int t = blockIdx.x * kManyWaves + wave; t < T; t += gridDim.x * kManyWaves) {
+    Token<C> tk;
+    load_token(p, global<float>(lg + (int64_t)t * p.E), global<float>(p.w_norm), global<float>(p.x_norm)[t], tk);
+    score_token(p, rows[wave], tk);
+    take_slots(p, rows[wave], tk);
+    if (!tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
+    else if ((threadIdx.x & 63) == 0) opens[atomicAdd(&n_open, 1)] = t;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && n_open) first_open = atomicAdd(p.open, n_open);
+  __syncthreads();
+  if ((int)threadIdx.x < n_open) p.open[1 + first_open + threadIdx.x] = opens[threadIdx.x];
+  add_counts(p, o, counts);
+}
+
+// Tokens of a call or of the list, a team of TW waves each.
+constexpr int kTeamThreads = 256;
+template <class T16, int C, int TW>
+__global__ __launch_bounds__(kTeamThreads) void router_select_kernel(RouterParams p, int T, int listed,
+                                                                     const T16* __restrict__ x,
+                                                                     const float* __restrict__ lg,
+                                                                     RouterOut o) {
+  constexpr int kThreads = kTeamThreads, kTeams = kThreads / 64 / TW;
+  __shared__ float rows[kThreads / 64][C * 64];
+  __shared__ OpenLds<C> lds[kTeams];
+  __shared__ int32_t counts[C * 64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave / TW;
+  const int n = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[0]) : T;
+  if ((int)blockIdx.x * kTeams >= n) return;
+  if (o.count) {
+    for (int e = threadIdx.x; e < C * 64; e += kThreads) counts[e] = 0;
+    __syncthreads();
+  }
+  for (int i = blockIdx.x * kTeams + team; i < n; i += gridDim.x * kTeams) {
+    const int t = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[1 + i]) : i;
+    Token<C> tk;
+    load_token(p, global<float>(lg + (int64_t)t * p.E), global<float>(p.w_norm), global<float>(p.x_norm)[t], tk);
+    select_token<T16, C, TW>(p, x + (int64_t)t * p.d, rows[wave], tk, lds[team]);
+    if (wave % TW == 0) finish(p, t, tk, o, counts);
+  }
+  add_counts(p, o, counts);
+}
+
+// ---- logits ---------------------------------------------------------------
 
 // Logits [T, E] of MT * 16 tokens and NT * 16 experts per block.  Every wave
 // takes its share of the columns for the whole tile, 64 columns (a line of
@@ -101,11 +997,14 @@ constexpr float kSumError = 0x1p-24f;
 // the wave's own: 16-byte chunk k of a row r lies at slot k ^ (r & 7), where
 // neither the writes nor the products' reads conflict.
 // Rows past the end are read as the last one and not written.
-template <class T16, int MT, int NT, int NW>
+//
+// kSelect: the block has all experts of its tokens and selects as well, a wave
+// per token (lg: the caller's or null; the counts are cleared beforehand).
+template <class T16, int MT, int NT, int NW, bool kSelect>
 __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, int T,
                                                                 const T16* __restrict__ x,
                                                                 float* __restrict__ lg,
-                                                                int32_t* __restrict__ count) {
+                                                                RouterOut o) {
   typedef typename Vec<T16>::x8 x8;
   constexpr int BM = MT * 16, BN = NT * 16, LD = BN + 4;
   constexpr int LA = 2 * MT, LB = 2 * NT;           // loads of a piece: 8 rows each
@@ -116,11 +1015,11 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
   __shared__ uint32_t nz[NW][BM + BN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t0 = blockIdx.x * BM, e0 = blockIdx.y * BN;
-  const bool norm_x = blockIdx.y == 0, norm_w = blockIdx.x == 0;
-  if (blockIdx.x == 0 && blockIdx.y == 0) {  // what the selection adds to
+  const bool norm_x = blockIdx.y == 0, norm_w = kSelect || blockIdx.x == 0;
+  if (!kSelect && blockIdx.x == 0 && blockIdx.y == 0) {  // what the selection adds to
     if (threadIdx.x == 0) p.open[0] = 0;
-    if (count)
-      for (int e = threadIdx.x; e < p.E; e += NW * 64) count[e] = 0;
+    if (o.count)
+      for (int e = threadIdx.x; e < p.E; e += NW * 64) o.count[e] = 0;
   }
   // this lane's chunks as offsets in bytes from the block's first row (a tile
   // has at most 128 rows of 32 KiB), so that loads take one uniform address
@@ -234,8 +1133,11 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
     float s = red[m * LD + c];
 #pragma unroll
     for (int w = 1; w < NW; ++w) s += red[(w * BM + m) * LD + c];
-    if (t0 + m < T && e0 + c < p.E) lg[(int64_t)(t0 + m) * p.E + e0 + c] = s;
+    const bool in = t0 + m < T && e0 + c < p.E;
+    if (in && lg) lg[(int64_t)(t0 + m) * p.E + e0 + c] = s;
+    if (kSelect) red[m * LD + c] = s;   // (over the first wave's sum, which only this thread reads)
   }
+  __shared__ float bounds[BM + BN];
   for (int v = threadIdx.x; v < BM + BN; v += NW * 64) {
     if (v < BM ? !norm_x : !norm_w) continue;
     float s = 0.0f;
@@ -245,913 +1147,106 @@ __global__ __launch_bounds__(NW * 64) void router_logits_kernel(RouterParams p, 
       z |= nz[w][v];
     }
     const float bound = error_norm(s, z);
-    if (v < BM && t0 + v < T) p.x_norm[t0 + v] = bound;
-    if (v >= BM && e0 + v - BM < p.E) p.w_norm[e0 + v - BM] = bound;
+    if (kSelect) bounds[v] = bound;
+    else if (v < BM && t0 + v < T) p.x_norm[t0 + v] = bound;
+    else if (v >= BM && e0 + v - BM < p.E) p.w_norm[e0 + v - BM] = bound;
   }
-}
-
-// ---- selection ------------------------------------------------------------
-
-__device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
-
-// Sum and maximum of doubles over a wave in registers (see wave_sum_dpp).
-template <int CTRL>
-__device__ inline double dpp_d(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-template <int CTRL>
-__device__ inline double dpp_of(double v) { return dpp_d<CTRL>(v); }
-template <int CTRL>
-__device__ inline float dpp_of(float v) { return dpp_f<CTRL>(v); }
-// The value that lane `from` (the same for all) has.
-__device__ inline float lane_value(float v, int from) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), from));
-}
-__device__ inline double lane_value(double v, int from) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, from);
-  const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), from);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-__device__ inline double pair_d(uint32_t lo, uint32_t hi) {
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-__device__ inline double wave_sum(double v) {
-  v += dpp_d<0xB1>(v);
-  v += dpp_d<0x4E>(v);
-  v += dpp_d<0x141>(v);
-  v += dpp_d<0x140>(v);
-  uint64_t u = __builtin_bit_cast(uint64_t, v);
-  auto l = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
-  auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-  v = pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
-  u = __builtin_bit_cast(uint64_t, v);
-  l = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
-  h = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
-  return pair_d(l[0], h[0]) + pair_d(l[1], h[1]);
-}
-__device__ inline double wave_max(double v) {
-  // order-preserving key, its upper half first
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint64_t k = u >> 63 ? ~u : u | 1ull << 63;
-  const uint32_t hi = wave_max_u32((uint32_t)(k >> 32));
-  const uint32_t lo = wave_max_u32((uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-  const uint64_t m = (uint64_t)hi << 32 | lo;
-  return __builtin_bit_cast(double, m >> 63 ? m & ~(1ull << 63) : ~m);
-}
-__device__ inline float key_float(uint32_t k) {
-  return __builtin_bit_cast(float, (k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
-}
-__device__ inline float wave_max(float v) { return key_float(wave_max_u32(float_key(v))); }
-
-// LDS of one wave is written and read by that wave alone.
-__device__ inline void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// x . w over d columns by one wave, in 64 bits (a product of two 16-bit
-// numbers is exact there).  Every lane gets the sum.
-template <class T16>
-__device__ inline double exact_dot(const T16* x, const T16* w, int d) {
-  typedef typename Vec<T16>::x8 x8;
-  constexpr int B = 8;  // pieces whose loads are in flight together
-  double s = 0.0;
-  for (int c0 = (threadIdx.x & 63) * 8; c0 < d; c0 += 512 * B) {
-    x8 a[B], b[B];
-#pragma unroll
-    for (int i = 0; i < B; ++i) {
-      const int c = min(c0 + 512 * i, d - 8);
-      a[i] = *global<x8>(x + c);
-      b[i] = *global<x8>(w + c);
-    }
-#pragma unroll
-    for (int i = 0; i < B; ++i)
-      if (c0 + 512 * i < d) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s = fma((double)(float)a[i][j], (double)(float)b[i][j], s);
-      }
-  }
-  return wave_sum(s);
-}
-
-// Two best values of each group and what decides about it: 64 / G lanes per
-// group (G the groups rounded up to a power of two) scan its members and join.
-template <class F>
-struct GroupBest {
-  F sum;   // of the group's best one or two; -inf for a group without any
-  F low;   // the least value that counts in it
-};
-template <class F>
-__device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, int lane, int per, int g) {
-  const F none = -__builtin_inff();
-  const int size = p.E / p.n_groups;
-  F best = none, second = none;
-  if (g < p.n_groups)
-    for (int i = lane & (per - 1); i < size; i += per) {
-      const F v = row[g * size + i];
-      second = v > best ? best : v > second ? v : second;
-      best = v > best ? v : best;
-    }
-  const auto join = [&](F ob, F os) {
-    const F lo = ob > best ? best : ob;
-    second = os > second ? os : second;
-    second = lo > second ? lo : second;
-    best = ob > best ? ob : best;
-  };
-  // lane ^ 1, lane ^ 2, mirrors in 8 and 16, then the other row of 16 and half
-  if (per > 1) join(dpp_of<0xB1>(best), dpp_of<0xB1>(second));
-  if (per > 2) join(dpp_of<0x4E>(best), dpp_of<0x4E>(second));
-  if (per > 4) join(dpp_of<0x141>(best), dpp_of<0x141>(second));
-  if (per > 8) join(dpp_of<0x140>(best), dpp_of<0x140>(second));
-  if (per > 16) join(__shfl_xor(best, 16, 64), __shfl_xor(second, 16, 64));
-  if (per > 32) join(__shfl_xor(best, 32, 64), __shfl_xor(second, 32, 64));
-  const bool two = p.group_best == 2 && second > none;
-  return {two ? best + second : best, two ? second : best};
-}
-
-// One token's fp32 selection, by one wave: lane i has the experts i, i + 64,
-// ... (C of them), lane k slot k.
-template <int C>
-struct Token {
-  float l[C], b[C], key[C], kerr[C];
-  float val[C];       // what groups count
-  bool exact[C];      // its row or the token's is all zeros: so is the sum
-  bool fit[C];        // can be selected at all
-  bool kept[C];       // ... and lies in a group that stays
-  // lanes of group g (lanes_per_group of them): its best members, whether it
-  // stays, the least sum that does and the largest that does not
-  GroupBest<float> group;
-  bool stays;
-  float in, out, group_err;
-  float top, z, zrel; // softmax: largest logit, denominator, its relative error
-  float margin;       // keys further apart are certainly in order
-  bool groups_open, slots_open;
-  int sel;
-  float sl;           // its logit
-};
-
-__device__ inline int lanes_per_group(const RouterParams& p) {
-  int per = 64;
-  while (64 / per < p.n_groups) per >>= 1;
-  return per;
-}
-
-// Error of a group's sum.
-template <int C>
-__device__ inline float group_margin(const Token<C>& tk) {
-  return tk.group_err + 5e-7f * fmaxf(fabsf(tk.in), fabsf(tk.out));
-}
-
-// The experts of the groups that stay.
-template <int C>
-__device__ inline void keep_groups(const RouterParams& p, Token<C>& tk) {
-  const int lane = threadIdx.x & 63, size = p.E / p.n_groups, per = lanes_per_group(p);
-  const uint64_t at = __ballot(tk.stays);
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-    tk.kept[c] = tk.fit[c] && (at >> min((c * 64 + lane) / size * per, 63) & 1);
-}
-
-// LDS of a block that works on one token whose selection is open.
-template <int C>
-struct OpenLds {
-  double row[C * 64];    // keys or scores for the groups' scan
-  double dots[C * 64];   // logits summed again
-  int32_t list[C * 64];  // ... and their experts
-  double sum[kRouterMaxGroups], low[kRouterMaxGroups];
-  float err[kRouterMaxGroups], more[2][kRouterMaxGroups];
-};
-
-// Sums the logits of the experts of `want` again, in 64 bits, the block's
-// waves in turn; take(c, lane, value) gets each.  Every wave has the same
-// `want` and calls this.
-template <class T16, int C, class Take>
-__device__ inline void sum_again(const RouterParams& p, const T16* xr, const bool (&want)[C],
-                                 OpenLds<C>& lds, Take take) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int n = 0;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const uint64_t m = __ballot(want[c]);
-    if (want[c] && threadIdx.x < 64)
-      lds.list[n + __popcll(m & ((1ull << lane) - 1ull))] = c * 64 + lane;
-    n += __popcll(m);
-  }
-  __syncthreads();
-  for (int i = wave; i < n; i += (int)(blockDim.x >> 6)) {
-    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
-    const double v = exact_dot(xr, static_cast<const T16*>(p.wg) + (int64_t)e * p.d, p.d);
-    if (lane == 0) lds.dots[i] = v;
-  }
-  __syncthreads();
-  for (int i = 0; i < n; ++i) {
-    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
-    take(e >> 6, e & 63, lds.dots[i]);
-  }
-  __syncthreads();
-}
-
-// The selection by 64-bit sums, whatever is open: experts whose order or group
-// is not certain are summed again (bound 0) until nothing is open.
-template <class T16, int C>
-__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, float xn,
-                             OpenLds<C>& lds) {
-  const int lane = threadIdx.x & 63;
-  const double none = -__builtin_inf();
-  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  double l[C];
-  float err[C];
-  bool want[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int e = c * 64 + lane;
-    l[c] = tk.l[c];
-    err[c] = 0.0f;
-    if (e < p.E && finite(tk.l[c])) {
-      const float n = global<float>(p.w_norm)[e];
-      // (rounding to fp32 sums below the smallest numbers adds to the bound)
-      err[c] = n > 0.0f && xn > 0.0f ? fminf(kSumError * xn * n + 1e-33f, 1e30f) : 0.0f;
-    }
-    want[c] = false;
-  }
-  const int per = lanes_per_group(p);
-  for (;;) {
-    sum_again(p, xr, want, lds, [&](int c, int at, double v) {
-#pragma unroll
-      for (int i = 0; i < C; ++i)
-        if (i == c && lane == at) {
-          l[i] = v;
-          err[i] = 0.0f;
-        }
-    });
-    double key[C], sc[C], kerr[C];
-    bool fit[C];
-    double zrel = 0.0;
-    if (soft) {
-      double top = none, z = 0.0;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (finite(tk.l[c])) top = fmax(top, l[c]);
-      top = wave_max(top);
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        sc[c] = finite(tk.l[c]) ? exp(l[c] - top) : 0.0;
-        z += sc[c];
-      }
-      z = wave_sum(z);
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        sc[c] = finite(tk.l[c]) ? sc[c] / z : 0.0;
-        zrel += sc[c] * err[c];
-      }
-      zrel = biased ? 1.01 * wave_sum(zrel) : 0.0;  // (without a bias the sum is common to all)
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c) sc[c] = finite(tk.l[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      fit[c] = tk.fit[c];
-      want[c] = false;
-      // slope of a score by its logit: s of the softmax's term, 1/4 at most of a sigmoid
-      const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
-      key[c] = biased ? sc[c] + tk.b[c] : l[c];
-      kerr[c] = biased ? serr : err[c];
-    }
-    bool open = false;
-    if (p.n_groups > 1) {
-      const int size = p.E / p.n_groups;
-      if (threadIdx.x < 64) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
-        lds.more[0][lane] = lds.more[1][lane] = 0.0f;
-      }
-      __syncthreads();
-      const int g = lane / per;
-      const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
-      if (threadIdx.x < 64 && (lane & (per - 1)) == 0) {
-        lds.sum[g] = gb.sum;
-        lds.low[g] = gb.low;
-      }
-      // A group's error: that of its most uncertain member, once or twice,
-      // among those that may be one of its best - that reach, with their own
-      // bound, down to the least that counts less the bounds of what counts.
-#pragma unroll
-      for (int round = 0; round < 2; ++round) {
-        __syncthreads();
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int e = c * 64 + lane;
-          if (!fit[c]) continue;
-          const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
-          const double reach = round == 0 ? lds.row[e] : lds.row[e] + serr + lds.err[e / size];
-          const bool in = reach >= lds.low[e / size];
-          if (round == 1) want[c] = in && err[c] > 0.0f;
-          if (in && serr > 0.0 && threadIdx.x < 64)
-            atomicMax(reinterpret_cast<unsigned*>(&lds.more[round][e / size]),
-                      __float_as_uint((float)(serr * 1.0001)));
-        }
-        __syncthreads();
-        if (threadIdx.x < 64) lds.err[lane] = lds.more[round][lane];
-      }
-      __syncthreads();
-      const bool is = lane < p.n_groups;
-      const double mine = is ? lds.sum[lane] : none;
-      int rank = 0;
-      for (int h = 0; h < p.n_groups; ++h) rank += lds.sum[h] > mine || (lds.sum[h] == mine && h < lane);
-      const uint64_t kept = __ballot(is && rank < p.top_groups);
-      bool unsure = false;
-      if (is && mine > none)
-        for (int h = 0; h < p.n_groups; ++h) {
-          const double v = lds.sum[h];
-          if (v > none && (kept >> lane & 1) != (kept >> h & 1))
-            unsure |= fabs(v - mine) <= p.group_best * ((double)lds.err[lane] + lds.err[h]) +
-                                            zrel * fmax(fabs(v), fabs(mine));
-        }
-      const uint64_t um = __ballot(unsure && (lds.err[lane] > 0.0f || zrel > 0.0));
-      open = um != 0;
-#pragma unroll
-      for (int c = 0; c < C; ++c) want[c] = want[c] && (um >> ((c * 64 + lane) / size) & 1);
-#pragma unroll
-      for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
-      __syncthreads();
-    }
-    if (!open) {
-      tk.sel = -1;
-      for (int k = 0; k < p.K; ++k) {
-        double bk = none;
-        bool any = false;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (fit[c]) {
-            bk = any ? fmax(bk, key[c]) : key[c];
-            any = true;
-          }
-        bk = wave_max(bk);
-        int be = -1;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const uint64_t m = __ballot(fit[c] && key[c] == bk);
-          if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
-        }
-        be = __builtin_amdgcn_readfirstlane(be);
-        if (be < 0) break;  // nobody left
-        double ml = 0.0, ms = 0.0, me = 0.0;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (c * 64 + lane == be) {
-            fit[c] = false;
-            ml = l[c];
-            ms = sc[c];
-            me = kerr[c];
-          }
-        ml = lane_value(ml, be & 63);
-        ms = lane_value(ms, be & 63);
-        me = lane_value(me, be & 63);
-        if (lane == k) {
-          tk.sel = be;
-          tk.sl = (float)ml;
-        }
-        bool near = false;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const double room = me + kerr[c] + zrel * fabs(ms - sc[c]);
-          if (fit[c] && room > 0.0 && bk - key[c] <= room) {
-            near = true;
-            want[c] = want[c] || err[c] > 0.0f;
-          }
-        }
-        if (__ballot(near)) {
-          open = true;
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (c * 64 + lane == be) want[c] = want[c] || err[c] > 0.0f;
-        }
-      }
-    }
-    if (!open) return;
-    bool some = false;
-#pragma unroll
-    for (int c = 0; c < C; ++c) some |= want[c];
-    if (!__ballot(some)) {
-      // only the softmax's denominator is uncertain: every logit that it adds
-#pragma unroll
-      for (int c = 0; c < C; ++c) want[c] = err[c] > 0.0f;
-    }
-  }
-}
-
-// log sigmoid(l) without overflow or loss far from 0
-__device__ inline float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
-
-// Descending order of a lane's C keys, each with its number c.
-template <int C>
-__device__ inline void sort_lane(uint32_t (&k)[C], int (&e)[C]) {
-  const auto step = [&](int i, int j) {
-    const bool swap = k[j] > k[i];
-    const uint32_t kt = swap ? k[j] : k[i];
-    k[j] = swap ? k[i] : k[j];
-    k[i] = kt;
-    const int et = swap ? e[j] : e[i];
-    e[j] = swap ? e[i] : e[j];
-    e[i] = et;
-  };
-  // odd-even merging: pairs, fours, eights
-#pragma unroll
-  for (int n = 1; n < C; n *= 2)
-#pragma unroll
-    for (int m = n; m >= 1; m /= 2)
-#pragma unroll
-      for (int j = m % n; j + m < C; j += 2 * m)
-#pragma unroll
-        for (int i = 0; i < m; ++i)
-          if (i + j + m < C && (i + j) / (2 * n) == (i + j + m) / (2 * n)) step(i + j, i + j + m);
-}
-
-// Scores, keys and groups of token t in fp32.  Keys are compared with one
-// margin, twice the largest bound of their errors.  For the slots each lane
-// sorts its keys, and a slot takes the largest of the lanes' first ones
-// (take_slots).  row: C * 64 floats of LDS of the wave's own.
-template <int C>
-__device__ inline void score_token(const RouterParams& p, int t, const float* lg, float xn,
-                                   float* row, Token<C>& tk) {
-  const int lane = threadIdx.x & 63;
-  const float none = -__builtin_inff();
-  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  float err[C], sc[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int e = c * 64 + lane;
-    const bool in = e < p.E;
-    tk.l[c] = in ? lg[(int64_t)t * p.E + e] : none;
-    tk.b[c] = in && biased ? global<float>(p.bias)[e] : 0.0f;
-    err[c] = in ? global<float>(p.w_norm)[e] : 0.0f;
-  }
-  float worst = 0.0f;
-  tk.top = none;
-  tk.z = 0.0f;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    tk.fit[c] = finite(tk.l[c]);
-    if (tk.fit[c]) tk.top = fmaxf(tk.top, tk.l[c]);
-    // (rounding to fp32 of the smallest numbers adds to a bound)
-    err[c] = xn > 0.0f && err[c] > 0.0f ? fminf(kSumError * xn * err[c] + 1e-33f, 1e30f) : 0.0f;
-    tk.exact[c] = err[c] == 0.0f;
-    worst = fmaxf(worst, tk.fit[c] ? err[c] : 0.0f);
-  }
-  // The scores by the fast exponential and reciprocal: within 1e-6 of a
-  // score, and of a softmax's term 1e-6 for each unit below the largest.
-  tk.zrel = soft ? wave_max(worst) + 4e-6f : 0.0f;
-  if (soft) {
-    tk.top = wave_max(tk.top);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      sc[c] = tk.fit[c] ? __expf(tk.l[c] - tk.top) : 0.0f;
-      tk.z += sc[c];
-    }
-    tk.z = wave_sum_dpp(tk.z);
-  }
-  float verr = 0.0f;  // largest error of what groups count
-  worst = 0.0f;
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    float e1;
-    if (soft) {
-      sc[c] = tk.fit[c] ? sc[c] * __frcp_rn(tk.z) : 0.0f;
-      e1 = tk.fit[c] ? sc[c] * 1.01f * (err[c] + tk.zrel + 1e-6f * (tk.top - tk.l[c])) : 0.0f;
-    } else {
-      sc[c] = tk.fit[c] ? __frcp_rn(1.0f + __expf(-tk.l[c])) : 0.0f;
-      // (the sigmoid's slope here, and what it may change by within the bound)
-      e1 = err[c] * (1.001f * sc[c] * (1.0f - sc[c]) + 0.1f * err[c]) + 1e-6f * sc[c];
-    }
-    tk.key[c] = tk.l[c];
-    if (biased) {
-      tk.fit[c] = tk.fit[c] && finite(tk.b[c]);
-      tk.key[c] = sc[c] + tk.b[c];
-      e1 += 1e-7f * fabsf(tk.key[c]);
-    }
-    verr = fmaxf(verr, tk.fit[c] ? e1 : 0.0f);
-    tk.kerr[c] = biased ? e1 : err[c];
-    worst = fmaxf(worst, tk.fit[c] ? tk.kerr[c] : 0.0f);
-    tk.kept[c] = tk.fit[c];
-  }
-  tk.margin = 2.0f * wave_max(worst);
-  tk.group_err = p.group_best * wave_max(verr);
-  tk.groups_open = false;
-  if (p.n_groups > 1) {
-    const int size = p.E / p.n_groups;
-    const int per = lanes_per_group(p);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      tk.val[c] = tk.fit[c] ? (biased ? tk.key[c] : sc[c]) : none;
-      row[c * 64 + lane] = tk.val[c];
-    }
-    wave_lds_fence();
-    const int g = lane / per;
-    tk.group = group_best(p, row, lane, per, g);
-    // a group's rank, in all of its lanes
-    int rank = 0;
-    for (int h = 0; h < p.n_groups; ++h) {
-      const float v = lane_value(tk.group.sum, h * per);
-      rank += v > tk.group.sum || (v == tk.group.sum && h < g);
-    }
-    const bool is = g < p.n_groups;
-    tk.stays = is && rank < p.top_groups;
-    // the least kept group against the best of the others
-    tk.in = -wave_max(tk.stays ? -tk.group.sum : none);
-    tk.out = wave_max(is && !tk.stays ? tk.group.sum : none);
-    tk.groups_open = tk.out > none && tk.in - tk.out <= 2.0f * group_margin(tk);
-    keep_groups(p, tk);
-    wave_lds_fence();
-  }
-}
-
-// Slots of the kept experts by their fp32 keys.
-template <int C>
-__device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& tk) {
-  const int lane = threadIdx.x & 63;
-  uint32_t hk[C];
-  int he[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    row[c * 64 + lane] = tk.l[c];
-    hk[c] = tk.kept[c] ? float_key(tk.key[c] + 0.0f) : 0u;  // (one zero)
-    he[c] = c * 64 + lane;
-  }
-  sort_lane(hk, he);
-  tk.sel = -1;
-  uint64_t near = 0;
-  float last = 0.0f;
-  for (int k = 0; k < p.K; ++k) {
-    const uint32_t m = __builtin_amdgcn_readfirstlane(wave_max_u32(hk[0]));
-    if (m == 0) break;  // nobody left
-    last = key_float(m);
-    const int from = __ffsll((unsigned long long)__ballot(hk[0] == m)) - 1;
-    const int e = __builtin_amdgcn_readlane(he[0], from);
-    if (lane == k) tk.sel = e;
-    const bool mine = lane == from;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      hk[c] = mine ? (c + 1 < C ? hk[c + 1] : 0u) : hk[c];
-      he[c] = mine ? (c + 1 < C ? he[c + 1] : 0) : he[c];
-    }
-    near |= __ballot(hk[0] >= float_key(last - tk.margin));
-  }
-  if (near) {
-    // again by the margin of those that count: the slots and what comes near
-    float worst = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      worst = fmaxf(worst, tk.kept[c] && tk.key[c] >= last - tk.margin ? tk.kerr[c] : 0.0f);
-    tk.margin = 2.0f * wave_max(worst);
-    near = 0;
-    for (int k = 0; k < p.K; ++k) {
-      const int e = __builtin_amdgcn_readlane(tk.sel, k);
-      if (e < 0) break;
-      float ke = 0.0f;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        near |= __ballot(tk.kept[c] && c * 64 + lane != e && fabsf(tk.key[c] - ke) <= tk.margin);
-    }
-  }
-  tk.slots_open = near != 0;
-  wave_lds_fence();
-  tk.sl = tk.sel >= 0 ? row[tk.sel] : 0.0f;
-  wave_lds_fence();
-}
-
-// The groups that stay where fp32 sums leave it open: those certainly in or
-// out keep their place (for each, all of the others or enough of them are
-// certainly on the other side of it), and the rest are ranked by the sums of
-// their members that may count, in 64 bits.
-template <class T16, int C>
-__device__ void settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
-  const int lane = threadIdx.x & 63;
-  const int size = p.E / p.n_groups, per = lanes_per_group(p), g = lane / per;
-  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  const double none = -__builtin_inf();
-  const float room = 2.0f * group_margin(tk);
-  const bool contested = g < p.n_groups && tk.group.sum > -__builtin_inff() &&
-                         (tk.stays ? tk.group.sum - tk.out <= room : tk.in - tk.group.sum <= room);
-  const uint64_t cm = __ballot(contested), sure = __ballot(tk.stays && !contested);
-  const int left = p.top_groups - __popcll(sure) / per;
-  bool want[C], again[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int at = min((c * 64 + lane) / size * per, 63);
-    const float low = __shfl(tk.group.low, at, 64);
-    want[c] = tk.fit[c] && (cm >> at & 1) && tk.val[c] >= low - room;
-    again[c] = want[c] && !tk.exact[c];
-  }
-  double l[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) l[c] = tk.l[c];
-  sum_again(p, xr, again, lds, [&](int c, int at, double v) {
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-      if (i == c && lane == at) l[i] = v;
-  });
-  if (threadIdx.x < 64) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      // (a softmax's denominator is common to all groups without a bias)
-      const double sc = soft ? exp(l[c] - tk.top) : 1.0 / (1.0 + exp(-l[c]));
-      lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
-    }
-  }
-  __syncthreads();
-  const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
-  int rank = 0;
-  for (int h = 0; h < p.n_groups; ++h) {
-    if (!(cm >> (h * per) & 1)) continue;
-    const double v = lane_value(gb.sum, h * per);
-    rank += v > gb.sum || (v == gb.sum && h < g);
-  }
-  tk.stays = (sure >> lane & 1) || (contested && rank < left);
-  keep_groups(p, tk);
-  __syncthreads();
-}
-
-// The order of the slots where only neighbours of it are open: the experts
-// within the margin of a slot's key are summed again, and those and the other
-// slots ranked anew, a lane each.  Every expert outside is certainly below
-// all slots.  False where this does not decide: too many experts, or a
-// softmax's denominator that is not known well enough.
-template <class T16, int C>
-__device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
-  const int lane = threadIdx.x & 63;
-  const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  bool want[C], slot[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) want[c] = slot[c] = false;
-  for (int k = 0; k < p.K; ++k) {
-    const int e = __builtin_amdgcn_readlane(tk.sel, k);
-    if (e < 0) break;
-    float ke = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (e >> 6 == c) ke = lane_value(tk.key[c], e & 63);
-    uint64_t near = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const bool self = c * 64 + lane == e;
-      const bool n = tk.kept[c] && !self && fabsf(tk.key[c] - ke) <= tk.margin;
-      want[c] |= n;
-      slot[c] |= self;
-      near |= __ballot(n);
-    }
-    if (near) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) want[c] |= c * 64 + lane == e;
-    }
-  }
-  int n = 0;
-#pragma unroll
-  for (int c = 0; c < C; ++c) n += __popcll(__ballot(want[c] || slot[c]));
-  if (n > 32) return false;
-  bool again[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) again[c] = want[c] && !tk.exact[c];
-  // lane u: member u, its logit and bias
-  int me = -1, at = 0;
-  double ml = 0.0;
-  float mb = 0.0f;
-  const auto add = [&](int c, int j, double v) {
-    float bj = 0.0f;
-#pragma unroll
-    for (int i = 0; i < C; ++i)
-      if (i == c) bj = lane_value(tk.b[i], j);
-    if (lane == at) {
-      me = c * 64 + j;
-      ml = v;
-      mb = bj;
-    }
-    ++at;
-  };
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    uint64_t m = __ballot((slot[c] || want[c]) && !again[c]);
-    for (; m; m &= m - 1) {
-      const int j = __ffsll((unsigned long long)m) - 1;
-      add(c, j, lane_value(tk.l[c], j));
-    }
-  }
-  sum_again(p, xr, again, lds, add);
-  double s = 0.0, k = ml;
-  if (biased) {
-    s = soft ? exp(ml - tk.top) / tk.z : 1.0 / (1.0 + exp(-ml));
-    k = s + mb;
-  }
-  const bool in = lane < n;
-  int rank = 0;
-  bool unsure = false;
-  for (int u = 0; u < n; ++u) {
-    const double ku = lane_value(k, u), su = lane_value(s, u);
-    const int eu = __builtin_amdgcn_readlane(me, u);
-    rank += ku > k || (ku == k && eu < me);
-    unsure |= soft && biased && u != lane && fabs(ku - k) <= 1.01 * tk.zrel * fabs(su - s);
-  }
-  if (__ballot(in && unsure)) return false;
-  const int K = min(p.K, n);
-  tk.sel = -1;
-  for (int r = 0; r < K; ++r) {
-    const int u = __ffsll((unsigned long long)__ballot(in && rank == r)) - 1;
-    const int e = __builtin_amdgcn_readlane(me, u);
-    const float v = (float)lane_value(ml, u);
-    if (lane == r) {
-      tk.sel = e;
-      tk.sl = v;
-    }
-  }
-  return true;
-}
-
-// Weights and outputs of token t from its selection, by one wave.  counts: the
-// block's, in LDS.
-template <int C>
-__device__ inline void finish(const RouterParams& p, int t, const Token<C>& tk, const RouterOut& o,
-                              int32_t* counts) {
-  const int lane = threadIdx.x & 63;
-  const float none = -__builtin_inff();
-  const bool soft = p.score == SCORE_SOFTMAX;
-  // the share of the selected scores by their logarithms, so that scores that
-  // underflow still have their ratios
-  const int sel = tk.sel;
-  const bool have = sel >= 0;
-  const float ls = !have ? none : soft ? tk.sl : log_sigmoid(tk.sl);
-  const float lm = wave_max(ls);  // (by every lane of the wave)
-  const float ex = have ? expf(ls - lm) : 0.0f;
-  const float sum = wave_sum_dpp(ex);
-  const float share = have ? ex / sum : 0.0f;
-  float w = share;
-  if (!p.renorm) w = !have ? 0.0f : soft ? expf(tk.sl - tk.top) / tk.z : 1.0f / (1.0f + expf(-tk.sl));
-  w *= p.scale;
-  // Eq. 2 over the shares: the score of a slot is the sum of those above it
-  int prec = PREC_SKIP;
-  if (o.table) {
-    float above = 0.0f;
-    bool first = true;
-    for (int j = 0; j < p.K; ++j) {
-      const float sj = lane_value(share, j);
-      if (sj > share || (sj == share && j < lane)) {
-        above += sj;
-        first = false;
-      }
-    }
-    if (have) {
-      const int tag = o.table[sel].tag;
-      if (tag == TAG_FP16 || tag == TAG_INT8) prec = PREC_HIGH;
-      else if (tag == TAG_INT4 || tag == TAG_INT2) prec = PREC_LOW;
-      else prec = first || above <= o.t1 ? PREC_HIGH : above <= o.t2 ? PREC_LOW : PREC_SKIP;
-    }
-  }
-  if (lane < p.K) {
-    const int64_t i = (int64_t)t * p.K + lane;
-    o.idx[i] = sel;
-    o.w[i] = w;
-    if (o.prec) o.prec[i] = (int8_t)prec;
-    if (o.user_idx) o.user_idx[i] = sel;
-    if (o.user_w) o.user_w[i] = w;
-    if (o.user_prec) o.user_prec[i] = (int8_t)prec;
-    if (o.count && have) atomicAdd(&counts[sel], 1);
-  }
-}
-
-// The block's counts into the call's, by neighbouring lanes: one request per
-// line.  (An atomic per slot on these few lines took 21 us for 1337 tokens of
-// 4 slots.)
-__device__ inline void add_counts(const RouterParams& p, const RouterOut& o, const int32_t* counts) {
-  if (!o.count) return;
-  __syncthreads();
-  for (int e = threadIdx.x; e < p.E; e += blockDim.x)
-    if (counts[e]) atomicAdd(o.count + e, counts[e]);
-}
-
-// A token per wave in turn; tokens whose selection fp32 leaves open go on a
-// list.  Few blocks of many waves, so that few of them add to the counts.
-constexpr int kManyThreads = 1024;
-constexpr int kManyWaves = kManyThreads / 64;
-constexpr int kManyBlocks = 256;
-template <int C>
-__global__ __launch_bounds__(kManyThreads) void router_select_kernel(RouterParams p, int T,
-                                                                     const float* __restrict__ lg,
-                                                                     RouterOut o) {
-  __shared__ float rows[kManyWaves][C * 64];
-  __shared__ int32_t counts[C * 64];
-  __shared__ int32_t n_open, first_open, opens[kManyThreads];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (threadIdx.x == 0) n_open = 0;
-  if (o.count)
-    for (int e = threadIdx.x; e < C * 64; e += kManyThreads) counts[e] = 0;
-  __syncthreads();
-  // (at most 65536 / (16 * 256) = 16 tokens a wave, one slot of opens each)
-  for (int t = blockIdx.x * kManyWaves + wave; t < T; t += gridDim.x * kManyWaves) {
-    Token<C> tk;
-    score_token(p, t, lg, global<float>(p.x_norm)[t], rows[wave], tk);
-    take_slots(p, rows[wave], tk);
-    if (!tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
-    else if ((threadIdx.x & 63) == 0) opens[atomicAdd(&n_open, 1)] = t;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0 && n_open) first_open = atomicAdd(p.open, n_open);
-  __syncthreads();
-  if ((int)threadIdx.x < n_open) p.open[1 + first_open + threadIdx.x] = opens[threadIdx.x];
-  add_counts(p, o, counts);
-}
-
-// A token per block: the call's, or those of the list.  Every wave makes the
-// same selection; where it is open they share the sums in 64 bits.
-constexpr int kOneThreads = 256;
-constexpr int kListBlocks = 768;
-template <class T16, int C>
-__global__ __launch_bounds__(kOneThreads) void router_select_open_kernel(RouterParams p, int T, int listed,
-                                                                         const T16* __restrict__ x,
-                                                                         const float* __restrict__ lg,
-                                                                         RouterOut o) {
-  __shared__ float rows[kOneThreads / 64][C * 64];
-  __shared__ OpenLds<C> lds;
-  __shared__ int32_t counts[C * 64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[0]) : T;
-  if ((int)blockIdx.x >= n) return;
-  if (o.count) {
-    for (int e = threadIdx.x; e < C * 64; e += kOneThreads) counts[e] = 0;
+  if constexpr (kSelect) {
+    static_assert(BN <= 64, "a lane per expert");
+    __shared__ float rows[NW][64];
+    __shared__ OpenLds<1> open[NW];
+    __shared__ int32_t counts[64];
+    if (o.count && threadIdx.x < 64) counts[threadIdx.x] = 0;
     __syncthreads();
-  }
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
-    const int t = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[1 + i]) : i;
-    const float xn = global<float>(p.x_norm)[t];
-    const T16* xr = x + (int64_t)t * p.d;
-    Token<C> tk;
-    score_token(p, t, lg, xn, rows[wave], tk);
-    // (scores that share an uncertain denominator beside biases that do not)
-    bool open = tk.groups_open && p.bias && p.score == SCORE_SOFTMAX;
-    if (!open) {
-      if (tk.groups_open) settle_groups(p, xr, tk, lds);
-      take_slots(p, rows[wave], tk);
-      if (tk.slots_open) open = !select_slots(p, xr, tk, lds);
+    for (int m = wave; m < BM && t0 + m < T; m += NW) {
+      Token<1> tk;
+      const bool in = lane < p.E;
+      tk.l[0] = in ? red[m * LD + lane] : -__builtin_inff();
+      tk.b[0] = in && p.bias ? global<float>(p.bias)[lane] : 0.0f;
+      tk.err[0] = in ? logit_error(bounds[m], bounds[BM + lane]) : 0.0f;
+      select_token<T16, 1, 1>(p, x + (int64_t)(t0 + m) * p.d, rows[wave], tk, open[wave]);
+      finish(p, t0 + m, tk, o, counts);
     }
-    if (open) select_exact(p, xr, tk, xn, lds);
-    if (wave == 0) finish(p, t, tk, o, counts);
+    add_counts(p, o, counts);
   }
-  add_counts(p, o, counts);
+}
+
+// Counts of a call whose first kernel already adds to them.
+__global__ void router_clear_kernel(int32_t* count, int E) {
+  for (int e = threadIdx.x; e < E; e += blockDim.x) count[e] = 0;
 }
 
 template <class T16, int MT, int NT, int NW>
-hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, int32_t* count, hipStream_t s) {
+hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, const RouterOut& o, hipStream_t s) {
   const dim3 grid((T + MT * 16 - 1) / (MT * 16), (p.E + NT * 16 - 1) / (NT * 16));
-  router_logits_kernel<T16, MT, NT, NW><<<grid, NW * 64, 0, s>>>(p, T, x, lg, count);
+  router_logits_kernel<T16, MT, NT, NW, false><<<grid, NW * 64, 0, s>>>(p, T, x, lg, o);
+  return hipGetLastError();
+}
+
+template <class T16, int C>
+hipError_t select(const RouterParams& p, int T, const T16* x, const float* lg, const RouterOut& o,
+                  hipStream_t s) {
+  // Up to 256 tokens a block each; up to 2048 a wave each, which sums open
+  // ones by itself; more by the kernel that leaves them to another.
+  constexpr int kBlockEach = 256, kWaveEach = 2048, kListBlocks = 768;
+  if (T <= kBlockEach) {
+    router_select_kernel<T16, C, 4><<<T, kTeamThreads, 0, s>>>(p, T, 0, x, lg, o);
+  } else if (T <= kWaveEach) {
+    router_select_kernel<T16, C, 1><<<(T + 3) / 4, kTeamThreads, 0, s>>>(p, T, 0, x, lg, o);
+  } else {
+    const int blocks = (T + kManyWaves - 1) / kManyWaves;
+    router_select_many_kernel<C><<<blocks < kManyBlocks ? blocks : kManyBlocks, kManyThreads, 0, s>>>(p, T, lg, o);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    router_select_kernel<T16, C, 4><<<kListBlocks, kTeamThreads, 0, s>>>(p, T, 1, x, lg, o);
+  }
   return hipGetLastError();
 }
 
 template <class T16>
 hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, hipStream_t s) {
-  float* lg = o.logits ? o.logits : p.logits;
-  // The largest tile that still gives about every compute unit a block: a
-  // block loads (tokens + experts) rows for tokens * experts sums.  us at d
-  // 4096, 256 experts, tiles of 64x64 / 64x32 / 32x32 / 16x32 / 16x16 on eight
-  // waves: 4096 tokens 21.9 26.8 32.8 43.7 53.1, 2048 20.4 15.9 17.9 22.9 28.1,
-  // 1024 19.7 14.6 11.0 13.6 15.6, 512 19.5 14.5 9.9 8.4 9.3, 64 18.9 14.4 9.8
-  // 7.3 5.7.  Two blocks of 64x64 fit a unit on four waves each: 8192 tokens
-  // 35.0, on eight 42.0.  With at most 16 experts the tokens' rows are what is
-  // loaded, and small blocks spread them best: 8192 tokens, 16 experts 16x16
-  // on 16 waves 14.6, 32x16 on eight 18.9.
-  auto blocks = [&](int m, int n) { return (int64_t)((T + m - 1) / m) * ((p.E + n - 1) / n); };
-  constexpr int kEnough = 200;
-  hipError_t e;
-  if (p.E <= 16) e = logits<T16, 1, 1, 16>(p, T, x, lg, o.count, s);
-  else if (blocks(64, 64) >= 2 * kEnough) e = logits<T16, 4, 4, 4>(p, T, x, lg, o.count, s);
-  else if (blocks(64, 64) >= kEnough) e = logits<T16, 4, 4, 8>(p, T, x, lg, o.count, s);
-  else if (blocks(64, 32) >= kEnough) e = logits<T16, 4, 2, 8>(p, T, x, lg, o.count, s);
-  else if (blocks(32, 32) >= kEnough) e = logits<T16, 2, 2, 8>(p, T, x, lg, o.count, s);
-  else if (blocks(16, 32) >= kEnough) e = logits<T16, 1, 2, 8>(p, T, x, lg, o.count, s);
-  else e = logits<T16, 1, 1, 8>(p, T, x, lg, o.count, s);
-  if (e != hipSuccess) return e;
-  // Up to kFew tokens a block each, in one launch; more a wave each, and the
-  // open ones a block each in another.
-  constexpr int kFew = 256;
-  const int C = p.E <= 64 ? 1 : p.E <= 128 ? 2 : p.E <= 256 ? 4 : 8;
-  if (T > kFew) {
-    const int blocks = (T + kManyWaves - 1) / kManyWaves, grid = blocks < kManyBlocks ? blocks : kManyBlocks;
-    if (C == 1) router_select_kernel<1><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
-    else if (C == 2) router_select_kernel<2><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
-    else if (C == 4) router_select_kernel<4><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
-    else router_select_kernel<8><<<grid, kManyThreads, 0, s>>>(p, T, lg, o);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (p.E <= 16) {
+    // all experts in one tile: one kernel
+    if (o.count) {
+      router_clear_kernel<<<1, 64, 0, s>>>(o.count, p.E);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    router_logits_kernel<T16, 1, 1, 8, true><<<(T + 15) / 16, 512, 0, s>>>(p, T, x, o.logits, o);
+    return hipGetLastError();
   }
-  const int listed = T > kFew, grid = listed ? kListBlocks : T;
-  if (C == 1) router_select_open_kernel<T16, 1><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
-  else if (C == 2) router_select_open_kernel<T16, 2><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
-  else if (C == 4) router_select_open_kernel<T16, 4><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
-  else router_select_open_kernel<T16, 8><<<grid, kOneThreads, 0, s>>>(p, T, listed, x, lg, o);
-  return hipGetLastError();
+  float* lg = o.logits ? o.logits : p.logits;
+  // The tile of which the busiest compute unit loads the fewest rows: a block
+  // loads tokens + experts of them, and there are 256 units.  us at d 4096, 256
+  // experts, tiles of 64x64 / 64x32 / 32x32 / 16x32 / 16x16 on eight waves:
+  // 4096 tokens 21.9 26.8 32.8 43.7 53.1, 2048 20.4 15.9 17.9 22.9 28.1, 1024
+  // 19.7 14.6 11.0 13.6 15.6, 512 19.5 14.5 9.9 8.4 9.3, 64 18.9 14.4 9.8 7.3
+  // 5.7.  Two blocks of 64x64 fit a unit on four waves each, which is faster
+  // where there are so many: 8192 tokens 35.0, on eight waves 42.0.
+  constexpr int kTiles[5][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}};
+  int tile = 0;
+  int64_t least = 0, blocks = 0;
+  for (int i = 0; i < 5; ++i) {
+    const int m = kTiles[i][0], n = kTiles[i][1];
+    const int64_t all = (int64_t)((T + m - 1) / m) * ((p.E + n - 1) / n), rows = (all + 255) / 256 * (m + n);
+    if (i == 0 || rows < least) {
+      tile = i;
+      least = rows;
+      blocks = all;
+    }
+  }
+  hipError_t e;
+  if (tile == 0) e = logits<T16, 1, 1, 8>(p, T, x, lg, o, s);
+  else if (tile == 1) e = logits<T16, 1, 2, 8>(p, T, x, lg, o, s);
+  else if (tile == 2) e = logits<T16, 2, 2, 8>(p, T, x, lg, o, s);
+  else if (tile == 3) e = logits<T16, 4, 2, 8>(p, T, x, lg, o, s);
+  else if (blocks <= 256) e = logits<T16, 4, 4, 8>(p, T, x, lg, o, s);
+  else e = logits<T16, 4, 4, 4>(p, T, x, lg, o, s);
+  if (e != hipSuccess) return e;
+  if (p.E <= 64) return select<T16, 1>(p, T, x, lg, o, s);
+  if (p.E <= 128) return select<T16, 2>(p, T, x, lg, o, s);
+  if (p.E <= 256) return select<T16, 4>(p, T, x, lg, o, s);
+  return select<T16, 8>(p, T, x, lg, o, s);
 }
 
 }  // namespace
