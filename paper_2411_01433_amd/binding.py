@@ -242,20 +242,28 @@ def _type16(dtype, name):
     raise ValueError(f"{name} must be torch.float16 or torch.bfloat16, got {dtype}")
 
 
-def _rows(t, dtype, name):
+def _rows(t, name):
     """Shape (T, d) of a two-dimensional tensor argument."""
-    torch = _th()
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+    if not isinstance(t, _th().Tensor) or t.dim() != 2:
         raise ValueError(f"{name} must be a two-dimensional device tensor")
     return t.shape
+
+
+def _on(device, where, *tensors):
+    """Refuse device tensors of another device (a kernel would read them through
+    addresses that mean something else on its own)."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != device:
+            raise ValueError(f"tensors must be on {where} ({device}), got {t.get_device()}")
 
 
 def layernorm(h, x, gain=None, bias=None, eps: float = 1e-5, stream=None):
     """x = layer norm of h, row by row: h fp32 [T, d], x fp16 or bf16 [T, d],
     gain / bias fp32 [d] or None."""
     torch = _th()
-    T, d = _rows(h, torch.float32, "h")
-    _rows(x, None, "x")
+    T, d = _rows(h, "h")
+    _rows(x, "x")
+    _on(torch.cuda.current_device() if h.is_cuda else -1, "the current device", h, x, gain, bias)
     _check(lib().moe_layernorm(
         _addr(h, torch.float32, (T, d), "h"), _addr(gain, torch.float32, (d,), "gain"),
         _addr(bias, torch.float32, (d,), "bias"), _addr(x, x.dtype, (T, d), "x"),
@@ -276,8 +284,10 @@ def layernorm_backward(d_x, h, d_h, gain=None, d_gain=None, d_bias=None, eps: fl
     uint8 of layernorm_workspace(T, d) bytes; without one it is allocated on
     the current stream, which `stream` then has to be (None)."""
     torch = _th()
-    T, d = _rows(h, torch.float32, "h")
-    _rows(d_x, None, "d_x")
+    T, d = _rows(h, "h")
+    _rows(d_x, "d_x")
+    _on(torch.cuda.current_device() if h.is_cuda else -1, "the current device", h, d_x, d_h, gain,
+        d_gain, d_bias, workspace)
     if workspace is None and (d_gain is not None or d_bias is not None):
         if stream is not None:
             raise ValueError("a call on a stream of its own needs a workspace")
@@ -311,10 +321,12 @@ class MoeRouter:
         desc = RouterDesc(d_model, n_experts, top_k, max_tokens, _type16(dtype, "dtype"), score,
                           n_groups, top_groups, group_best, 1 if renormalize else 0, scale,
                           MOE_ROUTER_BACKWARD if backward else 0)
+        gate = _ptr(w_router, dtype, (n_experts, d_model), "w_router")
+        bias_at = _ptr(bias, torch.float32, (n_experts,), "bias")
+        self._device = torch.cuda.current_device()
+        _on(self._device, "the current device", w_router, bias)
         h = ctypes.c_void_p()
-        _check(lib().moe_router_init(
-            ctypes.byref(desc), _ptr(w_router, dtype, (n_experts, d_model), "w_router"),
-            _ptr(bias, torch.float32, (n_experts,), "bias"), ctypes.byref(h)))
+        _check(lib().moe_router_init(ctypes.byref(desc), gate, bias_at, ctypes.byref(h)))
         self._keep = (w_router, bias)
         self._h = h
 
@@ -322,7 +334,8 @@ class MoeRouter:
         """x [T, d]; topk_idx int32, topk_w fp32 [T, K]; logits fp32 [T, E] or
         None; expert_count int32 [E] or None."""
         torch = _th()
-        T, _ = _rows(x, self.dtype, "x")
+        T, _ = _rows(x, "x")
+        _on(self._device, "the router's device", x, topk_idx, topk_w, logits, expert_count)
         _check(lib().moe_route(
             self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
             _addr(topk_idx, torch.int32, (T, self.K), "topk_idx"),
@@ -335,7 +348,8 @@ class MoeRouter:
         """From d_topk_w fp32 [T, K] (and d_logits fp32 [T, E] or None) to d_x
         [T, d] of x's type and d_w_router fp32 [E, d] (each or None)."""
         torch = _th()
-        T, _ = _rows(x, self.dtype, "x")
+        T, _ = _rows(x, "x")
+        _on(self._device, "the router's device", x, logits, topk_idx, d_topk_w, d_x, d_w_router, d_logits)
         _check(lib().moe_route_backward(
             self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
             _addr(logits, torch.float32, (T, self.E), "logits"),

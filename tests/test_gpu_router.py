@@ -119,6 +119,15 @@ CASES = [
     (1100, 256, 8, F16, 0, R.Rule(2)),
     (2100, 128, 40, F16, 0.002, R.Rule(4, renormalize=False)),
     (3000, 512, 256, F16, 0.0008, R.Rule(8, renormalize=False)),
+    # every kind of selection kernel at every number of experts per lane, and
+    # groups whose number or size is no power of two
+    (256, 128, 40, F16, 0.02, R.Rule(5, score=G, n_groups=5, top_groups=2, group_best=2)),
+    (700, 64, 96, F16, 0, R.Rule(6, n_groups=12, top_groups=5, group_best=2)),
+    (2300, 128, 100, BF16, 0.02, R.Rule(7, score=G, n_groups=20, top_groups=6, group_best=2)),
+    (2500, 64, 512, F16, 0.02, R.Rule(16, score=G, n_groups=32, top_groups=9, group_best=2)),
+    (5000, 64, 13, F16, 0, R.Rule(13, renormalize=False)),
+    (5001, 128, 16, BF16, 0.02, R.Rule(16, score=G, n_groups=16, top_groups=16)),
+    (4100, 256, 60, F16, 0.02, R.Rule(4, score=G, n_groups=3, top_groups=1)),
 ]
 
 
@@ -163,6 +172,40 @@ def test_near_ties_go_by_the_exact_sums():
         # (scores that saturate tie, so the logits are kept small)
         xs = x if bias is None else x / 256
         check(rule, xs.half().cuda(), wg.cuda(), None if bias is None else bias.cuda())
+
+
+@pytest.mark.parametrize("dtype,x_scale,w_scale", [
+    (F16, 2.0 ** -24, 1.0), (F16, 2.0 ** -24, 2.0 ** -20), (BF16, 1e-25, 1.0), (BF16, 1e15, 1e12),
+    (F16, 1024.0, 64.0)], ids=["f16_subnormal", "f16_both_subnormal", "bf16_tiny", "bf16_huge", "f16_large"])
+@pytest.mark.parametrize("E", [12, 40])
+def test_near_ties_at_the_ends_of_the_range(dtype, x_scale, w_scale, E):
+    """Products and squares near the ends of the types: the bound of the sums'
+    errors holds there too.  Integers times powers of two and a gate whose rows
+    differ in one place, so that many sums are near or equal."""
+    g = torch.Generator().manual_seed(13)
+    d, T = 192, 40
+    x = torch.randint(-7, 8, (T, d), generator=g).float() * x_scale
+    wg = torch.randint(-3, 4, (d,), generator=g).float().repeat(E, 1)
+    wg[torch.arange(E), torch.randint(0, d, (E,), generator=g)] += 1
+    wg *= w_scale
+    x, wg = x.to(dtype).cuda(), wg.to(dtype).cuda()
+    check(R.Rule(4), x, wg, None)
+    if x_scale < 1:
+        b = (torch.randn(E, generator=g) * 0.1).cuda()
+        check(R.Rule(4, score=G), x, wg, b)
+        check(R.Rule(4, renormalize=False), x, wg, b)
+
+
+def test_rows_of_zeros_in_a_long_call():
+    """A padded batch: tokens of zeros tie everywhere, by index."""
+    T, d, E = 2600, 128, 96
+    x, wg, _, _ = inputs(T, d, E, F16, 3, 0)
+    x[1000:2200] = 0
+    for bias in (None, torch.zeros(E, device="cuda")):
+        idx, _, _ = check(R.Rule(6, score=G, n_groups=8, top_groups=4, group_best=2), x, wg, bias)
+        assert (idx[1000:2200].cpu() == torch.arange(6)).all()
+    wg.zero_()   # and a gate that has not learnt anything yet
+    check(R.Rule(6, score=G), x, wg, torch.zeros(E, device="cuda"))
 
 
 def test_masked_experts_and_rows_without_any():
@@ -392,6 +435,27 @@ def test_refusals():
     r.destroy()
     with pytest.raises(P.MoeError):
         r.route(x, idx, w)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    import paper_2411_01433_amd as P
+    x, wg, _, _ = inputs(4, 128, 6, F16, 1, 0)
+    r = make(R.Rule(2), wg, None, 4, backward=True)
+    idx, w, lg, _ = outs(3, 2, 6)
+    h = torch.zeros((4, 128), device="cuda")
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        with pytest.raises(ValueError, match="current device"):
+            P.layernorm(h, x)
+        with pytest.raises(ValueError, match="current device"):
+            P.layernorm_backward(x, h, h)
+    r._device = 1
+    with pytest.raises(ValueError, match="router's device"):
+        r.route(x, idx, w)
+    with pytest.raises(ValueError, match="router's device"):
+        r.backward(x, lg, idx, w, x)
+    r._device = 0
+    r.destroy()
 
 
 def test_two_handles_on_two_streams():
