@@ -218,8 +218,9 @@ enum { MOE_F16 = 0, MOE_BF16 = 1 };
  *  h     device fp32 [n_tokens, d_model] (the residual stream)
  *  gain  device fp32 [d_model] or NULL (1);  bias  likewise or NULL (0)
  *  x     device, `type` [n_tokens, d_model] (output, overwritten)
- *  n_tokens >= 1; d_model a positive multiple of 64, <= 16384; eps >= 0.
- * Needs no handle; pointers 16-byte aligned; works on the current device. */
+ *  n_tokens 1..2097152; d_model a positive multiple of 64, <= 16384; eps >= 0.
+ * Needs no handle; pointers 16-byte aligned; works on the current device.
+ * Outputs overlap no input, here and in the entry points below. */
 moe_status moe_layernorm(const float* h, const float* gain, const float* bias, void* x,
                          int32_t type, int32_t n_tokens, int32_t d_model, float eps,
                          void* stream);
@@ -259,10 +260,11 @@ moe_status moe_layernorm_backward(const void* d_x, int32_t type, const float* h,
  *          largest; exact ties of keys or groups go to the lower index
  *   weight scale * s_e, with renormalize divided by the sum of the selected s
  * An expert whose logit or bias is not finite (a masked expert: bias -inf)
- * is never selected, and one whose logit is not finite has score 0.  If
- * fewer than top_k experts are left, the last slots hold index -1 and weight
- * 0.  Selection goes by the logits' sums in 64 bits, so it does not depend
- * on how many tokens a call has or how its sums are split. */
+ * is never selected, and one whose logit is not finite has score 0 (a logit
+ * is finite where its sum in fp32 is).  If fewer than top_k experts are left,
+ * the last slots hold index -1 and weight 0.  Selection goes by the logits'
+ * sums in 64 bits, so it does not depend on how many tokens a call has or how
+ * its sums are split. */
 typedef struct moe_router* moe_router_t;
 
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
@@ -345,8 +347,10 @@ moe_status moe_router_destroy(moe_router_t router);
  * expert is reported as index -1 and MOE_PREC_SKIP.
  *  - The router must be of type MOE_F16, with the layer's d_model, n_experts
  *    and top_k, at least its max_tokens, and on its device (else MOE_EINVAL).
- *  - It must outlive its use by the layer; one router may serve several
- *    layers whose calls do not overlap (its workspace is one).
+ *  - It must outlive its use by the layer, and by graphs that captured calls
+ *    of the layer with it; one router may serve several layers whose calls
+ *    do not overlap (its workspace is one).
+ *  - moe_predict keeps to the gates that its predictor was created with.
  *  - Not while a call of the layer is being enqueued by another thread. */
 moe_status moe_layer_set_router(moe_layer_t layer, moe_router_t router);
 

@@ -249,25 +249,51 @@ def _rows(t, name):
     return t.shape
 
 
-def _on(device, where, *tensors):
-    """Refuse device tensors of another device (a kernel would read them through
-    addresses that mean something else on its own)."""
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != device:
-            raise ValueError(f"tensors must be on {where} ({device}), got {t.get_device()}")
+def _addr_on(device, t, dtype, shape, name):
+    """_addr of a tensor on `device`: on another one its address would mean
+    something else to the kernel."""
+    if t is None:
+        return None
+    if (isinstance(t, _th().Tensor) and t.get_device() == device and t.is_cuda
+            and t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+        return t.data_ptr()
+    at = _ptr(t, dtype, shape, name).value
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on device {device}, got {t.get_device()}")
+    return at
+
+
+def _stream_on(device, stream):
+    """_stream, for None the current one of `device`."""
+    if stream is None:
+        raw = getattr(_th()._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(device)
+        stream = _th().cuda.current_stream(device)
+    return _stream(stream)
+
+
+def _current_device(t, name):
+    """The current device, where t has to be."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    device = t.get_device()
+    if device != _th().cuda.current_device():
+        raise ValueError(f"{name} must be on the current device")
+    return device
 
 
 def layernorm(h, x, gain=None, bias=None, eps: float = 1e-5, stream=None):
     """x = layer norm of h, row by row: h fp32 [T, d], x fp16 or bf16 [T, d],
-    gain / bias fp32 [d] or None."""
-    torch = _th()
-    T, d = _rows(h, "h")
+    gain / bias fp32 [d] or None, all on the current device."""
+    f32 = _th().float32
+    rows = T, d = _rows(h, "h")
     _rows(x, "x")
-    _on(torch.cuda.current_device() if h.is_cuda else -1, "the current device", h, x, gain, bias)
+    at, kind = _current_device(h, "h"), x.dtype
     _check(lib().moe_layernorm(
-        _addr(h, torch.float32, (T, d), "h"), _addr(gain, torch.float32, (d,), "gain"),
-        _addr(bias, torch.float32, (d,), "bias"), _addr(x, x.dtype, (T, d), "x"),
-        _type16(x.dtype, "x"), T, d, eps, _stream(stream)))
+        _addr_on(at, h, f32, rows, "h"), _addr_on(at, gain, f32, (d,), "gain"),
+        _addr_on(at, bias, f32, (d,), "bias"), _addr_on(at, x, kind, rows, "x"),
+        _type16(kind, "x"), T, d, eps, _stream_on(at, stream)))
 
 
 def layernorm_workspace(n_tokens: int, d_model: int) -> int:
@@ -280,35 +306,38 @@ def layernorm_workspace(n_tokens: int, d_model: int) -> int:
 def layernorm_backward(d_x, h, d_h, gain=None, d_gain=None, d_bias=None, eps: float = 1e-5,
                        accumulate: bool = False, workspace=None, stream=None):
     """Gradients of layernorm from d_x (fp16 or bf16 [T, d]): d_h fp32 [T, d]
-    (with accumulate added to), d_gain / d_bias fp32 [d] or None.  workspace:
-    uint8 of layernorm_workspace(T, d) bytes; without one it is allocated on
-    the current stream, which `stream` then has to be (None)."""
+    (with accumulate added to), d_gain / d_bias fp32 [d] or None, all on the
+    current device.  workspace: uint8 of layernorm_workspace(T, d) bytes;
+    without one it is allocated on the current stream, which `stream` then has
+    to be (None)."""
     torch = _th()
-    T, d = _rows(h, "h")
+    f32 = torch.float32
+    rows = T, d = _rows(h, "h")
     _rows(d_x, "d_x")
-    _on(torch.cuda.current_device() if h.is_cuda else -1, "the current device", h, d_x, d_h, gain,
-        d_gain, d_bias, workspace)
-    if workspace is None and (d_gain is not None or d_bias is not None):
-        if stream is not None:
-            raise ValueError("a call on a stream of its own needs a workspace")
+    alone = workspace is None and (d_gain is not None or d_bias is not None)
+    if alone and stream is not None:
+        raise ValueError("a call on a stream of its own needs a workspace")
+    at, kind = _current_device(h, "h"), d_x.dtype
+    if alone:
         workspace = torch.empty(layernorm_workspace(T, d), dtype=torch.uint8, device=h.device)
     ws = None
     if workspace is not None:
         if workspace.numel() < layernorm_workspace(T, d):
             raise ValueError(f"workspace must hold {layernorm_workspace(T, d)} bytes")
-        ws = _addr(workspace, torch.uint8, workspace.shape, "workspace")
+        ws = _addr_on(at, workspace, torch.uint8, workspace.shape, "workspace")
     _check(lib().moe_layernorm_backward(
-        _addr(d_x, d_x.dtype, (T, d), "d_x"), _type16(d_x.dtype, "d_x"),
-        _addr(h, torch.float32, (T, d), "h"), _addr(gain, torch.float32, (d,), "gain"), eps, T, d,
-        _addr(d_h, torch.float32, (T, d), "d_h"), 1 if accumulate else 0,
-        _addr(d_gain, torch.float32, (d,), "d_gain"), _addr(d_bias, torch.float32, (d,), "d_bias"),
-        ws, _stream(stream)))
+        _addr_on(at, d_x, kind, rows, "d_x"), _type16(kind, "d_x"),
+        _addr_on(at, h, f32, rows, "h"), _addr_on(at, gain, f32, (d,), "gain"), eps, T, d,
+        _addr_on(at, d_h, f32, rows, "d_h"), 1 if accumulate else 0,
+        _addr_on(at, d_gain, f32, (d,), "d_gain"), _addr_on(at, d_bias, f32, (d,), "d_bias"),
+        ws, _stream_on(at, stream)))
 
 
 class MoeRouter:
     """A routing rule over a borrowed gate w_router [E, d] (fp16 or bf16) and an
     optional borrowed balance bias fp32 [E]; see moe_router_init.  Both may be
-    updated in place between calls.  backward: the handle can run backward()."""
+    updated in place between calls.  backward: the handle can run backward().
+    Lives on the device that is current when it is made."""
 
     def __init__(self, d_model, n_experts, top_k, max_tokens, w_router, bias=None, dtype=None,
                  score=SCORE_SOFTMAX, n_groups=1, top_groups=1, group_best=1, renormalize=True,
@@ -321,12 +350,12 @@ class MoeRouter:
         desc = RouterDesc(d_model, n_experts, top_k, max_tokens, _type16(dtype, "dtype"), score,
                           n_groups, top_groups, group_best, 1 if renormalize else 0, scale,
                           MOE_ROUTER_BACKWARD if backward else 0)
-        gate = _ptr(w_router, dtype, (n_experts, d_model), "w_router")
-        bias_at = _ptr(bias, torch.float32, (n_experts,), "bias")
-        self._device = torch.cuda.current_device()
-        _on(self._device, "the current device", w_router, bias)
+        _rows(w_router, "w_router")
+        at = self._device = _current_device(w_router, "w_router")
         h = ctypes.c_void_p()
-        _check(lib().moe_router_init(ctypes.byref(desc), gate, bias_at, ctypes.byref(h)))
+        _check(lib().moe_router_init(
+            ctypes.byref(desc), _addr_on(at, w_router, dtype, (n_experts, d_model), "w_router"),
+            _addr_on(at, bias, torch.float32, (n_experts,), "bias"), ctypes.byref(h)))
         self._keep = (w_router, bias)
         self._h = h
 
@@ -335,13 +364,13 @@ class MoeRouter:
         None; expert_count int32 [E] or None."""
         torch = _th()
         T, _ = _rows(x, "x")
-        _on(self._device, "the router's device", x, topk_idx, topk_w, logits, expert_count)
+        at, K, E = self._device, self.K, self.E
         _check(lib().moe_route(
-            self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
-            _addr(topk_idx, torch.int32, (T, self.K), "topk_idx"),
-            _addr(topk_w, torch.float32, (T, self.K), "topk_w"),
-            _addr(logits, torch.float32, (T, self.E), "logits"),
-            _addr(expert_count, torch.int32, (self.E,), "expert_count"), _stream(stream)))
+            self._h, T, _addr_on(at, x, self.dtype, (T, self.d), "x"),
+            _addr_on(at, topk_idx, torch.int32, (T, K), "topk_idx"),
+            _addr_on(at, topk_w, torch.float32, (T, K), "topk_w"),
+            _addr_on(at, logits, torch.float32, (T, E), "logits"),
+            _addr_on(at, expert_count, torch.int32, (E,), "expert_count"), _stream_on(at, stream)))
 
     def backward(self, x, logits, topk_idx, d_topk_w, d_x=None, d_w_router=None, d_logits=None,
                  stream=None):
@@ -349,15 +378,15 @@ class MoeRouter:
         [T, d] of x's type and d_w_router fp32 [E, d] (each or None)."""
         torch = _th()
         T, _ = _rows(x, "x")
-        _on(self._device, "the router's device", x, logits, topk_idx, d_topk_w, d_x, d_w_router, d_logits)
+        at, K, E, f32 = self._device, self.K, self.E, torch.float32
         _check(lib().moe_route_backward(
-            self._h, T, _addr(x, self.dtype, (T, self.d), "x"),
-            _addr(logits, torch.float32, (T, self.E), "logits"),
-            _addr(topk_idx, torch.int32, (T, self.K), "topk_idx"),
-            _addr(d_topk_w, torch.float32, (T, self.K), "d_topk_w"),
-            _addr(d_logits, torch.float32, (T, self.E), "d_logits"),
-            _addr(d_x, self.dtype, (T, self.d), "d_x"),
-            _addr(d_w_router, torch.float32, (self.E, self.d), "d_w_router"), _stream(stream)))
+            self._h, T, _addr_on(at, x, self.dtype, (T, self.d), "x"),
+            _addr_on(at, logits, f32, (T, E), "logits"),
+            _addr_on(at, topk_idx, torch.int32, (T, K), "topk_idx"),
+            _addr_on(at, d_topk_w, f32, (T, K), "d_topk_w"),
+            _addr_on(at, d_logits, f32, (T, E), "d_logits"),
+            _addr_on(at, d_x, self.dtype, (T, self.d), "d_x"),
+            _addr_on(at, d_w_router, f32, (E, self.d), "d_w_router"), _stream_on(at, stream)))
 
     def destroy(self):
         if self._h is not None and self._h.value:
@@ -497,6 +526,8 @@ class MoeLayer:
     def set_router(self, router):
         """Route this layer's steps by `router` (a MoeRouter, kept alive by the
         layer), or by its own gate again (None)."""
+        if router is not None and router._h is None:
+            raise ValueError("the router was destroyed")
         _check(lib().moe_layer_set_router(self._h, None if router is None else router._h))
         self._router = router
 

@@ -84,7 +84,9 @@ moe_status check_desc(const moe_router_desc* d) {
 
 moe_status check_norm(int32_t type, int32_t n_tokens, int32_t d_model, float eps) {
   if (type != MOE_F16 && type != MOE_BF16) return rfail(MOE_EINVAL, "unknown type %d", type);
-  if (n_tokens < 1) return rfail(MOE_EINVAL, "n_tokens must be >= 1 (got %d)", n_tokens);
+  // (a launch has less than 2^32 threads, and a row up to 1024)
+  if (n_tokens < 1 || n_tokens > 1 << 21)
+    return rfail(MOE_EINVAL, "n_tokens must be in [1, 2097152] (got %d)", n_tokens);
   if (d_model <= 0 || d_model % 64 || d_model > 16384)
     return rfail(MOE_EINVAL, "d_model must be a positive multiple of 64, <= 16384 (got %d)", d_model);
   if (!(eps >= 0.0f)) return rfail(MOE_EINVAL, "eps must be >= 0");
@@ -169,9 +171,13 @@ moe_status moe_router_init(const moe_router_desc* desc, const void* w_router, co
   p.w_norm = reinterpret_cast<float*>(base + o_wn);
   p.open = reinterpret_cast<int32_t*>(base + o_open);
   p.grad_ws = r->backward ? base + o_grad : nullptr;
-  {
+  try {
     std::lock_guard<std::mutex> g(g_router_mu);
     g_router_live.insert(r);
+  } catch (...) {
+    (void)hipFree(r->arena);
+    delete r;
+    return rfail(MOE_ENOMEM, "host allocation failed");
   }
   *out = r;
   return MOE_OK;

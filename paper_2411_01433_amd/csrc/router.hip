@@ -14,8 +14,8 @@
 // also gives the norms of the rows of x and Wg, whose product bounds the
 // error of a logit, and the selection knows how near two keys may be to be in
 // order for certain.  Where two keys (or groups) that decide something are
-// nearer - for a few tokens in a hundred - a block per token sums the logits
-// in question again in 64 bits and decides by those.
+// nearer - for a few tokens in a hundred - the logits in question are summed
+// again in 64 bits, and those decide.
 #include "moe_internal.h"
 
 namespace moe {
@@ -86,13 +86,16 @@ __device__ inline float error_norm(float q2, uint32_t bits) {
 }
 constexpr float kSumError = 0x1p-24f;
 __device__ inline float logit_error(float qx, float qw) {
-  // (rounding to fp32 of the smallest numbers adds to a bound)
-  return qx > 0.0f && qw > 0.0f ? fminf(kSumError * qx * qw + 1e-33f, 1e30f) : 0.0f;
+  // (rounding to fp32 of the smallest numbers adds to a bound; sums that stay
+  // finite are off by less than the upper one, half a step of the largest
+  // number in each of at most 512 steps and their joins)
+  return qx > 0.0f && qw > 0.0f ? fminf(kSumError * qx * qw + 1e-33f, 1e35f) : 0.0f;
 }
 
 // ---- selection ------------------------------------------------------------
 
-__device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+constexpr float kLargest = 3.402823466e38f;
+__device__ inline bool finite(float v) { return fabsf(v) <= kLargest; }
 
 // Sum and maximum of doubles over a wave in registers (see wave_sum_dpp).
 template <int CTRL>
@@ -217,7 +220,10 @@ __device__ inline GroupBest<F> group_best(const RouterParams& p, const F* row, i
   if (per > 16) join(__shfl_xor(best, 16, 64), __shfl_xor(second, 16, 64));
   if (per > 32) join(__shfl_xor(best, 32, 64), __shfl_xor(second, 32, 64));
   const bool two = p.group_best == 2 && second > none;
-  return {two ? best + second : best, two ? second : best};
+  F sum = two ? best + second : best;
+  // two of the type's lowest are not the infinity of a group without any
+  if constexpr (sizeof(F) == 4) sum = two ? fminf(fmaxf(sum, -kLargest), kLargest) : sum;
+  return {sum, two ? second : best};
 }
 
 // One token's fp32 selection, by one wave: lane i has the experts i, i + 64,
@@ -258,6 +264,13 @@ __device__ inline float group_margin(const Token<C>& tk) {
   return tk.group_err + 5e-7f * fmaxf(fabsf(tk.in), fabsf(tk.out));
 }
 
+// Whether this lane's group may be on the other side within `room`.
+template <int C>
+__device__ inline bool contested(const RouterParams& p, const Token<C>& tk, float room) {
+  return (int)(threadIdx.x & 63) / lanes_per_group(p) < p.n_groups && tk.group.sum > -__builtin_inff() &&
+         (tk.stays ? tk.group.sum - tk.out <= room : tk.in - tk.group.sum <= room);
+}
+
 // The experts of the groups that stay.
 template <int C>
 __device__ inline void keep_groups(const RouterParams& p, Token<C>& tk) {
@@ -283,19 +296,16 @@ struct Team {
 // LDS of a team that works on a token whose selection is open.
 template <int C>
 struct OpenLds {
-  double row[C * 64];    // keys or scores for the groups' scan
+  double row[C * 64];    // logits, then keys or scores for the groups' scan
   double dots[C * 64];   // logits summed again
   int32_t list[C * 64];  // ... and their experts
-  double sum[kRouterMaxGroups], low[kRouterMaxGroups];
-  float err[kRouterMaxGroups], more[2][kRouterMaxGroups];
 };
 
 // Sums the logits of the experts of `want` again, in 64 bits, the team's
-// waves in turn; take(c, lane, value) gets each.  Every wave has the same
+// waves in turn: n of them, in lds.list and lds.dots.  Every wave has the same
 // `want` and calls this.
-template <class T16, int C, int TW, class Take>
-__device__ inline void sum_again(const RouterParams& p, const T16* xr, const bool (&want)[C],
-                                 OpenLds<C>& lds, Take take) {
+template <class T16, int C, int TW>
+__device__ inline int sum_again(const RouterParams& p, const T16* xr, const bool (&want)[C], OpenLds<C>& lds) {
   const int lane = threadIdx.x & 63;
   int n = 0;
 #pragma unroll
@@ -321,194 +331,87 @@ __device__ inline void sum_again(const RouterParams& p, const T16* xr, const boo
     }
   }
   Team<TW>::sync();
-  for (int i = 0; i < n; ++i) {
-    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
-    take(e >> 6, e & 63, lds.dots[i]);
-  }
-  Team<TW>::sync();
+  return n;
 }
 
-// The selection by 64-bit sums, whatever is open: experts whose order or group
-// is not certain are summed again (bound 0) until nothing is open.
+// The whole selection in 64 bits: every logit that enters it is summed again.
 template <class T16, int C, int TW>
-__device__ void select_exact(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+__device__ void select_all(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
   const int lane = threadIdx.x & 63;
   const double none = -__builtin_inf();
   const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
-  double l[C];
-  float err[C];
   bool want[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    l[c] = tk.l[c];
-    err[c] = finite(tk.l[c]) ? tk.err[c] : 0.0f;
-    want[c] = false;
+    want[c] = finite(tk.l[c]) && (soft || tk.fit[c]) && tk.err[c] > 0.0f;
+    if (Team<TW>::lead()) lds.row[c * 64 + lane] = tk.l[c];
   }
-  const int per = lanes_per_group(p);
-  for (;;) {
-    sum_again<T16, C, TW>(p, xr, want, lds, [&](int c, int at, double v) {
+  const int n = sum_again<T16, C, TW>(p, xr, want, lds);
+  if (Team<TW>::lead())
+    for (int i = lane; i < n; i += 64) lds.row[lds.list[i]] = lds.dots[i];
+  Team<TW>::sync();
+  double key[C], top = none, z = 0.0;
 #pragma unroll
-      for (int i = 0; i < C; ++i)
-        if (i == c && lane == at) {
-          l[i] = v;
-          err[i] = 0.0f;
-        }
-    });
-    double key[C], sc[C], kerr[C];
-    bool fit[C];
-    double zrel = 0.0;
-    if (soft) {
-      double top = none, z = 0.0;
+  for (int c = 0; c < C; ++c) {
+    key[c] = lds.row[c * 64 + lane];
+    if (finite(tk.l[c])) top = fmax(top, key[c]);
+  }
+  if (soft) {
+    top = wave_max(top);
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (finite(tk.l[c])) top = fmax(top, l[c]);
-      top = wave_max(top);
+    for (int c = 0; c < C; ++c) z += finite(tk.l[c]) ? exp(key[c] - top) : 0.0;
+    z = wave_sum(z);
+  }
+  Team<TW>::sync();
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        sc[c] = finite(tk.l[c]) ? exp(l[c] - top) : 0.0;
-        z += sc[c];
-      }
-      z = wave_sum(z);
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        sc[c] = finite(tk.l[c]) ? sc[c] / z : 0.0;
-        zrel += sc[c] * err[c];
-      }
-      zrel = biased ? 1.01 * wave_sum(zrel) : 0.0;  // (without a bias the sum is common to all)
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c) sc[c] = finite(tk.l[c]) ? 1.0 / (1.0 + exp(-l[c])) : 0.0;
+  for (int c = 0; c < C; ++c) {
+    tk.l[c] = finite(tk.l[c]) ? (float)key[c] : tk.l[c];
+    const double sc = !tk.fit[c] ? 0.0 : soft ? exp(key[c] - top) / z : 1.0 / (1.0 + exp(-key[c]));
+    if (biased) key[c] = sc + tk.b[c];
+    if (Team<TW>::lead()) lds.row[c * 64 + lane] = !tk.fit[c] ? none : biased ? key[c] : sc;
+    tk.kept[c] = tk.fit[c];
+  }
+  Team<TW>::sync();
+  if (p.n_groups > 1) {
+    const int per = lanes_per_group(p), g = lane / per;
+    const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
+    int rank = 0;
+#pragma unroll 1
+    for (int h = 0; h < p.n_groups; ++h) {
+      const double v = lane_value(gb.sum, h * per);
+      rank += v > gb.sum || (v == gb.sum && h < g);
     }
+    tk.stays = g < p.n_groups && rank < p.top_groups;
+    keep_groups(p, tk);
+  }
+  tk.sel = -1;
+  for (int k = 0; k < p.K; ++k) {
+    double best = none;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (tk.kept[c]) best = fmax(best, key[c]);
+    best = wave_max(best);
+    int e = -1;
+    float l = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      fit[c] = tk.fit[c];
-      want[c] = false;
-      // slope of a score by its logit: s of the softmax's term, 1/4 at most of a sigmoid
-      const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
-      key[c] = biased ? sc[c] + tk.b[c] : l[c];
-      kerr[c] = biased ? serr : err[c];
-    }
-    bool open = false;
-    if (p.n_groups > 1) {
-      const int size = p.E / p.n_groups;
-      if (Team<TW>::lead()) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) lds.row[c * 64 + lane] = fit[c] ? (biased ? key[c] : sc[c]) : none;
-        lds.more[0][lane] = lds.more[1][lane] = 0.0f;
-      }
-      Team<TW>::sync();
-      const int g = lane / per;
-      const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
-      if (Team<TW>::lead() && (lane & (per - 1)) == 0) {
-        lds.sum[g] = gb.sum;
-        lds.low[g] = gb.low;
-      }
-      // A group's error: that of its most uncertain member, once or twice,
-      // among those that may be one of its best - that reach, with their own
-      // bound, down to the least that counts less the bounds of what counts.
-#pragma unroll
-      for (int round = 0; round < 2; ++round) {
-        Team<TW>::sync();
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int e = c * 64 + lane;
-          if (!fit[c]) continue;
-          const double serr = soft ? 1.01 * sc[c] * err[c] : 0.25 * err[c];
-          const double reach = round == 0 ? lds.row[e] : lds.row[e] + serr + lds.err[e / size];
-          const bool in = reach >= lds.low[e / size];
-          if (round == 1) want[c] = in && err[c] > 0.0f;
-          if (in && serr > 0.0 && Team<TW>::lead())
-            atomicMax(reinterpret_cast<unsigned*>(&lds.more[round][e / size]),
-                      __float_as_uint((float)(serr * 1.0001)));
-        }
-        Team<TW>::sync();
-        if (Team<TW>::lead()) lds.err[lane] = lds.more[round][lane];
-      }
-      Team<TW>::sync();
-      const bool is = lane < p.n_groups;
-      const double mine = is ? lds.sum[lane] : none;
-      int rank = 0;
-      for (int h = 0; h < p.n_groups; ++h) rank += lds.sum[h] > mine || (lds.sum[h] == mine && h < lane);
-      const uint64_t kept = __ballot(is && rank < p.top_groups);
-      bool unsure = false;
-      if (is && mine > none)
-        for (int h = 0; h < p.n_groups; ++h) {
-          const double v = lds.sum[h];
-          if (v > none && (kept >> lane & 1) != (kept >> h & 1))
-            unsure |= fabs(v - mine) <= p.group_best * ((double)lds.err[lane] + lds.err[h]) +
-                                            zrel * fmax(fabs(v), fabs(mine));
-        }
-      const uint64_t um = __ballot(unsure && (lds.err[lane] > 0.0f || zrel > 0.0));
-      open = um != 0;
-#pragma unroll
-      for (int c = 0; c < C; ++c) want[c] = want[c] && (um >> ((c * 64 + lane) / size) & 1);
-#pragma unroll
-      for (int c = 0; c < C; ++c) fit[c] = fit[c] && (kept >> ((c * 64 + lane) / size) & 1);
-      Team<TW>::sync();
-    }
-    if (!open) {
-      tk.sel = -1;
-      for (int k = 0; k < p.K; ++k) {
-        double bk = none;
-        bool any = false;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (fit[c]) {
-            bk = any ? fmax(bk, key[c]) : key[c];
-            any = true;
-          }
-        bk = wave_max(bk);
-        int be = -1;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const uint64_t m = __ballot(fit[c] && key[c] == bk);
-          if (be < 0 && m) be = c * 64 + __ffsll((unsigned long long)m) - 1;
-        }
-        be = __builtin_amdgcn_readfirstlane(be);
-        if (be < 0) break;  // nobody left
-        double ml = 0.0, ms = 0.0, me = 0.0;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (c * 64 + lane == be) {
-            fit[c] = false;
-            ml = l[c];
-            ms = sc[c];
-            me = kerr[c];
-          }
-        ml = lane_value(ml, be & 63);
-        ms = lane_value(ms, be & 63);
-        me = lane_value(me, be & 63);
-        if (lane == k) {
-          tk.sel = be;
-          tk.sl = (float)ml;
-        }
-        bool near = false;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const double room = me + kerr[c] + zrel * fabs(ms - sc[c]);
-          if (fit[c] && room > 0.0 && bk - key[c] <= room) {
-            near = true;
-            want[c] = want[c] || err[c] > 0.0f;
-          }
-        }
-        if (__ballot(near)) {
-          open = true;
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (c * 64 + lane == be) want[c] = want[c] || err[c] > 0.0f;
-        }
+      const uint64_t m = __ballot(tk.kept[c] && key[c] == best);
+      if (e < 0 && m) {
+        const int at = __ffsll((unsigned long long)m) - 1;
+        e = c * 64 + at;
+        l = lane_value(tk.l[c], at);
       }
     }
-    if (!open) return;
-    bool some = false;
+    e = __builtin_amdgcn_readfirstlane(e);
+    if (e < 0) break;  // nobody left
 #pragma unroll
-    for (int c = 0; c < C; ++c) some |= want[c];
-    if (!__ballot(some)) {
-      // only the softmax's denominator is uncertain: every logit that it adds
-#pragma unroll
-      for (int c = 0; c < C; ++c) want[c] = err[c] > 0.0f;
+    for (int c = 0; c < C; ++c) tk.kept[c] = tk.kept[c] && c * 64 + lane != e;
+    if (lane == k) {
+      tk.sel = e;
+      tk.sl = l;
     }
   }
+  Team<TW>::sync();
 }
 
 // Descending order of a lane's C keys, each with its number c.
@@ -581,7 +484,8 @@ __device__ inline void score_token(const RouterParams& p, float* row, Token<C>& 
     }
     tk.z = wave_sum_dpp(tk.z);
   }
-  float verr = 0.0f;  // largest error of what groups count
+  float verr[C];      // errors of what groups count
+  float most = 0.0f;
   worst = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -600,13 +504,14 @@ __device__ inline void score_token(const RouterParams& p, float* row, Token<C>& 
       tk.key[c] = sc[c] + tk.b[c];
       e1 += 1e-7f * fabsf(tk.key[c]);
     }
-    verr = fmaxf(verr, tk.fit[c] ? e1 : 0.0f);
+    verr[c] = e1;
+    most = fmaxf(most, tk.fit[c] ? e1 : 0.0f);
     tk.kerr[c] = biased ? e1 : tk.err[c];
     worst = fmaxf(worst, tk.fit[c] ? tk.kerr[c] : 0.0f);
     tk.kept[c] = tk.fit[c];
   }
   tk.margin = 2.0f * wave_max(worst);
-  tk.group_err = p.group_best * wave_max(verr);
+  tk.group_err = p.group_best * wave_max(most);
   tk.groups_open = false;
   if (p.n_groups > 1) {
     const int per = lanes_per_group(p);
@@ -630,6 +535,22 @@ __device__ inline void score_token(const RouterParams& p, float* row, Token<C>& 
     tk.in = -wave_max(tk.stays ? -tk.group.sum : none);
     tk.out = wave_max(is && !tk.stays ? tk.group.sum : none);
     tk.groups_open = tk.out > none && tk.in - tk.out <= 2.0f * group_margin(tk);
+    if (tk.groups_open) {
+      // again by the errors of those that may count in a group whose place is
+      // open: a bias that masks has the largest, and counts nowhere
+      const float room = 2.0f * group_margin(tk);
+      const uint64_t cm = __ballot(contested(p, tk, room));
+      most = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int at = min(group_of(p, c * 64 + lane) * per, 63);
+        const float low = __shfl(tk.group.low, at, 64);
+        const bool counts = tk.fit[c] && (cm >> at & 1) && tk.val[c] >= low - room;
+        most = fmaxf(most, counts ? verr[c] : 0.0f);
+      }
+      tk.group_err = p.group_best * wave_max(most);
+      tk.groups_open = tk.in - tk.out <= 2.0f * group_margin(tk);
+    }
     keep_groups(p, tk);
     wave_lds_fence();
   }
@@ -695,17 +616,18 @@ __device__ inline void take_slots(const RouterParams& p, float* row, Token<C>& t
 // The groups that stay where fp32 sums leave it open: those certainly in or
 // out keep their place (for each, all of the others or enough of them are
 // certainly on the other side of it), and the rest are ranked by the sums of
-// their members that may count, in 64 bits.
+// their members that may count, in 64 bits.  False where a softmax's
+// denominator beside biases, which stays that of the fp32 sums, is not known
+// well enough for it.
 template <class T16, int C, int TW>
-__device__ void settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
+__device__ bool settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk, OpenLds<C>& lds) {
   const int lane = threadIdx.x & 63;
   const int per = lanes_per_group(p), g = lane / per;
   const bool biased = p.bias != nullptr, soft = p.score == SCORE_SOFTMAX;
   const double none = -__builtin_inf();
   const float room = 2.0f * group_margin(tk);
-  const bool contested = g < p.n_groups && tk.group.sum > -__builtin_inff() &&
-                         (tk.stays ? tk.group.sum - tk.out <= room : tk.in - tk.group.sum <= room);
-  const uint64_t cm = __ballot(contested), sure = __ballot(tk.stays && !contested);
+  const bool near = contested(p, tk, room);
+  const uint64_t cm = __ballot(near), sure = __ballot(tk.stays && !near);
   const int left = p.top_groups - __popcll(sure) / per;
   bool want[C], again[C];
 #pragma unroll
@@ -718,30 +640,40 @@ __device__ void settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk
   double l[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) l[c] = tk.l[c];
-  sum_again<T16, C, TW>(p, xr, again, lds, [&](int c, int at, double v) {
+  const int n = sum_again<T16, C, TW>(p, xr, again, lds);
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    const double v = lds.dots[i];
 #pragma unroll
-    for (int i = 0; i < C; ++i)
-      if (i == c && lane == at) l[i] = v;
-  });
-  if (Team<TW>::lead()) {
+    for (int c = 0; c < C; ++c)
+      if (c * 64 + lane == e) l[c] = v;
+  }
+  float most = 0.0f;   // of the scores that may count
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      // (a softmax's denominator is common to all groups without a bias)
-      const double sc = soft ? exp(l[c] - tk.top) : 1.0 / (1.0 + exp(-l[c]));
-      lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
-    }
+  for (int c = 0; c < C; ++c) {
+    // (a softmax's denominator is common to all groups without a bias)
+    const double sc = soft ? exp(l[c] - tk.top) / tk.z : 1.0 / (1.0 + exp(-l[c]));
+    if (Team<TW>::lead()) lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
+    most = fmaxf(most, want[c] ? (float)sc : 0.0f);
   }
   Team<TW>::sync();
   const GroupBest<double> gb = group_best(p, lds.row, lane, per, g);
   int rank = 0;
+#pragma unroll 1
   for (int h = 0; h < p.n_groups; ++h) {
     if (!(cm >> (h * per) & 1)) continue;
     const double v = lane_value(gb.sum, h * per);
     rank += v > gb.sum || (v == gb.sum && h < g);
   }
-  tk.stays = (sure >> lane & 1) || (contested && rank < left);
+  tk.stays = (sure >> lane & 1) || (near && rank < left);
   keep_groups(p, tk);
   Team<TW>::sync();
+  if (!soft || !biased) return true;
+  // (scores of two groups differ by less than they come to)
+  const double in = -wave_max(near && tk.stays ? -gb.sum : none);
+  const double out = wave_max(near && !tk.stays ? gb.sum : none);
+  return in - out > 1.01 * tk.zrel * p.group_best * wave_max(most);
 }
 
 // The order of the slots where only neighbours of it are open: the experts
@@ -808,7 +740,13 @@ __device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk,
       add(c, j, lane_value(tk.l[c], j));
     }
   }
-  sum_again<T16, C, TW>(p, xr, again, lds, add);
+  const int summed = sum_again<T16, C, TW>(p, xr, again, lds);
+#pragma unroll 1
+  for (int i = 0; i < summed; ++i) {
+    const int e = __builtin_amdgcn_readfirstlane(lds.list[i]);
+    add(e >> 6, e & 63, lds.dots[i]);
+  }
+  Team<TW>::sync();
   double s = 0.0, k = ml;
   if (biased) {
     s = soft ? exp(ml - tk.top) / tk.z : 1.0 / (1.0 + exp(-ml));
@@ -817,6 +755,7 @@ __device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk,
   const bool in = lane < n;
   int rank = 0;
   bool unsure = false;
+#pragma unroll 1
   for (int u = 0; u < n; ++u) {
     const double ku = lane_value(k, u), su = lane_value(s, u);
     const int eu = __builtin_amdgcn_readlane(me, u);
@@ -899,14 +838,13 @@ template <class T16, int C, int TW>
 __device__ inline void select_token(const RouterParams& p, const T16* xr, float* row, Token<C>& tk,
                                     OpenLds<C>& lds) {
   score_token(p, row, tk);
-  // (scores that share an uncertain denominator beside biases that do not)
-  bool open = tk.groups_open && p.bias && p.score == SCORE_SOFTMAX;
+  bool open = false;
+  if (tk.groups_open) open = !settle_groups<T16, C, TW>(p, xr, tk, lds);
   if (!open) {
-    if (tk.groups_open) settle_groups<T16, C, TW>(p, xr, tk, lds);
     take_slots(p, row, tk);
     if (tk.slots_open) open = !select_slots<T16, C, TW>(p, xr, tk, lds);
   }
-  if (open) select_exact<T16, C, TW>(p, xr, tk, lds);
+  if (open) select_all<T16, C, TW>(p, xr, tk, lds);
 }
 
 // The block's counts into the call's, by neighbouring lanes: one request per
@@ -953,13 +891,13 @@ __global__ __launch_bounds__(kManyThreads) void router_select_many_kernel(Router
 }
 
 // Tokens of a call or of the list, a team of TW waves each.
-constexpr int kTeamThreads = 256;
+constexpr int team_threads(int tw) { return tw < 4 ? 256 : tw * 64; }
 template <class T16, int C, int TW>
-__global__ __launch_bounds__(kTeamThreads) void router_select_kernel(RouterParams p, int T, int listed,
+__global__ __launch_bounds__(team_threads(TW)) void router_select_kernel(RouterParams p, int T, int listed,
                                                                      const T16* __restrict__ x,
                                                                      const float* __restrict__ lg,
                                                                      RouterOut o) {
-  constexpr int kThreads = kTeamThreads, kTeams = kThreads / 64 / TW;
+  constexpr int kThreads = team_threads(TW), kTeams = kThreads / 64 / TW;
   __shared__ float rows[kThreads / 64][C * 64];
   __shared__ OpenLds<C> lds[kTeams];
   __shared__ int32_t counts[C * 64];
@@ -970,12 +908,13 @@ __global__ __launch_bounds__(kTeamThreads) void router_select_kernel(RouterParam
     for (int e = threadIdx.x; e < C * 64; e += kThreads) counts[e] = 0;
     __syncthreads();
   }
+#pragma unroll 1
   for (int i = blockIdx.x * kTeams + team; i < n; i += gridDim.x * kTeams) {
     const int t = listed ? __builtin_amdgcn_readfirstlane(global<int32_t>(p.open)[1 + i]) : i;
     Token<C> tk;
     load_token(p, global<float>(lg + (int64_t)t * p.E), global<float>(p.w_norm), global<float>(p.x_norm)[t], tk);
     select_token<T16, C, TW>(p, x + (int64_t)t * p.d, rows[wave], tk, lds[team]);
-    if (wave % TW == 0) finish(p, t, tk, o, counts);
+    if (TW == 1 || Team<TW>::lead()) finish(p, t, tk, o, counts);
   }
   add_counts(p, o, counts);
 }
@@ -1186,19 +1125,32 @@ hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, const R
 template <class T16, int C>
 hipError_t select(const RouterParams& p, int T, const T16* x, const float* lg, const RouterOut& o,
                   hipStream_t s) {
-  // Up to 256 tokens a block each; up to 2048 a wave each, which sums open
-  // ones by itself; more by the kernel that leaves them to another.
-  constexpr int kBlockEach = 256, kWaveEach = 2048, kListBlocks = 768;
-  if (T <= kBlockEach) {
-    router_select_kernel<T16, C, 4><<<T, kTeamThreads, 0, s>>>(p, T, 0, x, lg, o);
-  } else if (T <= kWaveEach) {
-    router_select_kernel<T16, C, 1><<<(T + 3) / 4, kTeamThreads, 0, s>>>(p, T, 0, x, lg, o);
+  // Up to 2048 tokens a wave each, which sums again what is open in its own;
+  // more by the kernel that leaves open tokens to a list, with a block of four
+  // waves each.  us at d 4096, 60 experts / 256 in 8 groups, a wave each
+  // against the list: 256 tokens 6.0 10.0 / 17.3 30.3, 1024 9.4 13.0 / 19.1
+  // 31.8, 2048 15.3 16.1 / 23.2 31.1, 4096 26.2 19.0 / 35.1 34.3, 8192 44.1
+  // 22.3 / 54.6 45.6 (the list with a wave each 49.2).
+  // A softmax beside a bias may need all of a token's logits in 64 bits, for
+  // its denominator (45 us of one block at 256 experts): a block of eight
+  // waves each, for all tokens or those on the list: 64 tokens 20.2 32.7, 256
+  // 52.5 65.9, 512 58.4 67.1, 1024 74.1 67.1, 2048 118 89.
+  const bool wide = p.bias && p.score == SCORE_SOFTMAX;
+  constexpr int kWideEach = 512, kWaveEach = 2048, kListBlocks = 768;
+  // (one expert per lane leaves those kernels with scratch memory that they
+  // never touch)
+  constexpr int W = C < 2 ? 2 : C;
+  if (wide && T <= kWideEach) {
+    router_select_kernel<T16, W, 8><<<T, team_threads(8), 0, s>>>(p, T, 0, x, lg, o);
+  } else if (!wide && T <= kWaveEach) {
+    router_select_kernel<T16, C, 1><<<(T + 3) / 4, team_threads(1), 0, s>>>(p, T, 0, x, lg, o);
   } else {
     const int blocks = (T + kManyWaves - 1) / kManyWaves;
     router_select_many_kernel<C><<<blocks < kManyBlocks ? blocks : kManyBlocks, kManyThreads, 0, s>>>(p, T, lg, o);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    router_select_kernel<T16, C, 4><<<kListBlocks, kTeamThreads, 0, s>>>(p, T, 1, x, lg, o);
+    if (wide) router_select_kernel<T16, W, 8><<<kListBlocks, team_threads(8), 0, s>>>(p, T, 1, x, lg, o);
+    else router_select_kernel<T16, W, 4><<<kListBlocks, team_threads(4), 0, s>>>(p, T, 1, x, lg, o);
   }
   return hipGetLastError();
 }

@@ -235,6 +235,46 @@ def test_masked_experts_and_rows_without_any():
         assert (idx == -1).all() and (w == 0).all()
 
 
+@pytest.mark.parametrize("T", [5, 300, 2100])
+@pytest.mark.parametrize("E,G,keep", [(16, 4, 2), (64, 8, 3), (300, 10, 4)])
+def test_masks_of_the_lowest_value(T, E, G, keep):
+    """A bias of fp32's lowest value is finite: such experts come after all
+    others, by index, and groups of them before groups of experts at -inf,
+    though two of them add up to no fp32 number.  And of its largest value."""
+    x, wg, _, g = inputs(T, 128, E, F16, 23, 0)
+    lowest, size = torch.finfo(torch.float32).min, E // G
+    b = torch.randn(E, generator=g) * 0.02
+    b[torch.randperm(E, generator=g)[:E // 3]] = lowest
+    for score in (R.SIGMOID, R.SOFTMAX):
+        check(R.Rule(4, score=score, n_groups=G, top_groups=keep, group_best=2), x, wg, b.cuda())
+        check(R.Rule(4, score=score), x, wg, b.cuda())
+    rule = R.Rule(min(size + 1, 16), score=R.SIGMOID, n_groups=G, top_groups=2, group_best=2)
+    only = torch.full((E,), -float("inf"))   # all groups masked, one by the lowest value
+    only[size * (G - 1):] = lowest
+    only[3] = 0.0
+    idx, _, _ = check(rule, x, wg, only.cuda())
+    assert (idx[:, 1].cpu() == size * (G - 1)).all()
+    top = torch.zeros(E)
+    top[2 * size:] = -lowest
+    check(rule, x, wg, top.cuda())
+
+
+@pytest.mark.parametrize("score", [R.SIGMOID, R.SOFTMAX])
+@pytest.mark.parametrize("T", [1, 300, 2100])
+def test_biases_that_cancel_the_scores(T, score):
+    """Keys that are all within fp32's rounding of zero, of scores that differ:
+    every comparison takes the sums, and a softmax's denominator, in 64 bits."""
+    d, E = 192, 40
+    for seed in range(8):
+        x, wg, _, _ = inputs(T, d, E, F16, 100 + seed, 0)
+        x[:] = x[0]
+        l = _np(x[:1]) @ _np(wg).T
+        b = torch.from_numpy(-R.scores(R.Rule(4, score=score), l[0])).float().cuda()
+        check(R.Rule(4, score=score, n_groups=10, top_groups=3, group_best=2), x, wg, b)
+        check(R.Rule(6, score=score, n_groups=4, top_groups=2), x, wg, b)
+        check(R.Rule(4, score=score), x, wg, b)
+
+
 def test_far_logits():
     """Scores that saturate or underflow: shares by their logarithms."""
     T, d, E = 16, 128, 12
@@ -450,9 +490,9 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         with pytest.raises(ValueError, match="current device"):
             P.layernorm_backward(x, h, h)
     r._device = 1
-    with pytest.raises(ValueError, match="router's device"):
+    with pytest.raises(ValueError, match="on device 1"):
         r.route(x, idx, w)
-    with pytest.raises(ValueError, match="router's device"):
+    with pytest.raises(ValueError, match="on device 1"):
         r.backward(x, lg, idx, w, x)
     r._device = 0
     r.destroy()

@@ -251,3 +251,18 @@ def test_tuning_a_gate_by_the_experts_loads():
         assert off <= 2.0 ** -11, (name, off)
     assert np.linalg.norm(n(dwg) - rw) / np.linalg.norm(rw) <= 1e-5
     r.destroy()
+
+
+def test_a_destroyed_router_is_not_taken():
+    """... for the layer's own gate: the layer refuses it and keeps its router."""
+    wl, w, L, r, b = _layer(4)
+    L.set_router(r)
+    other = make(RULE, w[0], b, 4)
+    other.destroy()
+    with pytest.raises(ValueError, match="destroyed"):
+        L.set_router(other)
+    with pytest.raises(Exception, match="still route"):
+        r.destroy()
+    L.set_router(None)
+    r.destroy()
+    L.destroy()

@@ -68,7 +68,7 @@ def test_layernorm_rejects_bad_args():
 
     for bad in [dict(h=None), dict(x=None), dict(type=2), dict(T=0), dict(d=0), dict(d=96),
                 dict(d=16448), dict(eps=-1.0), dict(eps=float("nan")), dict(h=ODD), dict(x=ODD),
-                dict(gain=ODD), dict(bias=ODD)]:
+                dict(gain=ODD), dict(bias=ODD), dict(T=2097153)]:
         assert fwd(**bad) == B.MOE_EINVAL, bad
 
     def bwd(dx=P16, type=0, h=P16, gain=None, eps=1e-5, T=4, d=64, dh=P16, dg=P16, db=P16, ws=P16):
@@ -77,7 +77,7 @@ def test_layernorm_rejects_bad_args():
     for bad in [dict(dx=None), dict(h=None), dict(dh=None), dict(type=3), dict(T=0), dict(d=96),
                 dict(eps=-1.0), dict(ws=None), dict(ws=None, dg=None), dict(ws=None, db=None),
                 dict(dx=ODD), dict(h=ODD), dict(gain=ODD), dict(dh=ODD), dict(dg=ODD),
-                dict(db=ODD), dict(ws=ODD)]:
+                dict(db=ODD), dict(ws=ODD), dict(T=2097153)]:
         assert bwd(**bad) == B.MOE_EINVAL, bad
 
 
@@ -86,7 +86,7 @@ def test_layernorm_workspace_sizes():
     for T, d in [(1, 64), (200, 320), (8192, 4096), (100000, 16384)]:
         assert B.layernorm_workspace(T, d) % 256 == 0
     n = ctypes.c_int64()
-    for T, d in [(0, 64), (4, 96), (4, 0), (4, 16448)]:
+    for T, d in [(0, 64), (4, 96), (4, 0), (4, 16448), (2097153, 64)]:
         assert B.lib().moe_layernorm_workspace(T, d, ctypes.byref(n)) == B.MOE_EINVAL
     assert B.lib().moe_layernorm_workspace(4, 64, None) == B.MOE_EINVAL
 
