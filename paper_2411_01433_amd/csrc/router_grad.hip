@@ -10,10 +10,11 @@
 //
 // and then  d_x = dl Wg,  d_Wg = dl^T x,  two matrix products on the matrix
 // cores.  Their fp32 operand dl is split into numbers of 16 bits whose
-// products are added in fp32: for fp16 two of them (22 bits), scaled by a
-// power of two per group of 64 tokens so that the group's largest lies below
-// 2^15; for bf16, which has the range, three (24 bits) for d_Wg and the first
-// two (16 bits) for d_x, whose own 8 bits are far above.
+// products are added in fp32: for fp16 two of them (22 bits, or what is
+// above 2^-39 of the largest), scaled by a power of two per group of 64 tokens
+// so that the group's largest lies below 2^15; for bf16, which has the range,
+// three (24 bits) for d_Wg and the first two (16 bits) for d_x, whose own 8
+// bits are far above.
 #include "moe_internal.h"
 
 namespace moe {
@@ -114,6 +115,19 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
   const float none = -__builtin_inff();
   const int t0 = blockIdx.x * kGroupTokens + wave * kWaveTokens;   // the wave's first token
   const int mi = lane >> 4, k = lane & 15;                         // this lane's token and slot
+  // rows of the logits (a softmax of all experts) and of their gradient: on
+  // their way first
+  float ex[kWaveTokens][C], more[kWaveTokens][C];
+#pragma unroll
+  for (int i = 0; i < kWaveTokens; ++i)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int ee = c * 64 + lane;
+      const int64_t at = (int64_t)(t0 + i) * p.E + ee;
+      const bool in = t0 + i < T && ee < p.E;
+      ex[i][c] = full && in ? logits[at] : none;
+      more[i][c] = dl && in ? dl[at] : 0.0f;
+    }
   // slots
   int e = -1;
   float up = 0.0f, l = none;
@@ -126,17 +140,14 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
   }
   const bool have = e >= 0;
   // softmax of all experts: the rows' exponentials and sums
-  float ex[kWaveTokens][C], top = 0.0f, all = 1.0f;
+  float top = 0.0f, all = 1.0f;
   if (full) {
 #pragma unroll
     for (int i = 0; i < kWaveTokens; ++i) {
       float most = none, sum = 0.0f;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int ee = c * 64 + lane;
-        ex[i][c] = t0 + i < T && ee < p.E ? logits[(int64_t)(t0 + i) * p.E + ee] : none;
+      for (int c = 0; c < C; ++c)
         if (finite(ex[i][c])) most = fmaxf(most, ex[i][c]);
-      }
       most = wave_max_f(most);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -177,7 +188,7 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     for (int c = 0; c < C; ++c) {
       const int ee = c * 64 + lane;
       float v = full && ex[i][c] > 0.0f ? by * ex[i][c] : 0.0f;
-      if (dl && t0 + i < T && ee < p.E) v += dl[(int64_t)(t0 + i) * p.E + ee];
+      v += more[i][c];
       rows[wave * kWaveTokens + i][ee] = v;
     }
   }
@@ -397,27 +408,25 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
   }
 }
 
-// d_Wg of kCols columns: WE waves take 32 experts each, and the WT = 8 / WE
-// sets of them 64 tokens at a time in turn; x's rows of a set's tokens lie in
-// LDS.  Every 64 tokens' sum is scaled and added: their own scale allows it,
-// and a long sum keeps its bits.  Sets and blocks over the tokens write a
-// partial sum each, part[set][E][d].
-constexpr int kDwThreads = 512;
+// d_Wg of kCols columns: a block's WE waves take 32 experts each, of 64 tokens
+// at a time, whose rows of x lie in LDS.  Every 64 tokens' sum is scaled and
+// added: their own scale allows it, and a long sum keeps its bits.  Blocks over
+// the tokens write a partial sum each, part[block][E][d].
 template <class T16, int WE>
-__global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, int T,
+__global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, int T,
                                                                const T16* __restrict__ x,
                                                                const T16* __restrict__ fw,
                                                                const float* __restrict__ scales,
                                                                float* __restrict__ part) {
   typedef typename Split<T16>::x8 x8;
-  constexpr int WT = 8 / WE, kW = Split<T16>::kW;
-  constexpr int kLoads = 16 / WE;   // 16-byte chunks of 64 rows per thread of a set
+  constexpr int kW = Split<T16>::kW;
+  constexpr int kLoads = 16 / WE;   // 16-byte chunks of 64 rows per thread
   // a turn's loads during the turn before, where registers allow
-  constexpr bool kDlAhead = WE >= 4, kXAhead = WE >= 2;
-  constexpr int kTiles = WT <= 4 ? 2 : 1;  // two tiles in turn where LDS holds them
-  __shared__ __attribute__((aligned(16))) unsigned char tiles[kTiles][WT][kGroupTokens * 256];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int we = wave % WE, wt = wave / WE, set = blockIdx.x * WT + wt, sets = gridDim.x * WT;
+  constexpr bool kDlAhead = WE >= (kW == 2 ? 4 : 8), kXAhead = WE >= 2;
+  constexpr int kTiles = WE >= 2 ? 2 : 1;  // two tiles in turn where a unit's LDS holds them
+  __shared__ __attribute__((aligned(16))) unsigned char tiles[kTiles][kGroupTokens * 256];
+  const int lane = threadIdx.x & 63, we = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int set = blockIdx.x, sets = gridDim.x;
   const int n0 = blockIdx.y * kCols;
   const int ET = ((p.E + 31) & ~31) / 16, et = blockIdx.z * 16 + we * 2;
   const int groups = (T + kGroupTokens - 1) / kGroupTokens, turns = (groups + sets - 1) / sets;
@@ -453,7 +462,7 @@ __global__ __launch_bounds__(kDwThreads) void router_dw_kernel(RouterParams p, i
   if (kXAhead) load_x(0);
   if (kDlAhead) load_dl(0);
   for (int turn = 0; turn < turns; ++turn) {
-    unsigned char* tile = tiles[turn % kTiles][wt];
+    unsigned char* tile = tiles[turn % kTiles];
     if (!kXAhead) load_x(turn);
     if (kTiles == 1) __syncthreads();   // (the last turn's reads)
 #pragma unroll
@@ -546,13 +555,13 @@ __global__ __launch_bounds__(kJoinThreads) void router_join_kernel(const float* 
 }
 
 // Waves over the experts of a block of d_Wg, and the blocks over the tokens:
-// about one block per compute unit.
+// about eight waves per compute unit.
 int dw_waves(int E) { return E <= 32 ? 1 : E <= 64 ? 2 : E <= 128 ? 4 : 8; }
 int dw_splits(int T, int d, int E) {
   const int tiles = ((d + kCols - 1) / kCols) * ((E + 255) / 256);
-  const int sets = 8 / dw_waves(E), groups = (T + kGroupTokens - 1) / kGroupTokens;
-  const int want = (256 + tiles - 1) / tiles, most = (groups + sets - 1) / sets;
-  return want < most ? want : most;
+  const int groups = (T + kGroupTokens - 1) / kGroupTokens;
+  const int want = (2048 / dw_waves(E) + tiles - 1) / tiles;
+  return want < groups ? want : groups;
 }
 
 size_t up(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -563,7 +572,7 @@ struct Plan {
 template <class T16>
 Plan plan(int T, int d, int E) {
   const size_t Tp = ((size_t)T + 63) & ~(size_t)63, Ep = ((size_t)E + 31) & ~(size_t)31;
-  const size_t sets = (size_t)dw_splits(T, d, E) * (8 / dw_waves(E));
+  const size_t sets = (size_t)dw_splits(T, d, E);
   Plan q;
   size_t off = 0;
   q.fx = off; off += up(Tp * Ep * Split<T16>::kX * 2);
@@ -606,13 +615,13 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (!dwg) return hipSuccess;
-  const int we = dw_waves(p.E), splits = dw_splits(T, p.d, p.E), sets = splits * (8 / we);
-  const dim3 grid_w(splits, (p.d + kCols - 1) / kCols, (p.E + 255) / 256);
+  const int we = dw_waves(p.E), sets = dw_splits(T, p.d, p.E);
+  const dim3 grid_w(sets, (p.d + kCols - 1) / kCols, (p.E + 255) / 256);
   float* to = sets == 1 ? dwg : part;
-  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
-  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
-  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
-  else router_dw_kernel<T16, 8><<<grid_w, kDwThreads, 0, s>>>(p, T, x, fw, scales, to);
+  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, 64, 0, s>>>(p, T, x, fw, scales, to);
+  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, 128, 0, s>>>(p, T, x, fw, scales, to);
+  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, 256, 0, s>>>(p, T, x, fw, scales, to);
+  else router_dw_kernel<T16, 8><<<grid_w, 512, 0, s>>>(p, T, x, fw, scales, to);
   if ((e = hipGetLastError()) != hipSuccess || sets == 1) return e;
   const int64_t size = (int64_t)p.E * p.d;
   router_join_kernel<<<(unsigned)((size / 4 + 63) / 64), kJoinThreads, 0, s>>>(part, sets, size, dwg);
