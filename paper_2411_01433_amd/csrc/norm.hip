@@ -8,6 +8,11 @@
 // One block per row, which it holds in registers: h is read once.  The
 // variance is the mean square of the centred values (no difference of large
 // sums).  All of it in fp32; x and d_x are of 16 bits.
+//
+// Both passes are bound by memory: 8192 rows of 4096 take 37.2 us (5.4 TB/s of
+// h read and x written, a 1 GiB copy 5.1) and 58 + 4.6 us backward (5.7 TB/s
+// of h, d_x and d_h).  One row is two dependent trips to memory and a launch,
+// 3.0 us.
 #include "moe_internal.h"
 
 namespace moe {
@@ -16,7 +21,10 @@ namespace {
 
 constexpr int kPieces = 4;  // float4 pieces of a row per thread
 
-// Threads of a row's block: d <= 16 columns per thread.
+// Threads of a row's block: the fewest with at most 16 columns each.  us for
+// 8192 rows against the next larger block: d 320 6.5 9.3, 1024 9.8 13.0, 2048
+// 20.6 24.7, 4096 37.8 39.0, 8192 75.3 84.4; backward d 320 12.9 24.0, 1024
+// 18.4 26.1, 2048 34.1 51.3, 4096 58.4 62.7, 8192 109.5 147.3.
 inline int row_threads(int d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
 
 template <class T16>
@@ -219,6 +227,10 @@ __global__ __launch_bounds__(kSumThreads) void column_sums_kernel(const float* _
   }
 }
 
+// Blocks of the backward pass, as many as are at work at once: each has a row
+// of column sums that the second kernel reads.  us of both kernels for 8192 rows
+// with half / these / twice as many: d 1024 30.1 23.4 26.6, 2048 49.0 38.2
+// 42.6, 4096 62.1 63.0 71.4, 8192 167.9 114.0 120.7 (d 320 24.0 17.6 17.4).
 int backward_blocks(int T, int d) {
   const int most = d <= 1024 ? 1024 : d <= 4096 ? 512 : 256;
   return T < most ? T : most;

@@ -858,7 +858,9 @@ __device__ inline void add_counts(const RouterParams& p, const RouterOut& o, con
 }
 
 // Many tokens: one per wave in turn; those that fp32 leaves open go on a list.
-// Few blocks of many waves, so that few of them add to the counts.
+// Few blocks of many waves, so that few of them add to the counts.  Bound by
+// the issue of about 1100 vector instructions per token: 8192 tokens x 256
+// experts in groups 23.8 us.
 constexpr int kManyThreads = 1024;
 constexpr int kManyWaves = kManyThreads / 64;
 constexpr int kManyBlocks = 256;
@@ -890,7 +892,10 @@ __global__ __launch_bounds__(kManyThreads) void router_select_many_kernel(Router
   add_counts(p, o, counts);
 }
 
-// Tokens of a call or of the list, a team of TW waves each.
+// Tokens of a call or of the list, a team of TW waves each.  Bound by its
+// longest chain, an open token's: scores, then two or three rounds of sums in
+// 64 bits of a microsecond or two (32 tokens x 256 experts in groups 10 us, the
+// list of 8192 19 us).
 constexpr int team_threads(int tw) { return tw < 4 ? 256 : tw * 64; }
 template <class T16, int C, int TW>
 __global__ __launch_bounds__(team_threads(TW)) void router_select_kernel(RouterParams p, int T, int listed,
