@@ -197,3 +197,33 @@ def test_other_stream_and_graph():
             t.zero_()
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(snap(), want)), i
+
+
+def test_offsets_past_32_bits():
+    """4.9 GB of rows: the last of them as in a call of their own."""
+    import paper_2411_01433_amd as P
+    T, d, n = 75000, 16384, 3
+    g = torch.Generator(device="cuda").manual_seed(8)
+    h = torch.randn((T, d), generator=g, device="cuda")
+    gain = torch.randn(d, generator=g, device="cuda")
+    x = torch.empty((T, d), dtype=torch.float16, device="cuda")
+    P.layernorm(h, x, gain, gain)
+    tail = h[-n:].clone()
+    own = torch.empty((n, d), dtype=torch.float16, device="cuda")
+    P.layernorm(tail, own, gain, gain)
+    assert torch.equal(x[-n:], own)
+    # gradients of the first and the last rows only: the others add zeros
+    dx = x.zero_()
+    dx[0] = dx[-n:] = torch.randn(d, generator=g, device="cuda").half()
+    dg, db = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    dh = torch.empty_like(h)
+    P.layernorm_backward(dx, h, dh, gain, dg, db)
+    rows = torch.cat([h[:1], tail])
+    few, dfew = torch.cat([dx[:1], dx[-n:]]), torch.empty((n + 1, d), device="cuda")
+    dg2, db2 = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    P.layernorm_backward(few, rows, dfew, gain, dg2, db2)
+    assert torch.equal(dh[-n:], dfew[1:]) and torch.equal(dh[:1], dfew[:1])
+    # four terms each, in two orders: each order rounds three times to half a step
+    norm = (rows - rows.mean(1, keepdim=True)) / rows.std(1, keepdim=True)
+    for a, b, terms in ((dg, dg2, few.float() * norm), (db, db2, few.float())):
+        assert ((a - b).abs() <= 6 * U * 1.01 * terms.abs().sum(0)).all()

@@ -477,6 +477,36 @@ def test_refusals():
         r.route(x, idx, w)
 
 
+def test_offsets_past_31_bits():
+    """The largest call, 2 GiB of tokens: its last 64 as in a call of their own."""
+    T, d, E, n = 65536, 16384, 20, 64
+    rule = R.Rule(4, score=G, n_groups=5, top_groups=3, group_best=2)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((T, d), generator=g, device="cuda", dtype=F16)
+    wg = torch.randn((E, d), generator=g, device="cuda").mul_(d ** -0.5).to(F16)
+    b = torch.randn(E, generator=g, device="cuda") * 0.02
+    tail = x[-n:].clone()
+    own, _, lg2 = check(rule, tail, wg, b)
+    r = make(rule, wg, b, T, backward=True)
+    idx, w, lg = (torch.empty((T, k), dtype=t, device="cuda")
+                  for k, t in ((4, torch.int32), (4, torch.float32), (E, torch.float32)))
+    count = torch.empty(E, dtype=torch.int32, device="cuda")
+    r.route(x, idx, w, lg, count)
+    assert torch.equal(idx[-n:], own[:n])
+    assert torch.equal(count.long(), torch.bincount(idx.flatten().long(), minlength=E))
+    assert (np.abs(_np(lg[-n:]) - _np(tail) @ _np(wg).T) <= logit_bound(tail, wg)).all()
+    # gradients of the last 64 weights only: the others add zeros
+    up = torch.zeros((T, 4), device="cuda")
+    up[-n:] = torch.randn((n, 4), generator=g, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty((E, d), device="cuda")
+    r.backward(x, lg, idx, up, dx, dw)
+    dx2, dw2 = torch.empty_like(tail), torch.empty((E, d), device="cuda")
+    r.backward(tail, lg[-n:].clone(), idx[-n:].clone(), up[-n:].clone(), dx2, dw2)
+    assert torch.equal(dx[-n:], dx2) and torch.equal(dw, dw2)
+    assert not dx[:-n].any()
+    r.destroy()
+
+
 def test_tensors_of_another_device_are_refused(monkeypatch):
     import paper_2411_01433_amd as P
     x, wg, _, _ = inputs(4, 128, 6, F16, 1, 0)
