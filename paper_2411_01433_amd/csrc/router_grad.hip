@@ -13,8 +13,8 @@
 // products are added in fp32: for fp16 two of them (22 bits, or what is
 // above 2^-39 of the largest), scaled by a power of two per group of 64 tokens
 // so that the group's largest lies below 2^15; for bf16, which has the range,
-// three (24 bits) for d_Wg and the first two (16 bits) for d_x, whose own 8
-// bits are far above.
+// three (24 bits).  (Two for d_x, whose outputs hold 8 bits, round about one
+// in 500 of them to the wrong side.)
 #include "moe_internal.h"
 
 namespace moe {
@@ -28,11 +28,11 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 template <class T16> struct Split;
 template <> struct Split<f16> {
   typedef f16x8v x8;
-  static constexpr int kX = 2, kW = 2;  // parts of dl for d_x and d_Wg
+  static constexpr int kParts = 2;
 };
 template <> struct Split<bf16> {
   typedef bf16x8 x8;
-  static constexpr int kX = 2, kW = 3;
+  static constexpr int kParts = 3;
 };
 
 __device__ inline f32x4 mfma(f16x8v a, f16x8v b, f32x4 c) {
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
   if (lane == 0) tops[wave] = most;
   __syncthreads();
   float scale = 1.0f;
-  if constexpr (sizeof(T16) == 2 && Split<T16>::kW == 2) {
+  if constexpr (Split<T16>::kParts == 2) {
     float top = 0.0f;
 #pragma unroll
     for (int w = 0; w < kLogitThreads / 64; ++w) top = fmaxf(top, tops[w]);
@@ -238,9 +238,9 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = rows[tt * 16 + m][eb * 32 + term(g, j)] * scale;
-      T16* to = fx + (((int64_t)(blockIdx.x * 4 + tt) * EB + eb) * Split<T16>::kX * 64 + lane) * 8;
+      T16* to = fx + (((int64_t)(blockIdx.x * 4 + tt) * EB + eb) * Split<T16>::kParts * 64 + lane) * 8;
 #pragma unroll
-      for (int part = 0; part < Split<T16>::kX; ++part) {
+      for (int part = 0; part < Split<T16>::kParts; ++part) {
         x8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = next_part<T16>(v[j]);
@@ -253,9 +253,9 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
       float v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = rows[tb * 32 + term(g, j)][et * 16 + m] * scale;
-      T16* to = fw + (((int64_t)(blockIdx.x * 2 + tb) * ET + et) * Split<T16>::kW * 64 + lane) * 8;
+      T16* to = fw + (((int64_t)(blockIdx.x * 2 + tb) * ET + et) * Split<T16>::kParts * 64 + lane) * 8;
 #pragma unroll
-      for (int part = 0; part < Split<T16>::kW; ++part) {
+      for (int part = 0; part < Split<T16>::kParts; ++part) {
         x8 o;
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] = next_part<T16>(v[j]);
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
                                                                const float* __restrict__ scales,
                                                                T16* __restrict__ dx) {
   typedef typename Split<T16>::x8 x8;
-  constexpr int kX = Split<T16>::kX;
+  constexpr int kParts = Split<T16>::kParts;
   __shared__ __attribute__((aligned(16))) unsigned char tile[EB * 32 * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n0 = blockIdx.y * kCols, eb_n = (p.E + 31) / 32;
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
   const int first = blockIdx.x * 4 + wave, every = gridDim.x * 4, all = (T + 31) / 32;
   const int steps = first < all ? ((all - first + every - 1) / every) * eb_n : 0;
   f32x4 acc[2][8];
-  x8 a[2][8], b[4][2][kX];
+  x8 a[2][8], b[4][2][kParts];
   const auto zero = [&]() {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -349,12 +349,12 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
       for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   };
   int load_at = first, load_eb = 0;
-  const auto load_dl = [&](x8 (&bv)[2][kX]) {
+  const auto load_dl = [&](x8 (&bv)[2][kParts]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int part = 0; part < kX; ++part)
-        bv[i][part] = global<x8>(fx)[(((int64_t)(load_at * 2 + i) * eb_n + load_eb) * kX + part) * 64 + lane];
+      for (int part = 0; part < kParts; ++part)
+        bv[i][part] = global<x8>(fx)[(((int64_t)(load_at * 2 + i) * eb_n + load_eb) * kParts + part) * 64 + lane];
     if (++load_eb == eb_n) {
       load_eb = 0;
       if (load_at + every < all) load_at += every;  // (past the last tile: that one again)
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
         load_wg(next, a[(u + 1) & 1]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int part = 0; part < kX; ++part)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -428,10 +428,10 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
                                                                const float* __restrict__ scales,
                                                                float* __restrict__ part) {
   typedef typename Split<T16>::x8 x8;
-  constexpr int kW = Split<T16>::kW;
+  constexpr int kParts = Split<T16>::kParts;
   constexpr int kLoads = 16 / WE;   // 16-byte chunks of 64 rows per thread
   // a turn's loads during the turn before, where registers allow
-  constexpr bool kDlAhead = WE >= (kW == 2 ? 4 : 8), kXAhead = WE >= 2;
+  constexpr bool kDlAhead = WE >= (kParts == 2 ? 4 : 8), kXAhead = WE >= 2;
   constexpr int kTiles = WE >= 2 ? 2 : 1;  // two tiles in turn where a unit's LDS holds them
   __shared__ __attribute__((aligned(16))) unsigned char tiles[kTiles][kGroupTokens * 256];
   const int lane = threadIdx.x & 63, we = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   u32x4 ahead[kLoads];
-  x8 b[2][2][kW];   // [32 tokens][16 experts][part]
+  x8 b[2][2][kParts];   // [32 tokens][16 experts][part]
   float s = 0.0f;
   const auto load_x = [&](int turn) {
     const int t0 = (turn * sets + set) * kGroupTokens;
@@ -465,8 +465,8 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int part = 0; part < kW; ++part)
-          b[k][i][part] = global<x8>(fw)[(((int64_t)(group * 2 + k) * ET + tile_e + i) * kW + part) * 64 + lane];
+        for (int part = 0; part < kParts; ++part)
+          b[k][i][part] = global<x8>(fw)[(((int64_t)(group * 2 + k) * ET + tile_e + i) * kParts + part) * 64 + lane];
   };
   if (kXAhead) load_x(0);
   if (kDlAhead) load_dl(0);
@@ -482,13 +482,13 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
     if (kXAhead) load_x(turn + 1);
     if (!kDlAhead) load_dl(turn);
     __syncthreads();
-    x8 now[2][2][kW];
+    x8 now[2][2][kParts];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int part = 0; part < kW; ++part) now[k][i][part] = b[k][i][part];
+        for (int part = 0; part < kParts; ++part) now[k][i][part] = b[k][i][part];
     const float by = s;
     if (kDlAhead) load_dl(turn + 1);
     __builtin_amdgcn_sched_barrier(0);
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int part = 0; part < kW; ++part)
+          for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -587,8 +587,8 @@ Plan plan(int T, int d, int E) {
   const size_t sets = (size_t)dw_splits(T, d, E);
   Plan q;
   size_t off = 0;
-  q.fx = off; off += up(Tp * Ep * Split<T16>::kX * 2);
-  q.fw = off; off += up(Tp * Ep * Split<T16>::kW * 2);
+  q.fx = off; off += up(Tp * Ep * Split<T16>::kParts * 2);
+  q.fw = off; off += up(Tp * Ep * Split<T16>::kParts * 2);
   q.scales = off; off += up(Tp / kGroupTokens * sizeof(float));
   q.part = off; off += up(sets * E * d * sizeof(float));
   q.bytes = off;

@@ -1,0 +1,77 @@
+"""Bits that the routing's gradients hold, at inputs where they show.
+
+Where a token has a gradient for one expert alone, d_x is one product and
+d_w_router a sum of as many products as tokens have that expert: the exact
+values are known, and what is off is the rounding of the logits' gradient into
+parts of 16 bits (fp16 two: 2^-23 of a value; bf16 three: 2^-25), of the sums
+and of the output.  A step of the matrix cores cuts each of its products at
+2^-24 of its largest, cuts the sum so far there and rounds it: with n products
+in a sum of one part at most 3 n of 2^-24."""
+import numpy as np
+import pytest
+
+from oracle import routing_oracle as R
+from test_gpu_router import BF16, F16, U, _np, make
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2411_01433_amd as P
+    P.lib()
+    yield
+
+
+def half_step(v, dtype):
+    """Half a step of `dtype` at the values v, subnormals among them."""
+    bits, least = (11, -14) if dtype is F16 else (8, -126)
+    e = np.maximum(np.floor(np.log2(np.maximum(np.abs(v), 1e-300))), least)
+    return 2.0 ** (e - bits)
+
+
+def one_expert_each(T, d, E, dtype, seed):
+    """x, gate, a gradient of the logits with one expert per token, its experts."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((T, d), generator=g).to(dtype).cuda()
+    wg = torch.randn((E, d), generator=g).to(dtype).cuda()
+    e = torch.arange(T) % E
+    v = torch.randn(T, generator=g)
+    dl = torch.zeros((T, E))
+    dl[torch.arange(T), e] = v
+    return x, wg, dl, e
+
+
+def backward(x, wg, dl, rule=R.Rule(1)):
+    """(d_x, d_w_router) from a gradient of the logits alone."""
+    T, E = dl.shape
+    r = make(rule, wg, None, T, backward=True)
+    dx, dw = torch.empty_like(x), torch.empty(wg.shape, device="cuda")
+    idx = torch.full((T, rule.top_k), -1, dtype=torch.int32, device="cuda")
+    r.backward(x, torch.zeros((T, E), device="cuda"), idx,
+               torch.zeros((T, rule.top_k), device="cuda"), dx, dw, dl.cuda())
+    torch.cuda.synchronize()
+    r.destroy()
+    return _np(dx), _np(dw)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("T,d,E", [(64, 1024, 5), (130, 320, 60), (300, 256, 160), (100, 192, 512)])
+def test_products_hold_their_bits(T, d, E, dtype):
+    """d_x: the product of three parts at most, 9 + 1 of 2^-24, rounded once to
+    the output's type.  d_w_router: n tokens of an expert in 64, whose sums are
+    added (twice 2^-24 each, scale and sum)."""
+    x, wg, dl, e = one_expert_each(T, d, E, dtype, T + E)
+    dx, dw = backward(x, wg, dl)
+    want = dl.double().numpy() @ _np(wg)
+    off = np.abs(dx - want)
+    tol = half_step(want, dtype) + 11 * U * np.abs(want)
+    assert (off <= tol).all(), ((off > tol).mean(), (off / tol).max())
+    want = dl.double().numpy().T @ _np(x)
+    of = np.abs(dl.double().numpy()).T @ np.abs(_np(x))
+    n, sets = -(-64 // E), -(-T // 64)
+    assert (np.abs(dw - want) <= (9 * n + 2 + 2 * sets) * U * of).all()
