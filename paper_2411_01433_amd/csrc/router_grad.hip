@@ -11,8 +11,9 @@
 // and then  d_x = dl Wg,  d_Wg = dl^T x,  two matrix products on the matrix
 // cores.  Their fp32 operand dl is split into numbers of 16 bits whose
 // products are added in fp32: for fp16 two of them (22 bits, or what is
-// above 2^-39 of the largest), scaled by a power of two per group of 64 tokens
-// so that the group's largest lies below 2^15; for bf16, which has the range,
+// above 2^-39 of the largest), scaled by a power of two so that the largest of
+// those that one sum takes lies below 2^15: of a token for d_x, of an expert
+// and 64 tokens for d_Wg; for bf16, which has the range,
 // three (24 bits).  (Two for d_x, whose outputs hold 8 bits, round about one
 // in 500 of them to the wrong side.)
 #include "moe_internal.h"
@@ -29,10 +30,12 @@ template <class T16> struct Split;
 template <> struct Split<f16> {
   typedef f16x8v x8;
   static constexpr int kParts = 2;
+  static constexpr bool kScaled = true;
 };
 template <> struct Split<bf16> {
   typedef bf16x8 x8;
   static constexpr int kParts = 3;
+  static constexpr bool kScaled = false;
 };
 
 __device__ inline f32x4 mfma(f16x8v a, f16x8v b, f32x4 c) {
@@ -59,7 +62,18 @@ __device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 // T and E rounded up to 64 and 32, with zeros.
 __device__ inline int term(int g, int j) { return j < 4 ? 4 * g + j : 12 + 4 * g + j; }
 
-constexpr int kGroupTokens = 64;   // tokens with one scale
+constexpr int kGroupTokens = 64;   // tokens with one scale per expert
+
+// Power of two that brings a largest magnitude `top` to [2^14, 2^15) (to as
+// much as 2^110 allows; zero like the smallest numbers), and its inverse, by
+// their exponents.
+struct Scale {
+  float by, back;
+};
+__device__ inline Scale scale_of(float top) {
+  const int e = min(max(268 - (int)(__builtin_bit_cast(uint32_t, top) >> 23), 14), 237);
+  return {__builtin_bit_cast(float, (uint32_t)e << 23), __builtin_bit_cast(float, (uint32_t)(254 - e) << 23)};
+}
 
 // Part `part` of v: what is left of it after the parts before, in 16 bits.
 template <class T16>
@@ -107,11 +121,12 @@ template <class T16, int C>
 __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     RouterParams p, int T, const float* __restrict__ logits, const int32_t* __restrict__ idx,
     const float* __restrict__ dw, const float* __restrict__ dl, T16* __restrict__ fx,
-    T16* __restrict__ fw, float* __restrict__ scales) {
+    T16* __restrict__ fw, float* __restrict__ scale_x, float* __restrict__ scale_w) {
   typedef typename Split<T16>::x8 x8;
   constexpr int LD = C * 64 + 4;
+  constexpr bool kScaled = Split<T16>::kScaled;
   __shared__ float rows[kGroupTokens][LD];
-  __shared__ float tops[kLogitThreads / 64];
+  __shared__ float by_token[kGroupTokens];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int Ep = (p.E + 31) & ~31;
   const bool sig = p.score == SCORE_SIGMOID, full = !p.renorm && !sig;
@@ -211,33 +226,32 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     }
   }
   wave_lds_fence();
-  float most = 0.0f;
+  if (kScaled && fx) {
 #pragma unroll
-  for (int i = 0; i < kWaveTokens; ++i)
+    for (int i = 0; i < kWaveTokens; ++i) {
+      float most = 0.0f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const float v = rows[wave * kWaveTokens + i][c * 64 + lane];
-      if (finite(v)) most = fmaxf(most, fabsf(v));
+      for (int c = 0; c < C; ++c) {
+        const float v = rows[wave * kWaveTokens + i][c * 64 + lane];
+        if (finite(v)) most = fmaxf(most, fabsf(v));
+      }
+      const Scale s = scale_of(wave_max_f(most));
+      if (lane == 0) {
+        by_token[wave * kWaveTokens + i] = s.by;
+        scale_x[t0 + i] = s.back;
+      }
     }
-  most = wave_max_f(most);
-  if (lane == 0) tops[wave] = most;
-  __syncthreads();
-  float scale = 1.0f;
-  if constexpr (Split<T16>::kParts == 2) {
-    float top = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kLogitThreads / 64; ++w) top = fmaxf(top, tops[w]);
-    if (top > 0.0f) scale = ldexpf(1.0f, min(max(14 - ilogbf(top), -113), 110));
   }
-  if (threadIdx.x == 0) scales[blockIdx.x] = 1.0f / scale;
+  __syncthreads();
   const int m = lane & 15, g = lane >> 4;
   const int EB = Ep / 32, ET = Ep / 16;
   if (fx)
     for (int q = wave; q < 4 * EB; q += kLogitThreads / 64) {
       const int tt = q / EB, eb = q - tt * EB;
+      const float by = kScaled ? by_token[tt * 16 + m] : 1.0f;
       float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = rows[tt * 16 + m][eb * 32 + term(g, j)] * scale;
+      for (int j = 0; j < 8; ++j) v[j] = rows[tt * 16 + m][eb * 32 + term(g, j)] * by;
       T16* to = fx + (((int64_t)(blockIdx.x * 4 + tt) * EB + eb) * Split<T16>::kParts * 64 + lane) * 8;
 #pragma unroll
       for (int part = 0; part < Split<T16>::kParts; ++part) {
@@ -248,18 +262,33 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
       }
     }
   if (fw)
-    for (int q = wave; q < 2 * ET; q += kLogitThreads / 64) {
-      const int tb = q / ET, et = q - tb * ET;
-      float v[8];
+    for (int et = wave; et < ET; et += kLogitThreads / 64) {
+      float v[2][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = rows[tb * 32 + term(g, j)][et * 16 + m] * scale;
-      T16* to = fw + (((int64_t)(blockIdx.x * 2 + tb) * ET + et) * Split<T16>::kParts * 64 + lane) * 8;
+      for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-      for (int part = 0; part < Split<T16>::kParts; ++part) {
-        x8 o;
+        for (int j = 0; j < 8; ++j) v[tb][j] = rows[tb * 32 + term(g, j)][et * 16 + m];
+      if constexpr (kScaled) {
+        float most = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = next_part<T16>(v[j]);
-        *reinterpret_cast<x8*>(to + part * 512) = o;
+        for (int j = 0; j < 16; ++j)
+          if (finite(v[j >> 3][j & 7])) most = fmaxf(most, fabsf(v[j >> 3][j & 7]));
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        const Scale s = scale_of(fmaxf(most, __shfl_xor(most, 32, 64)));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j >> 3][j & 7] *= s.by;
+        if (g == 0) scale_w[blockIdx.x * Ep + et * 16 + m] = s.back;
+      }
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
+        T16* to = fw + (((int64_t)(blockIdx.x * 2 + tb) * ET + et) * Split<T16>::kParts * 64 + lane) * 8;
+#pragma unroll
+        for (int part = 0; part < Split<T16>::kParts; ++part) {
+          x8 o;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = next_part<T16>(v[tb][j]);
+          *reinterpret_cast<x8*>(to + part * 512) = o;
+        }
       }
     }
 }
@@ -312,7 +341,7 @@ constexpr int kDxThreads = 256;
 template <class T16, int EB>
 __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p, int T,
                                                                const T16* __restrict__ fx,
-                                                               const float* __restrict__ scales,
+                                                               const float* __restrict__ scale_x,
                                                                T16* __restrict__ dx) {
   typedef typename Split<T16>::x8 x8;
   constexpr int kParts = Split<T16>::kParts;
@@ -342,7 +371,11 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
   const int steps = first < all ? ((all - first + every - 1) / every) * eb_n : 0;
   f32x4 acc[2][8];
   x8 a[2][8], b[4][2][kParts];
-  const auto zero = [&]() {
+  float scale[2];   // of this lane's two tokens
+  const auto start = [&](int w32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      scale[i] = Split<T16>::kScaled ? global<float>(scale_x)[w32 * 32 + i * 16 + (lane & 15)] : 1.0f;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -366,10 +399,10 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
       av[j] = read_columns<T16, 8>(tile, eb * 32, (j >> 1) * 64 + q * 16 + (j & 1) * 8);
   };
   const auto write = [&](int w32) {
-    const float s = global<float>(scales)[w32 * 32 / kGroupTokens];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int t = w32 * 32 + i * 16 + (lane & 15);
+      const float s = scale[i];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int c = n0 + k * 32 + g * 8;
@@ -387,7 +420,7 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
 #pragma unroll
   for (int u = 0; u < 3; ++u) load_dl(b[u]);
   load_wg(0, a[0]);
-  zero();
+  start(first);
   int w32 = first, eb = 0;
   for (int s0 = 0; s0 < steps; s0 += 4) {
 #pragma unroll
@@ -405,8 +438,8 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
             for (int i = 0; i < 2; ++i) acc[i][j] = mfma(a[u & 1][j], b[u][i][part], acc[i][j]);
         if (next == 0) {
           write(w32);
-          zero();
-          w32 += every;
+          if (w32 + every < all) w32 += every;
+          start(w32);
         }
         eb = next;
       }
@@ -416,7 +449,8 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
 
 // d_Wg of kCols columns: a block's WE waves take 32 experts each, of 64 tokens
 // at a time, whose rows of x lie in LDS.  Every 64 tokens' sum is scaled and
-// added: their own scale allows it, and a long sum keeps its bits.  Blocks over
+// added: a long sum keeps its bits, and an expert whose gradients are far below
+// the others' in these tokens (a softmax of all experts) its own.  Blocks over
 // the tokens write a partial sum each, part[block][E][d].
 // 8192 tokens x 256 experts, d 4096: 39 us (a library product of the unsplit
 // operands 59), of which x comes from memory at 1.9 TB/s; the rest is the
@@ -425,7 +459,7 @@ template <class T16, int WE>
 __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, int T,
                                                                const T16* __restrict__ x,
                                                                const T16* __restrict__ fw,
-                                                               const float* __restrict__ scales,
+                                                               const float* __restrict__ scale_w,
                                                                float* __restrict__ part) {
   typedef typename Split<T16>::x8 x8;
   constexpr int kParts = Split<T16>::kParts;
@@ -447,7 +481,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   u32x4 ahead[kLoads];
   x8 b[2][2][kParts];   // [32 tokens][16 experts][part]
-  float s = 0.0f;
+  float s[2] = {1.0f, 1.0f};   // scales of this lane's two experts
   const auto load_x = [&](int turn) {
     const int t0 = (turn * sets + set) * kGroupTokens;
 #pragma unroll
@@ -459,7 +493,11 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
   };
   const auto load_dl = [&](int turn) {
     const int group = min(turn * sets + set, groups - 1), tile_e = min(et, ET - 2);
-    s = global<float>(scales)[group];
+    if constexpr (Split<T16>::kScaled) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        s[i] = global<float>(scale_w)[(group * ET + tile_e + i) * 16 + (lane & 15)];
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -489,7 +527,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int part = 0; part < kParts; ++part) now[k][i][part] = b[k][i][part];
-    const float by = s;
+    const float by[2] = {s[0], s[1]};
     if (kDlAhead) load_dl(turn + 1);
     __builtin_amdgcn_sched_barrier(0);
     if (!mine || turn * sets + set >= groups) continue;
@@ -525,7 +563,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[i][(j - 1) * 2 + h] += by * sum[(j - 1) & 1][h][i];
+          for (int i = 0; i < 2; ++i) acc[i][(j - 1) * 2 + h] += by[i] * sum[(j - 1) & 1][h][i];
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -579,7 +617,7 @@ int dw_splits(int T, int d, int E) {
 size_t up(size_t b) { return (b + 255) & ~(size_t)255; }
 
 struct Plan {
-  size_t fx, fw, scales, part, bytes;  // offsets of the workspace
+  size_t fx, fw, scale_x, scale_w, part, bytes;  // offsets of the workspace
 };
 template <class T16>
 Plan plan(int T, int d, int E) {
@@ -589,19 +627,20 @@ Plan plan(int T, int d, int E) {
   size_t off = 0;
   q.fx = off; off += up(Tp * Ep * Split<T16>::kParts * 2);
   q.fw = off; off += up(Tp * Ep * Split<T16>::kParts * 2);
-  q.scales = off; off += up(Tp / kGroupTokens * sizeof(float));
+  q.scale_x = off; off += up(Split<T16>::kScaled ? Tp * sizeof(float) : 0);
+  q.scale_w = off; off += up(Split<T16>::kScaled ? Tp / kGroupTokens * Ep * sizeof(float) : 0);
   q.part = off; off += up(sets * E * d * sizeof(float));
   q.bytes = off;
   return q;
 }
 
 template <class T16, int EB>
-void dx_launch(const RouterParams& p, int T, const T16* fx, const float* scales, T16* dx, hipStream_t s) {
+void dx_launch(const RouterParams& p, int T, const T16* fx, const float* sx, T16* dx, hipStream_t s) {
   // about two blocks per compute unit, 128 tokens a block and turn.  us at 8192
   // tokens, d 4096, with one / two / four blocks: 8 experts 17.4 15.1 16.9, 60
   // 21.2 18.2 21.0, 256 41.1 35.0 38.9
   const int cols = (p.d + kCols - 1) / kCols, turns = (T + 127) / 128, want = (512 + cols - 1) / cols;
-  router_dx_kernel<T16, EB><<<dim3(want < turns ? want : turns, cols), kDxThreads, 0, s>>>(p, T, fx, scales, dx);
+  router_dx_kernel<T16, EB><<<dim3(want < turns ? want : turns, cols), kDxThreads, 0, s>>>(p, T, fx, sx, dx);
 }
 
 template <class T16>
@@ -611,31 +650,32 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
   char* base = static_cast<char*>(p.grad_ws);
   T16* fx = dx ? reinterpret_cast<T16*>(base + q.fx) : nullptr;
   T16* fw = dwg ? reinterpret_cast<T16*>(base + q.fw) : nullptr;
-  float* scales = reinterpret_cast<float*>(base + q.scales);
+  float* sx = reinterpret_cast<float*>(base + q.scale_x);
+  float* sw = reinterpret_cast<float*>(base + q.scale_w);
   float* part = reinterpret_cast<float*>(base + q.part);
   const int grid = (T + kGroupTokens - 1) / kGroupTokens;
-  if (p.E <= 64) router_dlogits_kernel<T16, 1><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, scales);
-  else if (p.E <= 128) router_dlogits_kernel<T16, 2><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, scales);
-  else if (p.E <= 256) router_dlogits_kernel<T16, 4><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, scales);
-  else router_dlogits_kernel<T16, 8><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, scales);
+  if (p.E <= 64) router_dlogits_kernel<T16, 1><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
+  else if (p.E <= 128) router_dlogits_kernel<T16, 2><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
+  else if (p.E <= 256) router_dlogits_kernel<T16, 4><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
+  else router_dlogits_kernel<T16, 8><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (dx) {
-    if (p.E <= 32) dx_launch<T16, 1>(p, T, fx, scales, dx, s);
-    else if (p.E <= 64) dx_launch<T16, 2>(p, T, fx, scales, dx, s);
-    else if (p.E <= 128) dx_launch<T16, 4>(p, T, fx, scales, dx, s);
-    else if (p.E <= 256) dx_launch<T16, 8>(p, T, fx, scales, dx, s);
-    else dx_launch<T16, 16>(p, T, fx, scales, dx, s);
+    if (p.E <= 32) dx_launch<T16, 1>(p, T, fx, sx, dx, s);
+    else if (p.E <= 64) dx_launch<T16, 2>(p, T, fx, sx, dx, s);
+    else if (p.E <= 128) dx_launch<T16, 4>(p, T, fx, sx, dx, s);
+    else if (p.E <= 256) dx_launch<T16, 8>(p, T, fx, sx, dx, s);
+    else dx_launch<T16, 16>(p, T, fx, sx, dx, s);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (!dwg) return hipSuccess;
   const int we = dw_waves(p.E), sets = dw_splits(T, p.d, p.E);
   const dim3 grid_w(sets, (p.d + kCols - 1) / kCols, (p.E + 255) / 256);
   float* to = sets == 1 ? dwg : part;
-  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, 64, 0, s>>>(p, T, x, fw, scales, to);
-  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, 128, 0, s>>>(p, T, x, fw, scales, to);
-  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, 256, 0, s>>>(p, T, x, fw, scales, to);
-  else router_dw_kernel<T16, 8><<<grid_w, 512, 0, s>>>(p, T, x, fw, scales, to);
+  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, 64, 0, s>>>(p, T, x, fw, sw, to);
+  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, 128, 0, s>>>(p, T, x, fw, sw, to);
+  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, 256, 0, s>>>(p, T, x, fw, sw, to);
+  else router_dw_kernel<T16, 8><<<grid_w, 512, 0, s>>>(p, T, x, fw, sw, to);
   if ((e = hipGetLastError()) != hipSuccess || sets == 1) return e;
   const int64_t size = (int64_t)p.E * p.d;
   router_join_kernel<<<(unsigned)((size / 4 + 63) / 64), kJoinThreads, 0, s>>>(part, sets, size, dwg);

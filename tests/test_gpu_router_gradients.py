@@ -75,3 +75,59 @@ def test_products_hold_their_bits(T, d, E, dtype):
     of = np.abs(dl.double().numpy()).T @ np.abs(_np(x))
     n, sets = -(-64 // E), -(-T // 64)
     assert (np.abs(dw - want) <= (9 * n + 2 + 2 * sets) * U * of).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("T,d,E", [(64, 256, 64), (192, 128, 160), (70, 320, 24)])
+def test_small_gradients_beside_large_ones(T, d, E, dtype):
+    """Experts whose gradients are 2^-6 to 2^-60 of others' in the same tokens
+    keep the bits of their gate rows, and tokens beside one whose gradient is
+    2^60 times theirs (and leaves the range of fp16) the bits of their d_x."""
+    x, wg, dl, e = one_expert_each(T, d, E, dtype, 5 * T)
+    for step in (6, 12):
+        small = dl * torch.exp2(-step * (torch.arange(E) % 6).float())
+        _, dw = backward(x, wg, small)
+        want = small.double().numpy().T @ _np(x)
+        of = np.abs(small.double().numpy()).T @ np.abs(_np(x))
+        n, sets = -(-64 // E), -(-T // 64)
+        assert (np.abs(dw - want) <= (9 * n + 2 + 2 * sets) * U * of).all()
+    dl[3] *= 2.0 ** 60
+    dx, _ = backward(x, wg, dl)
+    want = dl.double().numpy() @ _np(wg)
+    rest = np.arange(T) != 3
+    tol = half_step(want, dtype) + 11 * U * np.abs(want)
+    assert (np.abs(dx - want) <= tol)[rest].all()
+    if dtype is F16:
+        far = np.abs(want[3]) > 2 * 65504
+        assert far.any() and np.isinf(dx[3, far]).all()
+
+
+def test_unlikely_experts_of_a_softmax_over_all():
+    """Gate rows of experts whose logits lie 15, 20 and 25 below the rest, whose
+    gradients are products of their scores: within the functions' rounding, 64 u
+    (1 + the largest |logit|) of every term, the parts' and the sums'."""
+    T, d, E = 128, 192, 60
+    rule = R.Rule(4, renormalize=False)
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((T, d), generator=g).half().cuda()
+    wg = (torch.randn((E, d), generator=g) * 0.05).half().cuda()
+    l = x.float() @ wg.float().T
+    l[:, 7] -= 15
+    l[:, 8] -= 20
+    l[:, 9] -= 25
+    l64 = _np(l)
+    idx = np.stack([R.select(rule, r) for r in l64])
+    dw = torch.randn((T, 4), generator=g)
+    r = make(rule, wg, None, T, backward=True)
+    out = torch.empty((E, d), device="cuda")
+    r.backward(x, l, torch.from_numpy(idx).cuda(), dw.cuda(), None, out)
+    torch.cuda.synchronize()
+    r.destroy()
+    _, want, _ = R.route_backward(rule, _np(x), _np(wg), l64, idx, dw.numpy())
+    # magnitudes of the terms: the softmax's mean is a sum of four
+    terms = np.stack([R.scores(rule, l64[t]) * (np.abs(dw[t].numpy() * R.scores(rule, l64[t])[idx[t]]).sum()
+                      + np.isin(np.arange(E), idx[t]) * np.abs(dw[t].numpy()).max()) for t in range(T)])
+    of = terms.T @ np.abs(_np(x))
+    # (64 tokens in each of two parts: 3 x 64 x 2 of 2^-24, and the functions')
+    big = 1 + np.abs(l64).max()
+    assert (np.abs(_np(out) - want) <= (64 * big + 3 * 128 + 6) * U * of).all()
