@@ -320,7 +320,8 @@ moe_status moe_route(moe_router_t router, int32_t n_tokens, const void* x, int32
  * selection itself, and so the bias, has none).
  *  x, logits, topk_idx  as passed to and written by moe_route; a slot whose
  *            index is outside [0, n_experts), or whose logit is not finite,
- *            counts nothing, and equal indices of a token add up
+ *            counts nothing, and equal indices of a token add up; x of a token
+ *            without any gradient (a padded row) may hold anything, NaN too
  *  d_topk_w  device fp32 [n_tokens, top_k]
  *  d_logits  device fp32 [n_tokens, n_experts] or NULL: the gradient of
  *            losses on the logits themselves (balance, magnitude)

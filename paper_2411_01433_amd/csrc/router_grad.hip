@@ -121,7 +121,8 @@ template <class T16, int C>
 __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     RouterParams p, int T, const float* __restrict__ logits, const int32_t* __restrict__ idx,
     const float* __restrict__ dw, const float* __restrict__ dl, T16* __restrict__ fx,
-    T16* __restrict__ fw, float* __restrict__ scale_x, float* __restrict__ scale_w) {
+    T16* __restrict__ fw, float* __restrict__ scale_x, float* __restrict__ scale_w,
+    uint32_t* __restrict__ live) {
   typedef typename Split<T16>::x8 x8;
   constexpr int LD = C * 64 + 4;
   constexpr bool kScaled = Split<T16>::kScaled;
@@ -226,6 +227,19 @@ __global__ __launch_bounds__(kLogitThreads) void router_dlogits_kernel(
     }
   }
   wave_lds_fence();
+  if (fw) {
+    // tokens that have a gradient at all, a bit each: the others' x may hold
+    // anything (a padded row; one of no finite logit)
+    uint32_t on = 0;
+#pragma unroll
+    for (int i = 0; i < kWaveTokens; ++i) {
+      bool any = false;
+#pragma unroll
+      for (int c = 0; c < C; ++c) any |= !(rows[wave * kWaveTokens + i][c * 64 + lane] == 0.0f);
+      on |= (__ballot(any) != 0 ? 1u : 0u) << i;
+    }
+    if (lane == 0) live[blockIdx.x * (kLogitThreads / 64) + wave] = on;
+  }
   if (kScaled && fx) {
 #pragma unroll
     for (int i = 0; i < kWaveTokens; ++i) {
@@ -460,6 +474,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
                                                                const T16* __restrict__ x,
                                                                const T16* __restrict__ fw,
                                                                const float* __restrict__ scale_w,
+                                                               const uint32_t* __restrict__ live,
                                                                float* __restrict__ part) {
   typedef typename Split<T16>::x8 x8;
   constexpr int kParts = Split<T16>::kParts;
@@ -480,6 +495,8 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
   u32x4 ahead[kLoads];
+  uint32_t on[kLoads];   // which of a chunk's four tokens have a gradient
+  static_assert(kWaveTokens == 4, "four tokens per word of live");
   x8 b[2][2][kParts];   // [32 tokens][16 experts][part]
   float s[2] = {1.0f, 1.0f};   // scales of this lane's two experts
   const auto load_x = [&](int turn) {
@@ -487,6 +504,7 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int v = (i * WE + we) * 64 + lane, t = t0 + (v >> 4), c = n0 + (v & 15) * 8;
+      on[i] = global<uint32_t>(live)[min(turn * sets + set, groups - 1) * 16 + i * WE + we];
       // (rows past the end as zeros: what lies there may be no number)
       ahead[i] = t < T && c < p.d ? *global<u32x4>(x + (int64_t)t * p.d + c) : u32x4{0, 0, 0, 0};
     }
@@ -515,7 +533,8 @@ __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, i
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int v = (i * WE + we) * 64 + lane;
-      tile_put<32>(tile, v >> 4, (v & 15) * 16, ahead[i]);
+      const bool has = on[i] >> (lane >> 4) & 1;
+      tile_put<32>(tile, v >> 4, (v & 15) * 16, has ? ahead[i] : u32x4{0, 0, 0, 0});
     }
     if (kXAhead) load_x(turn + 1);
     if (!kDlAhead) load_dl(turn);
@@ -617,7 +636,7 @@ int dw_splits(int T, int d, int E) {
 size_t up(size_t b) { return (b + 255) & ~(size_t)255; }
 
 struct Plan {
-  size_t fx, fw, scale_x, scale_w, part, bytes;  // offsets of the workspace
+  size_t fx, fw, scale_x, scale_w, live, part, bytes;  // offsets of the workspace
 };
 template <class T16>
 Plan plan(int T, int d, int E) {
@@ -629,6 +648,7 @@ Plan plan(int T, int d, int E) {
   q.fw = off; off += up(Tp * Ep * Split<T16>::kParts * 2);
   q.scale_x = off; off += up(Split<T16>::kScaled ? Tp * sizeof(float) : 0);
   q.scale_w = off; off += up(Split<T16>::kScaled ? Tp / kGroupTokens * Ep * sizeof(float) : 0);
+  q.live = off; off += up(Tp / kWaveTokens * sizeof(uint32_t));
   q.part = off; off += up(sets * E * d * sizeof(float));
   q.bytes = off;
   return q;
@@ -652,12 +672,13 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
   T16* fw = dwg ? reinterpret_cast<T16*>(base + q.fw) : nullptr;
   float* sx = reinterpret_cast<float*>(base + q.scale_x);
   float* sw = reinterpret_cast<float*>(base + q.scale_w);
+  uint32_t* live = reinterpret_cast<uint32_t*>(base + q.live);
   float* part = reinterpret_cast<float*>(base + q.part);
   const int grid = (T + kGroupTokens - 1) / kGroupTokens;
-  if (p.E <= 64) router_dlogits_kernel<T16, 1><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
-  else if (p.E <= 128) router_dlogits_kernel<T16, 2><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
-  else if (p.E <= 256) router_dlogits_kernel<T16, 4><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
-  else router_dlogits_kernel<T16, 8><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw);
+  if (p.E <= 64) router_dlogits_kernel<T16, 1><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw, live);
+  else if (p.E <= 128) router_dlogits_kernel<T16, 2><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw, live);
+  else if (p.E <= 256) router_dlogits_kernel<T16, 4><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw, live);
+  else router_dlogits_kernel<T16, 8><<<grid, kLogitThreads, 0, s>>>(p, T, logits, idx, dw, dl, fx, fw, sx, sw, live);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (dx) {
@@ -672,10 +693,10 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const float* logits, 
   const int we = dw_waves(p.E), sets = dw_splits(T, p.d, p.E);
   const dim3 grid_w(sets, (p.d + kCols - 1) / kCols, (p.E + 255) / 256);
   float* to = sets == 1 ? dwg : part;
-  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, 64, 0, s>>>(p, T, x, fw, sw, to);
-  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, 128, 0, s>>>(p, T, x, fw, sw, to);
-  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, 256, 0, s>>>(p, T, x, fw, sw, to);
-  else router_dw_kernel<T16, 8><<<grid_w, 512, 0, s>>>(p, T, x, fw, sw, to);
+  if (we == 1) router_dw_kernel<T16, 1><<<grid_w, 64, 0, s>>>(p, T, x, fw, sw, live, to);
+  else if (we == 2) router_dw_kernel<T16, 2><<<grid_w, 128, 0, s>>>(p, T, x, fw, sw, live, to);
+  else if (we == 4) router_dw_kernel<T16, 4><<<grid_w, 256, 0, s>>>(p, T, x, fw, sw, live, to);
+  else router_dw_kernel<T16, 8><<<grid_w, 512, 0, s>>>(p, T, x, fw, sw, live, to);
   if ((e = hipGetLastError()) != hipSuccess || sets == 1) return e;
   const int64_t size = (int64_t)p.E * p.d;
   router_join_kernel<<<(unsigned)((size / 4 + 63) / 64), kJoinThreads, 0, s>>>(part, sets, size, dwg);

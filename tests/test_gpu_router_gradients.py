@@ -131,3 +131,40 @@ def test_unlikely_experts_of_a_softmax_over_all():
     # (64 tokens in each of two parts: 3 x 64 x 2 of 2^-24, and the functions')
     big = 1 + np.abs(l64).max()
     assert (np.abs(_np(out) - want) <= (64 * big + 3 * 128 + 6) * U * of).all()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("T,E", [(70, 8), (150, 60), (200, 100), (321, 256)])
+def test_tokens_without_a_gradient_may_hold_anything(T, E, dtype):
+    """Padded rows of NaN and infinities, whose slots are empty or whose
+    gradients are zero, among the others: the gradients of a call in which
+    those rows are zeros, bit for bit."""
+    d, rule = 192, R.Rule(4, score=R.SIGMOID)
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn((T, d), generator=g).to(dtype)
+    wg = (torch.randn((E, d), generator=g) * 0.1).to(dtype).cuda()
+    pad = torch.zeros(T, dtype=torch.bool)
+    pad[3:9] = pad[63:65] = pad[T - 5:] = True
+    if T > 192:
+        pad[128:192] = True   # 64 tokens that the kernels take together
+    clean = torch.where(pad[:, None], torch.zeros_like(x), x).cuda()
+    x[pad] = float("nan")
+    x[4], x[7, :9] = float("inf"), -float("inf")
+    x = x.cuda()
+    r = make(rule, wg, None, T, backward=True)
+    idx = torch.empty((T, 4), dtype=torch.int32, device="cuda")
+    w, lg = torch.empty((T, 4), device="cuda"), torch.empty((T, E), device="cuda")
+    r.route(x, idx, w, lg)
+    assert (idx[pad.cuda()] == -1).all()
+    up = torch.randn((T, 4), generator=g).cuda()
+    dl = (0.1 * torch.randn((T, E), generator=g))
+    dl[pad] = 0
+    for extra in (None, dl.cuda()):
+        got, want = [], []
+        for v, into in ((x, got), (clean, want)):
+            dx, dw = torch.empty_like(x), torch.empty((E, d), device="cuda")
+            r.backward(v, lg, idx, up, dx, dw, extra)
+            into += [dx, dw]
+        assert torch.isfinite(want[1]).all() and (want[0][pad.cuda()] == 0).all()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    r.destroy()
