@@ -255,6 +255,7 @@ struct Token {
   float in, out, group_err;
   float top, z, zrel; // softmax: largest logit, denominator, its relative error
   float margin;       // keys further apart are certainly in order
+  bool vague;         // scores whose errors are no small part of them
   bool groups_open, slots_open;
   int sel;
   float sl;           // its logit
@@ -374,6 +375,8 @@ __device__ void select_all(const RouterParams& p, const T16* xr, Token<C>& tk, O
 #pragma unroll
     for (int c = 0; c < C; ++c) z += finite(tk.l[c]) ? exp(key[c] - top) : 0.0;
     z = wave_sum(z);
+    tk.top = (float)top;   // (for the weights)
+    tk.z = (float)z;
   }
   Team<TW>::sync();
 #pragma unroll
@@ -486,8 +489,13 @@ __device__ inline void score_token(const RouterParams& p, float* row, Token<C>& 
     worst = fmaxf(worst, tk.fit[c] ? tk.err[c] : 0.0f);
   }
   // The scores by the fast exponential and reciprocal: within 1e-6 of a
-  // score, and of a softmax's term 1e-6 for each unit below the largest.
+  // score, of a sigmoid 1.2e-7 more for each unit below 0 (the exponent's
+  // rounding), and of a softmax's term 1e-6 for each unit below the largest.
   tk.zrel = soft ? wave_max(worst) + 4e-6f : 0.0f;
+  // A relative error r of a term counts as 1.01 r, which holds for its
+  // exponential up to 0.015; logits known less well, of thousands, leave all to
+  // 64 bits where scores enter the selection.
+  tk.vague = soft && (biased || p.n_groups > 1) && tk.zrel > 0.007f;
   if (soft) {
     tk.top = wave_max(tk.top);
 #pragma unroll
@@ -509,7 +517,8 @@ __device__ inline void score_token(const RouterParams& p, float* row, Token<C>& 
     } else {
       sc[c] = tk.fit[c] ? __builtin_amdgcn_rcpf(1.0f + __expf(-tk.l[c])) : 0.0f;
       // (the sigmoid's slope here, and what it may change by within the bound)
-      e1 = tk.err[c] * (1.001f * sc[c] * (1.0f - sc[c]) + 0.1f * tk.err[c]) + 1e-6f * sc[c];
+      e1 = tk.err[c] * (1.001f * sc[c] * (1.0f - sc[c]) + 0.1f * tk.err[c]) +
+           (1e-6f + 1.2e-7f * fmaxf(-tk.l[c], 0.0f)) * sc[c];
     }
     tk.key[c] = tk.l[c];
     if (biased) {
@@ -851,8 +860,8 @@ template <class T16, int C, int TW>
 __device__ inline void select_token(const RouterParams& p, const T16* xr, float* row, Token<C>& tk,
                                     OpenLds<C>& lds) {
   score_token(p, row, tk);
-  bool open = false;
-  if (tk.groups_open) open = !settle_groups<T16, C, TW>(p, xr, tk, lds);
+  bool open = tk.vague;
+  if (!open && tk.groups_open) open = !settle_groups<T16, C, TW>(p, xr, tk, lds);
   if (!open) {
     take_slots(p, row, tk);
     if (tk.slots_open) open = !select_slots<T16, C, TW>(p, xr, tk, lds);
@@ -895,7 +904,7 @@ __global__ __launch_bounds__(kManyThreads) void router_select_many_kernel(Router
     load_token(p, global<float>(lg + (int64_t)t * p.E), global<float>(p.w_norm), global<float>(p.x_norm)[t], tk);
     score_token(p, rows[wave], tk);
     take_slots(p, rows[wave], tk);
-    if (!tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
+    if (!tk.vague && !tk.groups_open && !tk.slots_open) finish(p, t, tk, o, counts);
     else if ((threadIdx.x & 63) == 0) opens[atomicAdd(&n_open, 1)] = t;
   }
   __syncthreads();

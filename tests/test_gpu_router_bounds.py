@@ -195,3 +195,51 @@ def test_selection_of_such_rows(kind, dtype):
         xs = (x.float() / max(1.0, (x.double() @ w.double().T).abs().max().item() / 4)).to(dtype)
         check(R.Rule(2, score=G), xs, w, b)
         check(R.Rule(2, score=G, n_groups=4, top_groups=2, group_best=2), xs, w, b)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("T,E,waves", [(1, 3, 8), (5, 40, 8), (600, 64, 8), (8192, 256, 4)])
+@pytest.mark.parametrize("n_groups", [1, 2])
+def test_scores_of_logits_that_fp32_does_not_know(T, E, waves, n_groups, dtype):
+    """Logits of some millions, whose fp32 sums are off by ones: a softmax beside
+    a bias, where the mask of the largest logit leaves scores that its error
+    makes a hundred times too small.  The score of an unmasked expert, about
+    0.27, counts against another's bias of 0.2."""
+    d = 4096
+    rows = torch.zeros((3, d))       # x, the masked expert, the other one
+    mine = torch.zeros(d, dtype=torch.bool)
+    for i in range(0, d // 64, waves):
+        mine[64 * i:64 * i + 64] = True
+    rows[0, mine] = 2.0 ** -12
+    rows[2, mine] = 1.859375 * 2.0 ** -12
+    rows[1] = -rows[2]
+    rows[:, 0] = torch.tensor([1.0, 1.5, 1.5])
+    n = int(mine.sum()) - 3
+    want = int(2 * n * 1.859375 + 2.5)
+    first = want & ~((1 << max(0, want.bit_length() - 8)) - 1)
+    rows[0, 1] = rows[0, 2] = 2.0 ** -6
+    rows[2, 1] = rows[2, 2] = 0.0
+    rows[1, 1], rows[1, 2] = first * 2.0 ** -18, (want - first) * 2.0 ** -18
+    rows[0] *= 2.0 ** 12
+    rows[1:] *= 2.0 ** 11
+    assert torch.equal(rows.to(dtype).float(), rows)
+    l = (rows[1:].double() @ rows[0].double()).numpy()
+    assert 0.5 < l[0] - l[1] < 1.5 and l[0] > 1e7
+    E += E % n_groups
+    wg = torch.zeros((E, d))
+    wg[0], wg[E - 1] = rows[1], rows[2]   # (in the first and the last group)
+    b = torch.full((E,), -1.0)
+    b[0], b[1], b[E - 1] = -float("inf"), 0.2, 0.0
+    wg, x = wg.to(dtype).cuda(), rows[0].expand(T, d).to(dtype).cuda().contiguous()
+    rule = R.Rule(1, renormalize=False, n_groups=n_groups, top_groups=1)
+    r = make(rule, wg, b.cuda(), T)
+    idx, w = torch.empty((T, 1), dtype=torch.int32, device="cuda"), torch.empty((T, 1), device="cuda")
+    r.route(x, idx, w)
+    torch.cuda.synchronize()
+    r.destroy()
+    score = R.scores(rule, np.concatenate([l[:1], np.zeros(E - 2), l[1:]]))[E - 1]
+    assert score > 0.25
+    assert (idx == E - 1).all()
+    # its weight by the sums in 64 bits, the logits rounded to fp32 (half a step
+    # of 2^23 and more is 0.5)
+    assert (np.abs(np.log(_np(w)) - np.log(score)) <= 1.01).all()
