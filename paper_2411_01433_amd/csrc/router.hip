@@ -169,6 +169,14 @@ __device__ inline void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// The same order for the compiler alone, which may take a lane's address as not
+// another's: a wave's LDS operations are done in their order, so that nothing
+// has to be waited for, least of all global loads on their way.
+__device__ inline void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // x . w for two rows w over d columns by one wave, in 64 bits (a product of two
 // 16-bit numbers is exact there).  Every lane gets the sums.
 template <class T16>
@@ -1049,6 +1057,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void router_logits_kernel(RouterPa
       }
     }
     load(i + 1);
+    wave_lds_order();
     __builtin_amdgcn_sched_barrier(0);
     // the piece's sums from zero (see the error of a logit), a row of tiles at
     // a time: registers
@@ -1069,6 +1078,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void router_logits_kernel(RouterPa
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[k][j] += sum[j];
     }
+    wave_lds_order();   // (the next piece is written over this one)
   }
   __syncthreads();
   float* red = reinterpret_cast<float*>(lds);
