@@ -29,6 +29,8 @@ moe_status fail(moe_status st, const char* fmt, ...) {
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   g_err = buf;
+  // reported here, not by the check of a later launch that succeeds
+  if (st == MOE_ENOMEM || st == MOE_EHIP) (void)hipGetLastError();
   return st;
 }
 

@@ -50,6 +50,8 @@ moe_status sfail(moe_status st, const char* fmt, ...) {
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   moe::set_last_error(buf);
+  // reported here, not by the check of a later launch that succeeds
+  if (st == MOE_ENOMEM || st == MOE_EHIP) (void)hipGetLastError();
   return st;
 }
 
