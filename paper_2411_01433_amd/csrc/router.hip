@@ -85,9 +85,9 @@ __device__ inline bool any_bits(u32x4 u) {
 // u q(x) q(w),
 //   q(x)^2 = 1.01 (sum over groups |x_g|^2 + sum over pieces |x_i|^2)
 //            + (waves + 7) |x|^2 + d 2^-28 (fp16).
-// (A sum over all of a wave's columns at once would have q 1.8 to 2.5 times
-// that at d 4096, and twice the tokens that it leaves open: 8192 x 256 in
-// groups 81 us for 76.)
+// (A sum over all of a wave's columns at once would have a bound 2 to 3 times as
+// large at d 4096: 8192 x 256 in groups 81 us instead of 76, for the tokens that
+// it leaves open.)
 // The squares of fp16 do not underflow in fp32; those of bf16 do below 1e-19,
 // and then count as the largest norm that can go with so small a sum (and with
 // subnormals).  A row of zeros has q 0, and its logits are exact.
@@ -131,6 +131,11 @@ __device__ inline double lane_value(double v, int from) {
   const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, from);
   const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), from);
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// (exp(-v) leaves the range below -709, before its inverse does)
+__device__ inline double sigmoid(double v) {
+  const double z = exp(-fabs(v));
+  return (v < 0.0 ? z : 1.0) / (1.0 + z);
 }
 __device__ inline double pair_d(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
@@ -390,7 +395,7 @@ __device__ void select_all(const RouterParams& p, const T16* xr, Token<C>& tk, O
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     tk.l[c] = finite(tk.l[c]) ? (float)key[c] : tk.l[c];
-    const double sc = !tk.fit[c] ? 0.0 : soft ? exp(key[c] - top) / z : 1.0 / (1.0 + exp(-key[c]));
+    const double sc = !tk.fit[c] ? 0.0 : soft ? exp(key[c] - top) / z : sigmoid(key[c]);
     if (biased) key[c] = sc + tk.b[c];
     if (Team<TW>::lead()) lds.row[c * 64 + lane] = !tk.fit[c] ? none : biased ? key[c] : sc;
     tk.kept[c] = tk.fit[c];
@@ -683,7 +688,7 @@ __device__ bool settle_groups(const RouterParams& p, const T16* xr, Token<C>& tk
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     // (a softmax's denominator is common to all groups without a bias)
-    const double sc = soft ? exp(l[c] - tk.top) / tk.z : 1.0 / (1.0 + exp(-l[c]));
+    const double sc = soft ? exp(l[c] - tk.top) / tk.z : sigmoid(l[c]);
     if (Team<TW>::lead()) lds.row[c * 64 + lane] = want[c] ? (biased ? sc + tk.b[c] : sc) : none;
     most = fmaxf(most, want[c] ? (float)sc : 0.0f);
   }
@@ -779,7 +784,7 @@ __device__ bool select_slots(const RouterParams& p, const T16* xr, Token<C>& tk,
   Team<TW>::sync();
   double s = 0.0, k = ml;
   if (biased) {
-    s = soft ? exp(ml - tk.top) / tk.z : 1.0 / (1.0 + exp(-ml));
+    s = soft ? exp(ml - tk.top) / tk.z : sigmoid(ml);
     k = s + mb;
   }
   const bool in = lane < n;

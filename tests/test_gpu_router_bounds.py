@@ -243,3 +243,19 @@ def test_scores_of_logits_that_fp32_does_not_know(T, E, waves, n_groups, dtype):
     # its weight by the sums in 64 bits, the logits rounded to fp32 (half a step
     # of 2^23 and more is 0.5)
     assert (np.abs(np.log(_np(w)) - np.log(score)) <= 1.01).all()
+
+
+@pytest.mark.parametrize("T,E", [(3, 12), (3, 60), (2100, 96)])
+@pytest.mark.parametrize("n_groups", [1, 4])
+def test_sigmoids_at_the_end_of_64_bits(T, E, n_groups):
+    """Scores of logits from -744 to -700, which are 1e-304 to 1e-323, beside a
+    bias of zeros: they have an order in 64 bits."""
+    d = 64
+    x = torch.zeros((T, d))
+    x[:, 0] = 1.0
+    wg = torch.zeros((E, d))
+    g = torch.Generator().manual_seed(E)
+    wg[:, 0] = -744.0 + 44 * torch.rand(E, generator=g)
+    wg[:, 0] = torch.round(wg[:, 0])
+    check(R.Rule(4, score=G, n_groups=n_groups, top_groups=1 if n_groups == 1 else 2, group_best=2),
+          x.half().cuda(), wg.half().cuda(), torch.zeros(E, device="cuda"))
