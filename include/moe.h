@@ -322,10 +322,12 @@ moe_status moe_route(moe_router_t router, int32_t n_tokens, const void* x, int32
  *            index is outside [0, n_experts), or whose logit is not finite,
  *            counts nothing, and equal indices of a token add up; x of a token
  *            without any gradient (a padded row) may hold anything, NaN too
- *  d_topk_w  device fp32 [n_tokens, top_k]
+ *  d_topk_w  device fp32 [n_tokens, top_k]: the caller's (a layer has no
+ *            backward pass to give it)
  *  d_logits  device fp32 [n_tokens, n_experts] or NULL: the gradient of
  *            losses on the logits themselves (balance, magnitude)
- *  d_x       device, `type` [n_tokens, d_model] or NULL: overwritten
+ *  d_x       device, `type` [n_tokens, d_model] or NULL: overwritten.  Every
+ *            row of w_router enters it and has to be finite
  *  d_w_router  device fp32 [n_experts, d_model] or NULL: overwritten
  * Pointers 16-byte aligned (topk_idx and d_topk_w 4-byte).  Sums run in a
  * fixed order: the same call gives the same bits. */
@@ -347,7 +349,8 @@ moe_status moe_router_destroy(moe_router_t router);
  * expert of the largest one runs at full precision.  A slot without an
  * expert is reported as index -1 and MOE_PREC_SKIP.
  *  - The router must be of type MOE_F16, with the layer's d_model, n_experts
- *    and top_k, at least its max_tokens, and on its device (else MOE_EINVAL).
+ *    and top_k (so 64 experts and top 8 at most), at least its max_tokens, and
+ *    on its device (else MOE_EINVAL).
  *  - It must outlive its use by the layer, and by graphs that captured calls
  *    of the layer with it; one router may serve several layers whose calls
  *    do not overlap (its workspace is one).

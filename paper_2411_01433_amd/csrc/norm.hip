@@ -13,10 +13,10 @@
 // not small against the spread the squares are summed again.  All of it in
 // fp32; x and d_x are of 16 bits.
 //
-// Both passes are bound by memory: 8192 rows of 4096 take 37.2 us (5.4 TB/s of
-// h read and x written, a 1 GiB copy 5.1) and 58 + 4.6 us backward (5.7 TB/s
+// Both passes are bound by memory: 8192 rows of 4096 take 37.5 us (5.4 TB/s of
+// h read and x written, a 1 GiB copy 5.1) and 60 + 4.7 us backward (5.6 TB/s
 // of h, d_x and d_h).  One row is two dependent trips to memory and a launch,
-// 3.0 us.
+// 3.3 us.
 #include "moe_internal.h"
 
 namespace moe {
@@ -26,9 +26,9 @@ namespace {
 constexpr int kPieces = 4;  // float4 pieces of a row per thread
 
 // Threads of a row's block: the fewest with at most 16 columns each.  us for
-// 8192 rows against the next larger block: d 320 6.5 9.3, 1024 9.8 13.0, 2048
-// 20.6 24.7, 4096 37.8 39.0, 8192 75.3 84.4; backward d 320 12.9 24.0, 1024
-// 18.4 26.1, 2048 34.1 51.3, 4096 58.4 62.7, 8192 109.5 147.3.
+// 8192 rows against the next larger block: d 320 5.7 11.2, 1024 10.2 13.1, 2048
+// 20.5 24.8, 4096 37.2 39.6, 8192 73.3 82.9; backward d 320 14.3 26.8, 1024
+// 19.4 31.1, 2048 37.6 64.7, 4096 61.5 77.0, 8192 109 160.
 inline int row_threads(int d) { return d <= 1024 ? 64 : d <= 4096 ? 256 : d <= 8192 ? 512 : 1024; }
 
 template <class T16>
@@ -264,8 +264,10 @@ __global__ __launch_bounds__(kSumThreads) void column_sums_kernel(const float* _
 
 // Blocks of the backward pass, as many as are at work at once: each has a row
 // of column sums that the second kernel reads.  us of both kernels for 8192 rows
-// with half / these / twice as many: d 1024 30.1 23.4 26.6, 2048 49.0 38.2
-// 42.6, 4096 62.1 63.0 71.4, 8192 167.9 114.0 120.7 (d 320 24.0 17.6 17.4).
+// with half / these / twice as many: d 320 26.6 18.2 19.7, 1024 33.9 24.3 30.0,
+// 2048 54.8 41.9 45.4, 4096 66.6 65.7 72.3, 8192 190 115 124.  A call of few rows
+// writes a row of sums for each of them: 512 rows with half / these, d 2048 10.7
+// 12.6, 4096 14.9 17.8, 8192 21.5 19.5; the rule does not go by that.
 int backward_blocks(int T, int d) {
   const int most = d <= 1024 ? 1024 : d <= 4096 ? 512 : 256;
   return T < most ? T : most;

@@ -820,8 +820,11 @@ __device__ inline void finish(const RouterParams& p, int t, const Token<C>& tk, 
   const int lane = threadIdx.x & 63;
   const float none = -__builtin_inff();
   const bool soft = p.score == SCORE_SOFTMAX;
-  // shares of the selected scores, so that scores that underflow still have
-  // their ratios
+  // The weights are those of the logits' fp32 sums (of the 64-bit ones where
+  // the token was open), whose error is theirs: 9e-8 on average at 1337 tokens x
+  // 60 experts, d 2048, the denominator's fast exponential among it.
+  // Shares of the selected scores, so that scores that underflow still have
+  // their ratios.
   const int sel = tk.sel;
   const bool have = sel >= 0;
   const float lm = wave_max(have ? tk.sl : none);  // (by every lane of the wave)
@@ -895,7 +898,7 @@ __device__ inline void add_counts(const RouterParams& p, const RouterOut& o, con
 // Many tokens: one per wave in turn; those that fp32 leaves open go on a list.
 // Few blocks of many waves, so that few of them add to the counts.  Bound by
 // the issue of about 1100 vector instructions per token: 8192 tokens x 256
-// experts in groups 23.8 us.
+// experts in groups 23.6 us.
 constexpr int kManyThreads = 1024;
 constexpr int kManyWaves = kManyThreads / 64;
 constexpr int kManyBlocks = 256;
@@ -929,8 +932,8 @@ __global__ __launch_bounds__(kManyThreads) void router_select_many_kernel(Router
 
 // Tokens of a call or of the list, a team of TW waves each.  Bound by its
 // longest chain, an open token's: scores, then two or three rounds of sums in
-// 64 bits of a microsecond or two (32 tokens x 256 experts in groups 10 us, the
-// list of 8192 19 us).
+// 64 bits of a microsecond or two (32 tokens x 256 experts in groups 9 to 16 us,
+// as the inputs leave some open, the list of 8192 20 us).
 constexpr int team_threads(int tw) { return tw < 4 ? 256 : tw * 64; }
 template <class T16, int C, int TW>
 __global__ __launch_bounds__(team_threads(TW)) void router_select_kernel(RouterParams p, int T, int listed,
@@ -1172,7 +1175,7 @@ hipError_t logits(const RouterParams& p, int T, const T16* x, float* lg, const R
   // blocks go to the eight dies in turn: those of one tile of tokens to the same
   // die, one right after another, which then finds the tokens in its L2 (us at
   // d 4096, against all tiles of tokens for one of experts after another: 16000
-  // x 256 72 87, 3000 x 256 20.3 24.4, 8192 x 512 65 69, 8192 x 256 35.0 35.2)
+  // x 256 69 86, 3000 x 256 21.3 25.0, 8192 x 512 63 67, 8192 x 256 35.0 35.2)
   const int tiles = (T + MT * 16 - 1) / (MT * 16), dies = tiles < 8 ? tiles : 8;
   const dim3 grid(dies, (p.E + NT * 16 - 1) / (NT * 16), (tiles + dies - 1) / dies);
   router_logits_kernel<T16, MT, NT, NW, false><<<grid, NW * 64, 0, s>>>(p, T, x, lg, o);
@@ -1184,14 +1187,17 @@ hipError_t select(const RouterParams& p, int T, const T16* x, const float* lg, c
                   hipStream_t s) {
   // Up to 2048 tokens a wave each, which sums again what is open in its own;
   // more by the kernel that leaves open tokens to a list, with a block of four
-  // waves each.  us at d 4096, 60 experts / 256 in 8 groups, a wave each
-  // against the list: 256 tokens 6.0 10.0 / 17.3 30.3, 1024 9.4 13.0 / 19.1
-  // 31.8, 2048 15.3 16.1 / 23.2 31.1, 4096 26.2 19.0 / 35.1 34.3, 8192 44.1
-  // 22.3 / 54.6 45.6 (the list with a wave each 49.2).
+  // waves each.  us at d 4096 with the experts' counts, 60 experts / 256 in 8
+  // groups / 512 in 8 groups, a wave each against the list: 256 tokens 5.5 8.2 /
+  // 17.1 30.8 / 24.7 47.9, 1024 9.8 16.4 / 18.2 32.5 / 25.0 48.5, 2048 16.3 18.2
+  // / 24.5 32.2 / 28.1 48.2, 4096 27.8 20.4 / 35.3 35.0 / 48.5 49.0, 8192 45.2
+  // 23.1 / 52.2 47.6 / 74.6 64.0.  Without the counts, to which many blocks add,
+  // a wave each is up to a tenth faster still at 8192 tokens x 256 (36.8 40.5).
   // A softmax beside a bias may need all of a token's logits in 64 bits, for
   // its denominator (45 us of one block at 256 experts): a block of eight
-  // waves each, for all tokens or those on the list: 64 tokens 20.2 32.7, 256
-  // 52.5 65.9, 512 58.4 67.1, 1024 74.1 67.1, 2048 118 89.
+  // waves each, for all tokens or those on the list: 64 tokens 17.6 29.5, 256
+  // 18.0 29.8, 512 30.2 30.2, 1024 45.0 30.8, 2048 75.1 31.5 (where none needs
+  // all; with one that does 98 and 85), 8192 282 131.
   const bool wide = p.bias && p.score == SCORE_SOFTMAX;
   constexpr int kWideEach = 512, kWaveEach = 2048, kListBlocks = 768;
   // (one expert per lane leaves those kernels with scratch memory that they
@@ -1228,10 +1234,10 @@ hipError_t run(const RouterParams& p, int T, const T16* x, const RouterOut& o, h
   // The tile of which the busiest compute unit loads the fewest rows: a block
   // loads tokens + experts of them, and there are 256 units.  us at d 4096, 256
   // experts, tiles of 64x64 / 64x32 / 32x32 / 16x32 / 16x16 on eight waves:
-  // 4096 tokens 21.9 26.8 32.8 43.7 53.1, 2048 20.4 15.9 17.9 22.9 28.1, 1024
-  // 19.7 14.6 11.0 13.6 15.6, 512 19.5 14.5 9.9 8.4 9.3, 64 18.9 14.4 9.8 7.3
-  // 5.7.  Two blocks of 64x64 fit a unit on four waves each, which is faster
-  // where there are so many: 8192 tokens 35.0, on eight waves 42.0.
+  // 4096 tokens 23.4 27.8 29.8 37.4 45.6, 2048 21.4 16.0 17.6 22.3 26.7, 1024
+  // 21.1 15.4 11.6 13.6 16.2, 512 21.0 14.8 10.5 8.4 10.1, 64 20.7 14.2 10.0 7.6
+  // 6.0.  Two blocks of 64x64 fit a unit on four waves each, which is faster
+  // where there are so many: 8192 tokens 34.8, on eight waves 40.3.
   constexpr int kTiles[5][2] = {{16, 16}, {16, 32}, {32, 32}, {64, 32}, {64, 64}};
   int tile = 0;
   int64_t least = 0, blocks = 0;

@@ -112,8 +112,9 @@ __device__ inline void wave_lds_fence() {
 // Gradient of the logits of 64 tokens, and its fragments.  A wave has four
 // tokens: 16 lanes each for their slots, all lanes for their rows of experts.
 // Bound by two dependent trips to memory (index, then logit) and the writing of
-// the fragments: 8192 tokens x 256 experts 11.8 us (16.8 MB written), 1337 x 60
-// of a softmax of all experts 6.2 us, 512 x 8 4.2 us.
+// the fragments, on a block for 64 tokens: 8192 tokens x 256 experts 13.1 us
+// (16.8 MB written, 128 of 256 units), 1337 x 60 of a softmax of all experts 7.2
+// us, 512 x 8 5.9 us.
 constexpr int kLogitThreads = 1024;
 constexpr int kWaveTokens = kGroupTokens / (kLogitThreads / 64);
 static_assert(kWaveTokens * 16 == 64 && kRouterMaxTopK <= 16, "a lane per slot");
@@ -348,7 +349,7 @@ __device__ inline typename Split<T16>::x8 read_columns(const unsigned char* tile
 // its tokens' dl for all columns.  Rows of the result are columns of
 // d, ordered so that a lane has 8 neighbouring ones of a token: tile 2 s + h,
 // row 4 q + r is column 32 s + 8 q + 4 h + r.
-// 8192 tokens x 256 experts, d 4096: 35 us (0.98 PFLOP/s of the split products,
+// 8192 tokens x 256 experts, d 4096: 36 us (0.95 PFLOP/s of the split products,
 // whose operands a wave reads from L2 and LDS in turn; a library product of the
 // unsplit operands takes 32).
 constexpr int kDxThreads = 256;
@@ -466,8 +467,8 @@ __global__ __launch_bounds__(kDxThreads, 2) void router_dx_kernel(RouterParams p
 // added: a long sum keeps its bits, and an expert whose gradients are far below
 // the others' in these tokens (a softmax of all experts) its own.  Blocks over
 // the tokens write a partial sum each, part[block][E][d].
-// 8192 tokens x 256 experts, d 4096: 39 us (a library product of the unsplit
-// operands 59), of which x comes from memory at 1.9 TB/s; the rest is the
+// 8192 tokens x 256 experts, d 4096: 41 us (a library product of the unsplit
+// operands 59), of which x comes from memory at 1.8 TB/s; the rest is the
 // transposing reads of x's tile, each for 32 experts' products.
 template <class T16, int WE>
 __global__ __launch_bounds__(WE * 64, 2) void router_dw_kernel(RouterParams p, int T,
@@ -623,8 +624,9 @@ __global__ __launch_bounds__(kJoinThreads) void router_join_kernel(const float* 
 // Waves over the experts of a block of d_Wg, and the blocks over the tokens:
 // eight waves per compute unit above 128 experts, else four.  us of product and
 // sum at d 4096 with half / these / twice as many: 8192 tokens x 256 experts
-// 65.8 45.9 58.0, 1000 x 256 19.5 19.4 31.4; with these / twice: 8192 x 100 34.8
-// 35.6, 1000 x 100 12.6 15.7, 8192 x 60 36.2 37.5, 8192 x 8 28.0 28.5.
+// 69.4 47.4 59.6, 1000 x 256 24.7 25.2 37.6, 8192 x 100 50.6 33.4 30.2, 1000 x
+// 100 16.3 17.6 20.8, 8192 x 60 40.6 30.5 29.4, 8192 x 8 30.3 24.0 22.6 (twice
+// as many are also twice the workspace).
 int dw_waves(int E) { return E <= 32 ? 1 : E <= 64 ? 2 : E <= 128 ? 4 : 8; }
 int dw_splits(int T, int d, int E) {
   const int tiles = ((d + kCols - 1) / kCols) * ((E + 255) / 256);
@@ -657,8 +659,8 @@ Plan plan(int T, int d, int E) {
 template <class T16, int EB>
 void dx_launch(const RouterParams& p, int T, const T16* fx, const float* sx, T16* dx, hipStream_t s) {
   // about two blocks per compute unit, 128 tokens a block and turn.  us at 8192
-  // tokens, d 4096, with one / two / four blocks: 8 experts 17.4 15.1 16.9, 60
-  // 21.2 18.2 21.0, 256 41.1 35.0 38.9
+  // tokens, d 4096, with one / two / four blocks: 8 experts 16.0 15.9 16.5, 60
+  // 19.8 18.2 19.0, 256 42.6 35.4 37.2
   const int cols = (p.d + kCols - 1) / kCols, turns = (T + 127) / 128, want = (512 + cols - 1) / cols;
   router_dx_kernel<T16, EB><<<dim3(want < turns ? want : turns, cols), kDxThreads, 0, s>>>(p, T, fx, sx, dx);
 }
