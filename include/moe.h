@@ -329,6 +329,8 @@ moe_status moe_route(moe_router_t router, int32_t n_tokens, const void* x, int32
  *  d_x       device, `type` [n_tokens, d_model] or NULL: overwritten.  Every
  *            row of w_router enters it and has to be finite
  *  d_w_router  device fp32 [n_experts, d_model] or NULL: overwritten
+ * The logits' gradient enters both products with 22 bits (MOE_F16) or 24
+ * (MOE_BF16) of each value, sums are in fp32.
  * Pointers 16-byte aligned (topk_idx and d_topk_w 4-byte).  Sums run in a
  * fixed order: the same call gives the same bits. */
 moe_status moe_route_backward(moe_router_t router, int32_t n_tokens, const void* x,

@@ -13,9 +13,10 @@
 // products are added in fp32: for fp16 two of them (22 bits, or what is
 // above 2^-39 of the largest), scaled by a power of two so that the largest of
 // those that one sum takes lies below 2^15: of a token for d_x, of an expert
-// and 64 tokens for d_Wg; for bf16, which has the range,
-// three (24 bits).  (Two for d_x, whose outputs hold 8 bits, round about one
-// in 500 of them to the wrong side.)
+// and 64 tokens for d_Wg; for bf16, which has the range, three (24 bits).  (Two
+// for d_x, whose outputs hold 8 bits, round about one in 500 of them to the
+// wrong side.)  With these d_Wg is 1.3e-7 off for both types at 512 to 8192
+// tokens, an fp32 product 1.4e-7 to 6.6e-7.
 #include "moe_internal.h"
 
 namespace moe {
