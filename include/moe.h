@@ -360,6 +360,122 @@ moe_status moe_router_destroy(moe_router_t router);
  *  - Not while a call of the layer is being enqueued by another thread. */
 moe_status moe_layer_set_router(moe_layer_t layer, moe_router_t router);
 
+/* ---- Products grouped by expert ------------------------------------------
+ * The experts' matrix products on their own, for layers that the fused entry
+ * points above do not run: other activations, tuning (with the backward pass
+ * below), 4-bit weights (moe_mx_product).  The rows of x are sorted by expert:
+ * expert e has the expert_count[e] rows (as moe_route counts them) behind
+ * those of the experts before it, and
+ *   y[r] = W[e(r)] x[r]
+ *  x       device, `type` [n_rows, d_in];  y  device, `type` [n_rows, d_out]
+ *  w       device, `type` [n_experts, d_out, d_in]
+ *  expert_count  device int32 [n_experts], or NULL: one expert with all rows
+ *          (n_experts 1, a plain product).  A negative count is no row, and
+ *          counts that sum to more than n_rows end at n_rows.
+ *  Rows behind the last expert's are not read, and those of y are left as they
+ *  were.  An expert without rows is not read.
+ *  type    MOE_F16 or MOE_BF16;  n_rows 0..2097152 (0: no work; x and y may be
+ *          NULL);  d_in, d_out  positive multiples of 64, <= 65536
+ *  n_experts  1..512
+ * Sums are in fp32, in an order that does not depend on the call before;
+ * results are rounded once.  Pointers 16-byte aligned, expert_count 4-byte.
+ * Needs no handle; works on the current device; outputs overlap no input,
+ * here and in the entry points below. */
+moe_status moe_grouped_product(const void* x, const void* w, const int32_t* expert_count, void* y,
+                               int32_t type, int32_t n_rows, int32_t d_in, int32_t d_out,
+                               int32_t n_experts, void* stream);
+
+/* Backward pass of moe_grouped_product:
+ *   d_x[r] = W[e(r)]^T d_y[r]
+ *   d_w[e] = sum over the rows r of e of d_y[r] x[r]^T
+ *  d_y     device, `type` [n_rows, d_out]: the gradient of y
+ *  x, w, expert_count and sizes as in the forward call; x may be NULL when d_w
+ *          is, and w when d_x is
+ *  d_x     device, `type` [n_rows, d_in] or NULL; rows behind the last
+ *          expert's are left as they were
+ *  d_w     device fp32 [n_experts, d_out, d_in] or NULL: overwritten (zeros
+ *          for an expert without rows), or with accumulate != 0 added to
+ * One of d_x and d_w must not be NULL.  The same call gives the same bits. */
+moe_status moe_grouped_product_backward(const void* d_y, const void* x, const void* w,
+                                        const int32_t* expert_count, void* d_x, float* d_w,
+                                        int32_t accumulate, int32_t type, int32_t n_rows,
+                                        int32_t d_in, int32_t d_out, int32_t n_experts,
+                                        void* stream);
+
+/* ---- Microscaled 4-bit floating point ------------------------------------
+ * The OCP microscaling format MXFP4: 32 consecutive columns of a row share a
+ * scale 2^e, stored as the byte e + 127, and hold a code of 4 bits each, sign
+ * and magnitude {0, 0.5, 1, 1.5, 2, 3, 4, 6}; column 2 j in the lower half of
+ * byte j.  The quantiser takes e = floor(log2 max|v|) - 2, at least -127 (a
+ * block of zeros: -127), and the code nearest to v / 2^e, ties to the even
+ * code, magnitudes beyond 6 to 6.  A block with an infinity or NaN gets the
+ * scale byte 255: all of it is NaN.
+ *  v       device, `type` [rows, cols]
+ *  codes   device u8 [rows, cols / 2];  scales  device u8 [rows, cols / 32]
+ *  values  device, `type` [rows, cols] or NULL: what the codes stand for
+ *          (exact in either type), for training through the rounding; may be v
+ *  type    MOE_F16 or MOE_BF16;  rows 0..2^31 - 1;  cols a positive multiple
+ *          of 64, <= 65536;  rows * cols < 2^36
+ * Pointers 16-byte aligned, scales 2-byte.  Needs no handle. */
+moe_status moe_mx_quantize(const void* v, int32_t type, int64_t rows, int64_t cols, void* codes,
+                           void* scales, void* values, void* stream);
+
+/* moe_grouped_product with W in MXFP4, and x in 16 bits or in MXFP4 too.
+ *  w_codes   device u8 [n_experts, d_out, d_in / 2];  w_scales  device u8
+ *            [n_experts, d_out, d_in / 32]
+ *  x         x_scales NULL: device, `type` [n_rows, d_in]; W's values enter
+ *            in that type (MOE_BF16 holds all below 2^128; MOE_F16 those of any
+ *            matrix quantised from fp16, others are rounded to it)
+ *            else device u8 [n_rows, d_in / 2], the codes of rows quantised
+ *            with the scales x_scales, device u8 [n_rows, d_in / 32]
+ *  y         device, `type` [n_rows, d_out]
+ * Everything else as moe_grouped_product; scales 2-byte aligned.  A scale byte
+ * of 255 gives NaN in every output that its block enters. */
+moe_status moe_mx_product(const void* x, const void* x_scales, const void* w_codes,
+                          const void* w_scales, const int32_t* expert_count, void* y, int32_t type,
+                          int32_t n_rows, int32_t d_in, int32_t d_out, int32_t n_experts,
+                          void* stream);
+
+/* ---- Gradient norm and clipping -------------------------------------------
+ * The end of a backward pass (moe_route_backward, moe_layernorm_backward,
+ * moe_grouped_product_backward): one norm over all gradients, and all of them
+ * scaled where it is too large.  A handle holds the list of the tensors. */
+typedef struct moe_gradients* moe_gradients_t;
+
+enum { MOE_F32 = 2 };  /* a third number format, for gradients */
+
+/* Create a list of n tensors (1..65536).
+ *  grads   host array of n device pointers, aligned to their elements
+ *  outs    host array of n device pointers, or NULL: scaled in place.  outs[i]
+ *          may be grads[i]; otherwise no two tensors overlap
+ *  sizes   host array: elements of each tensor, >= 0, their sum < 2^38 (a
+ *          tensor of none may have NULL pointers)
+ *  types   host array: MOE_F16, MOE_BF16 or MOE_F32 (grads and outs alike)
+ * The arrays are copied, the tensors borrowed: they must outlive their use.
+ * Allocates the list and a workspace on the current device and synchronises
+ * `stream`.  One handle must not be used from two streams concurrently. */
+moe_status moe_gradients_init(int32_t n, const void* const* grads, void* const* outs,
+                              const int64_t* sizes, const int32_t* types, void* stream,
+                              moe_gradients_t* out);
+
+/* norm = sqrt(sum of all squares), summed in 64 bits: device fp32 [1].  The
+ * same gradients give the same bits. */
+moe_status moe_gradients_norm(moe_gradients_t gradients, float* norm, void* stream);
+
+/* outs = grads * min(1, max_norm / (norm + 1e-6)) with the norm at `norm`
+ * (device fp32 [1]: the one above, or one joined over several devices'
+ * gradients).  Where it is not finite nothing is scaled, so that the caller
+ * can see it and skip the step.  max_norm finite, > 0. */
+moe_status moe_gradients_scale(moe_gradients_t gradients, float max_norm, const float* norm,
+                               void* stream);
+
+/* moe_gradients_norm and moe_gradients_scale in one call. */
+moe_status moe_gradients_clip(moe_gradients_t gradients, float max_norm, float* norm,
+                              void* stream);
+
+/* Free the list and its workspace (synchronises the device first). */
+moe_status moe_gradients_destroy(moe_gradients_t gradients);
+
 /* Copy an expert's quantised copy out (for inspection and parity).
  *  matrix  0 = W1, 1 = W3, 2 = W2;  bits 8, 4 or 2 (the copy must exist)
  *  codes   device u8 [rows, cols*bits/8];  scales device fp16 [rows, cols/32]

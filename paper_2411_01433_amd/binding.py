@@ -17,7 +17,7 @@ MOE_OK, MOE_EINVAL, MOE_ENOMEM, MOE_EHIP, MOE_ESTATE, MOE_EUNSUPPORTED = 0, -1, 
 TAG_FP16, TAG_INT4, TAG_INT2, TAG_MISS_INT4, TAG_MISS_INT2 = 0, 1, 2, 3, 4
 TAG_INT8, TAG_MISS_INT8_INT2 = 5, 6  # int8 models: int8 high copy, int2 low copy
 PREC_HIGH, PREC_LOW, PREC_SKIP = 0, 1, 2
-MOE_F16, MOE_BF16 = 0, 1
+MOE_F16, MOE_BF16, MOE_F32 = 0, 1, 2
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 MOE_ROUTER_BACKWARD = 1
 
@@ -39,6 +39,9 @@ EXPORTED = (
     "moe_layernorm", "moe_layernorm_workspace", "moe_layernorm_backward",
     "moe_router_init", "moe_route", "moe_route_backward", "moe_router_destroy",
     "moe_layer_set_router",
+    "moe_grouped_product", "moe_grouped_product_backward", "moe_mx_quantize", "moe_mx_product",
+    "moe_gradients_init", "moe_gradients_norm", "moe_gradients_scale", "moe_gradients_clip",
+    "moe_gradients_destroy",
 )
 
 
@@ -149,6 +152,17 @@ def lib() -> ctypes.CDLL:
     L.moe_route_backward.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.moe_router_destroy.argtypes = [vp]
     L.moe_layer_set_router.argtypes = [vp, vp]
+    sizes = [i32] * 5  # type, n_rows, d_in, d_out, n_experts
+    L.moe_grouped_product.argtypes = [vp, vp, vp, vp] + sizes + [vp]
+    L.moe_grouped_product_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32] + sizes + [vp]
+    L.moe_mx_quantize.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp]
+    L.moe_mx_product.argtypes = [vp, vp, vp, vp, vp, vp] + sizes + [vp]
+    L.moe_gradients_init.argtypes = [i32, ctypes.POINTER(vp), ctypes.POINTER(vp),
+                                     ctypes.POINTER(i64), pi32, vp, ctypes.POINTER(vp)]
+    L.moe_gradients_norm.argtypes = [vp, vp, vp]
+    L.moe_gradients_scale.argtypes = [vp, ctypes.c_float, vp, vp]
+    L.moe_gradients_clip.argtypes = [vp, ctypes.c_float, vp, vp]
+    L.moe_gradients_destroy.argtypes = [vp]
     L.moe_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
         if name != "moe_last_error":
@@ -331,6 +345,151 @@ def layernorm_backward(d_x, h, d_h, gain=None, d_gain=None, d_bias=None, eps: fl
         _addr_on(at, d_h, f32, rows, "d_h"), 1 if accumulate else 0,
         _addr_on(at, d_gain, f32, (d,), "d_gain"), _addr_on(at, d_bias, f32, (d,), "d_bias"),
         ws, _stream_on(at, stream)))
+
+
+def _weights(w, name):
+    """Shape (E, d_out, cols) of a three-dimensional tensor argument."""
+    if not isinstance(w, _th().Tensor) or w.dim() != 3:
+        raise ValueError(f"{name} must be a three-dimensional device tensor")
+    return w.shape
+
+
+def grouped_product(x, w, y, count=None, stream=None):
+    """y[r] = w[e(r)] x[r] for rows sorted by expert: x [R, d_in], y [R, d_out]
+    and w [E, d_out, d_in], all fp16 or bf16; count int32 [E] rows of each
+    expert (None: the one expert has all rows).  All on the current device."""
+    R, d_in = _rows(x, "x")
+    E, d_out, _ = _weights(w, "w")
+    at, kind = _current_device(x, "x"), x.dtype
+    _check(lib().moe_grouped_product(
+        _addr_on(at, x, kind, (R, d_in), "x"), _addr_on(at, w, kind, (E, d_out, d_in), "w"),
+        _addr_on(at, count, _th().int32, (E,), "count"),
+        _addr_on(at, y, kind, (R, d_out), "y"), _type16(kind, "x"), R, d_in, d_out, E,
+        _stream_on(at, stream)))
+
+
+def grouped_product_backward(d_y, x, w, count=None, d_x=None, d_w=None, accumulate: bool = False,
+                             stream=None):
+    """Gradients of grouped_product from d_y [R, d_out]: d_x [R, d_in] of x's
+    type and d_w fp32 [E, d_out, d_in] (with accumulate added to), either of
+    them None.  x may be None without d_w, w without d_x."""
+    if d_x is None and d_w is None:
+        raise ValueError("d_x and d_w are both None")
+    R, d_out = _rows(d_y, "d_y")
+    full = w if w is not None else d_w
+    E, _, d_in = _weights(full, "w" if w is not None else "d_w")
+    if x is None and d_w is not None:
+        raise ValueError("d_w needs x")
+    if w is None and d_x is not None:
+        raise ValueError("d_x needs w")
+    at, kind = _current_device(d_y, "d_y"), d_y.dtype
+    shape = (E, d_out, d_in)
+    _check(lib().moe_grouped_product_backward(
+        _addr_on(at, d_y, kind, (R, d_out), "d_y"), _addr_on(at, x, kind, (R, d_in), "x"),
+        _addr_on(at, w, kind, shape, "w"), _addr_on(at, count, _th().int32, (E,), "count"),
+        _addr_on(at, d_x, kind, (R, d_in), "d_x"), _addr_on(at, d_w, _th().float32, shape, "d_w"),
+        1 if accumulate else 0, _type16(kind, "d_y"), R, d_in, d_out, E, _stream_on(at, stream)))
+
+
+def mx_quantize(v, codes, scales, values=None, stream=None):
+    """Quantise v [rows, cols] (fp16 or bf16) to MXFP4: codes uint8 [rows,
+    cols / 2], scales uint8 [rows, cols / 32]; values, of v's type and shape (or
+    v itself): what they stand for."""
+    torch = _th()
+    rows, cols = _rows(v, "v")
+    at, kind = _current_device(v, "v"), v.dtype
+    _check(lib().moe_mx_quantize(
+        _addr_on(at, v, kind, (rows, cols), "v"), _type16(kind, "v"), rows, cols,
+        _addr_on(at, codes, torch.uint8, (rows, cols // 2), "codes"),
+        _addr_on(at, scales, torch.uint8, (rows, cols // 32), "scales"),
+        _addr_on(at, values, kind, (rows, cols), "values"), _stream_on(at, stream)))
+
+
+def mx_product(x, codes, scales, y, count=None, x_scales=None, stream=None):
+    """grouped_product with weights in MXFP4: codes uint8 [E, d_out, d_in / 2],
+    scales uint8 [E, d_out, d_in / 32], y [R, d_out] fp16 or bf16.  x [R, d_in]
+    of y's type, or with x_scales uint8 [R, d_in / 32] its codes uint8
+    [R, d_in / 2]."""
+    torch = _th()
+    R, cols = _rows(x, "x")
+    _rows(y, "y")
+    E, d_out, half = _weights(codes, "codes")
+    d_in = 2 * half
+    at, kind = _current_device(x, "x"), y.dtype
+    if x_scales is None:
+        xa = _addr_on(at, x, kind, (R, d_in), "x")
+    else:
+        xa = _addr_on(at, x, torch.uint8, (R, half), "x")
+    _check(lib().moe_mx_product(
+        xa, _addr_on(at, x_scales, torch.uint8, (R, d_in // 32), "x_scales"),
+        _addr_on(at, codes, torch.uint8, (E, d_out, half), "codes"),
+        _addr_on(at, scales, torch.uint8, (E, d_out, d_in // 32), "scales"),
+        _addr_on(at, count, torch.int32, (E,), "count"),
+        _addr_on(at, y, kind, (R, d_out), "y"), _type16(kind, "y"), R, d_in, d_out, E,
+        _stream_on(at, stream)))
+
+
+class MoeGradients:
+    """A list of gradient tensors (fp32, fp16 or bf16, any shapes, contiguous,
+    on the current device) and where their scaled values go: outs, of the same
+    types and sizes, or in place (None).  The tensors are kept alive."""
+
+    def __init__(self, grads, outs=None, stream=None):
+        torch = _th()
+        grads = list(grads)
+        outs = None if outs is None else list(outs)
+        n = len(grads)
+        if outs is not None and len(outs) != n:
+            raise ValueError(f"outs must be {n} tensors, got {len(outs)}")
+        kinds = {torch.float16: MOE_F16, torch.bfloat16: MOE_BF16, torch.float32: MOE_F32}
+        self.device = None
+        for i, g in enumerate(grads):
+            for name, t in (("grads", g),) + ((("outs", outs[i]),) if outs is not None else ()):
+                if not isinstance(t, torch.Tensor) or t.dtype not in kinds:
+                    raise ValueError(f"{name}[{i}] must be a tensor of fp32, fp16 or bf16")
+                self.device = _current_device(t, f"{name}[{i}]")
+                _addr_on(self.device, t, g.dtype, g.shape, f"{name}[{i}]")
+        ptrs = ctypes.c_void_p * n
+        h = ctypes.c_void_p()
+        _check(lib().moe_gradients_init(
+            n, ptrs(*[g.data_ptr() for g in grads]),
+            None if outs is None else ptrs(*[t.data_ptr() for t in outs]),
+            (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
+            (ctypes.c_int32 * n)(*[kinds[g.dtype] for g in grads]), _stream(stream),
+            ctypes.byref(h)))
+        self._h, self._keep = h, (grads, outs)
+
+    def _norm(self, norm):
+        return _addr_on(self.device, norm, _th().float32, (1,), "norm")
+
+    def norm(self, norm, stream=None):
+        """norm (fp32 [1]) = the norm of all of them."""
+        _check(lib().moe_gradients_norm(self._h, self._norm(norm),
+                                        _stream_on(self.device, stream)))
+
+    def scale(self, max_norm: float, norm, stream=None):
+        """outs = grads * min(1, max_norm / (norm + 1e-6)); not scaled where norm
+        (fp32 [1]) is not finite."""
+        _check(lib().moe_gradients_scale(self._h, max_norm, self._norm(norm),
+                                         _stream_on(self.device, stream)))
+
+    def clip(self, max_norm: float, norm, stream=None):
+        """norm() and scale() in one call."""
+        _check(lib().moe_gradients_clip(self._h, max_norm, self._norm(norm),
+                                        _stream_on(self.device, stream)))
+
+    def destroy(self):
+        if self._h is not None and self._h.value:
+            _check(lib().moe_gradients_destroy(self._h))
+        self._h = None
+        self._keep = None
+
+    def __del__(self):
+        try:
+            if getattr(self, "_h", None) is not None and self._h.value:
+                lib().moe_gradients_destroy(self._h)
+        except Exception:
+            pass
 
 
 class MoeRouter:

@@ -302,6 +302,35 @@ struct RouterUse {
 bool router_use(struct ::moe_router* r, RouterUse* out);
 bool router_hold(struct ::moe_router* r, int by);  // by: +1 or -1; false if not live
 
+// ---- products grouped by expert, MXFP4, gradients (grouped.hip, mx.hip,
+// mx_product.hip, gradients.hip) --------------------------------------------
+constexpr int kGroupedMaxRows = 1 << 21;
+constexpr int kMxBlock = 32;        // columns that share a scale
+
+enum { TYPE_F32 = 2 };
+
+// One grouped product: expert e has the next count[e] of the n rows (count
+// null: the one expert has them all).
+struct Grouped {
+  const int32_t* count;
+  int32_t type, n, d_in, d_out, E;
+};
+
+// One piece of a gradient tensor, at most kPieceElems elements.
+struct GradPiece {
+  const void* in;
+  void* out;
+  int32_t n, type;
+};
+constexpr int kPieceElems = 1 << 15;
+
+struct GradList {
+  const GradPiece* pieces;  // device
+  double* sums;             // one per piece
+  unsigned* done;           // pieces summed (zero between launches)
+  int32_t n;
+};
+
 // Static scratch of the allocation-free decode step (noalloc.hip): its size,
 // and its device address on `device` (looked up on the first call, which
 // must find `device` current; later calls return the kept address).
@@ -334,6 +363,19 @@ size_t layernorm_workspace(int T, int d);
 hipError_t launch_layernorm_backward(const void* dx, int type, const float* h, const float* gain,
                                      float eps, int T, int d, float* dh, bool accumulate,
                                      float* d_gain, float* d_bias, void* ws, hipStream_t s);
+hipError_t launch_grouped_product(const Grouped& g, const void* x, const void* w, void* y,
+                                  hipStream_t s);
+hipError_t launch_grouped_dx(const Grouped& g, const void* dy, const void* w, void* dx,
+                             hipStream_t s);
+hipError_t launch_grouped_dw(const Grouped& g, const void* dy, const void* x, float* dw,
+                             bool accumulate, hipStream_t s);
+hipError_t launch_mx_quantize(const void* v, int type, int64_t rows, int64_t cols, uint8_t* codes,
+                              uint8_t* scales, void* values, hipStream_t s);
+hipError_t launch_mx_product(const Grouped& g, const void* x, const uint8_t* xs,
+                             const uint8_t* w, const uint8_t* ws, void* y, hipStream_t s);
+hipError_t launch_gradients_norm(const GradList& g, float* norm, hipStream_t s);
+hipError_t launch_gradients_scale(const GradList& g, float max_norm, const float* norm,
+                                  hipStream_t s);
 hipError_t launch_decode_up(const ExpertEntry* table, const WorkList* wl,
                             const int32_t* perm, const f16* x, f16* h,
                             int T, int d, int f, int K, int max_groups,
