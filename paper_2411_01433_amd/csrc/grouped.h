@@ -1,7 +1,7 @@
 // Work items of a grouped product: which expert's rows a block takes.
 #pragma once
 
-#include "moe_internal.h"
+#include "tile.h"
 
 namespace moe {
 
@@ -33,14 +33,43 @@ __device__ inline int lanes_up_to(int v) {
 
 constexpr int kLaneExperts = kRouterMaxExperts / 64;  // most experts of a lane
 
-// Rows of expert e (all lanes of the wave take part and get them).
-__device__ inline Rows expert_rows(const Grouped& g, int e) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int i = lane; i < e; i += 64) before += count_of(g, i);
-  before = min(__builtin_amdgcn_readlane(lanes_up_to(before), 63), g.n);
-  return {before, __builtin_amdgcn_readfirstlane(min(count_of(g, e), g.n - before))};
-}
+// The counts of all experts in a wave's registers: a lane holds `per`
+// consecutive ones, cut at the call's rows, and the first row of its first.
+struct Counts {
+  int per, n[kLaneExperts], first;
+
+  __device__ inline void init(const Grouped& g) {
+    const int lane = threadIdx.x & 63;
+    per = (g.E + 63) >> 6;
+    int own = 0;
+#pragma unroll
+    for (int j = 0; j < kLaneExperts; ++j) {
+      const int e = lane * per + j;
+      n[j] = j < per && e < g.E ? count_of(g, e) : 0;
+      own += n[j];
+    }
+    first = min(lanes_up_to(own) - own, g.n);
+    int at = first;
+#pragma unroll
+    for (int j = 0; j < kLaneExperts; ++j) {
+      n[j] = min(n[j], g.n - at);
+      at += n[j];
+    }
+  }
+  // Rows of expert e (uniform).
+  __device__ inline Rows rows(int e) const {
+    const int lane = e / per, k = e - lane * per;
+    int at = first, own = n[0];
+#pragma unroll
+    for (int j = 1; j < kLaneExperts; ++j) {
+      if (j <= k) {
+        at += n[j - 1];
+        own = n[j];
+      }
+    }
+    return {__builtin_amdgcn_readlane(at, lane), __builtin_amdgcn_readlane(own, lane)};
+  }
+};
 
 // One row tile of an expert: rows [row, row + n) of the call.
 struct RowTile {
@@ -48,19 +77,10 @@ struct RowTile {
   int part;            // column tile
 };
 
-// Row tiles of at most M rows come in two runs over the experts: first the
-// full ones and the remainders of more than 3/4, which take the largest block,
-// then the smaller remainders, so that these fill the last round.  An item is
-// a row tile and one of `parts` column tiles; up to `super` row tiles of an
-// expert alternate fastest, so that the blocks that run together on a die
-// share the columns' operand and the rows'.
-template <int M>
-__device__ inline int big_tiles(int n) { return n / M + (n % M > 3 * M / 4); }
-
-// The block's item of the numbering above.  The hardware hands block b to die
-// b % 8: whole sets of 256 items (one per compute unit) go to the dies in runs
-// of 32, what is left in eighths.  false: no work.  One wave computes it; every
-// wave of a block gets the same.
+// The numbers of n items that a die takes, and the item at one of its places
+// (-1: none).  The hardware hands block b to die b % 8; whole sets of 256
+// items (one per compute unit) go to the dies in runs of 32, what is left in
+// eighths, so that every die gets the same mix.
 __device__ inline int die_slots(int n) { return (n >> 8) * 32 + (((n & 255) + 7) >> 3); }
 __device__ inline int die_item(int n, int die, int slot) {
   const int sets = n >> 8, left = n & 255, per = (left + 7) >> 3;
@@ -69,76 +89,119 @@ __device__ inline int die_item(int n, int die, int slot) {
   return q < per && item < left ? 256 * sets + item : -1;
 }
 
+// The row tiles of a call, at most M rows each.  They come in two runs over the
+// experts: first the full ones and the remainders of more than 3/4, which take
+// the largest block, then the smaller remainders, so that these fill the last
+// round.  An item is a row tile and one of `parts` column tiles; up to kSuper
+// row tiles of an expert alternate fastest, so that the blocks that run
+// together on a die share the columns' operand and the rows'.
 template <int M>
-__device__ inline bool take_row_tile(const Grouped& g, int parts, int super, RowTile& t) {
-  const int lane = threadIdx.x & 63;
-  // a lane holds `per` consecutive experts
-  const int per = (g.E + 63) >> 6;
-  int c[kLaneExperts], own = 0;
-#pragma unroll
-  for (int j = 0; j < kLaneExperts; ++j) {
-    const int e = lane * per + j;
-    c[j] = j < per && e < g.E ? count_of(g, e) : 0;
-    own += c[j];
-  }
-  const int before = lanes_up_to(own) - own;
-  int first = min(before, g.n), big = 0, rest = 0;
-  const int first0 = first;
-#pragma unroll
-  for (int j = 0; j < kLaneExperts; ++j) {
-    c[j] = min(c[j], g.n - first);
-    first += c[j];
-    const int b = big_tiles<M>(c[j]);
-    big += b;
-    rest += c[j] > b * M;
-  }
-  const int up_big = lanes_up_to(big), up_rest = lanes_up_to(rest);
-  const int n_big = __builtin_amdgcn_readlane(up_big, 63) * parts;
-  const int n_rest = __builtin_amdgcn_readlane(up_rest, 63) * parts;
-  const int slot = blockIdx.x >> 3, die = blockIdx.x & 7, slots_big = die_slots(n_big);
-  const bool small = slot >= slots_big;
-  const int item = small ? die_item(n_rest, die, slot - slots_big) : die_item(n_big, die, slot);
-  if (item < 0) return false;
-  const int up = small ? up_rest : up_big, mine = small ? rest : big;
-  const int at = __ffsll((unsigned long long)__ballot(up * parts > item)) - 1;
-  // that lane's expert: the others compute something in range and are not read
-  int in = item - (up - mine) * parts, row = first0, expert = lane * per, rows = 0, tiles = 1, found = 0;
-#pragma unroll
-  for (int j = 0; j < kLaneExperts; ++j) {
-    const int b = big_tiles<M>(c[j]);
-    const int k = small ? (c[j] > b * M) : b;
-    const bool here = !found && in < k * parts;
-    if (here) {
-      expert = lane * per + j;
-      rows = c[j];
-      tiles = k;
-      found = 1;
-    }
-    if (!found) {
-      in -= k * parts;
-      row += c[j];
-    }
-  }
-  in = __builtin_amdgcn_readlane(in, at);
-  row = __builtin_amdgcn_readlane(row, at);
-  rows = __builtin_amdgcn_readlane(rows, at);
-  tiles = __builtin_amdgcn_readlane(tiles, at);
-  t.expert = __builtin_amdgcn_readlane(expert, at);
-  const int sup = in / (super * parts), left = in - sup * (super * parts);
-  const int width = min(super, tiles - sup * super);
-  t.part = __builtin_amdgcn_readfirstlane(left / width);
-  const int k = sup * super + left - t.part * width;
-  const int r0 = small ? big_tiles<M>(rows) * M : k * M;
-  t.row = __builtin_amdgcn_readfirstlane(row + r0);
-  t.n = __builtin_amdgcn_readfirstlane(min(M, rows - r0));
-  return true;
-}
+struct RowTiles {
+  static constexpr int kSuper = 8;
+  int parts, n_big, n_rest, slots_big, slots;
+  Counts counts;
+  int big, rest, up_big, up_rest;  // of the lane's experts, and up to them
 
-// Blocks for any counts: a tile of the first run has more than 3/4 M rows, and
-// an expert at most one of the second.
-inline unsigned row_tile_blocks(const Grouped& g, int M, int parts) {
-  const int64_t tiles = g.n / (3 * M / 4 + 1) + (g.E < g.n ? g.E : g.n);
-  return (unsigned)((tiles * parts + 7) / 8 + 2) * 8;
+  static __device__ inline int big_of(int n) { return n / M + (n % M > 3 * M / 4); }
+  static __device__ inline int rest_of(int n) { return n > big_of(n) * M; }
+
+  // (all lanes of a wave, as get)
+  __device__ inline void init(const Grouped& g, int parts_) {
+    parts = parts_;
+    counts.init(g);
+    big = rest = 0;
+#pragma unroll
+    for (int j = 0; j < kLaneExperts; ++j) {
+      big += big_of(counts.n[j]);
+      rest += rest_of(counts.n[j]);
+    }
+    up_big = lanes_up_to(big);
+    up_rest = lanes_up_to(rest);
+    n_big = __builtin_amdgcn_readlane(up_big, 63) * parts;
+    n_rest = __builtin_amdgcn_readlane(up_rest, 63) * parts;
+    slots_big = die_slots(n_big);
+    slots = slots_big + die_slots(n_rest);
+  }
+
+  // The item of a die's place; false: none there.
+  __device__ inline bool get(int die, int slot, RowTile& t) const {
+    const int lane = threadIdx.x & 63;
+    const bool small = slot >= slots_big;
+    const int item = small ? die_item(n_rest, die, slot - slots_big) : die_item(n_big, die, slot);
+    if (item < 0) return false;
+    const int up = small ? up_rest : up_big, mine = small ? rest : big;
+    const int at = __ffsll((unsigned long long)__ballot(up * parts > item)) - 1;
+    // that lane's expert: what the others compute is not read
+    int in = item - (up - mine) * parts, row = counts.first, expert = lane * counts.per, rows = 0, tiles = 1;
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < kLaneExperts; ++j) {
+      const int k = (small ? rest_of(counts.n[j]) : big_of(counts.n[j])) * parts;
+      const bool here = !found && in < k;
+      if (here) {
+        expert = lane * counts.per + j;
+        rows = counts.n[j];
+        tiles = k;
+      }
+      found = found || here;
+      if (!found) {
+        in -= k;
+        row += counts.n[j];
+      }
+    }
+    in = __builtin_amdgcn_readlane(in, at);
+    row = __builtin_amdgcn_readlane(row, at);
+    rows = __builtin_amdgcn_readlane(rows, at);
+    tiles = __builtin_amdgcn_readlane(tiles, at) / parts;
+    t.expert = __builtin_amdgcn_readlane(expert, at);
+    const int sup = in / (kSuper * parts), left = in - sup * (kSuper * parts);
+    const int width = min(kSuper, tiles - sup * kSuper);
+    t.part = __builtin_amdgcn_readfirstlane(left / width);
+    const int k = sup * kSuper + left - t.part * width;
+    const int r0 = small ? big_of(rows) * M : k * M;
+    t.row = __builtin_amdgcn_readfirstlane(row + r0);
+    t.n = __builtin_amdgcn_readfirstlane(min(M, rows - r0));
+    return true;
+  }
+};
+
+template <int TYPE> struct Elem { typedef f16 T; };
+template <> struct Elem<tile::BF16> { typedef bf16 T; };
+
+// Blocks of 64 TA columns and up to 64 TA rows, with the LDS of one (TA 4) or
+// two (TA 2) blocks per unit, and as many blocks as the chip holds: each takes
+// one item after another.
+template <int TA> constexpr int kLds = TA == 4 ? 160 * 1024 : 80 * 1024;
+template <int TA> constexpr int kRows = 64 * TA;
+template <int TA> constexpr int kBlocks = TA == 4 ? 256 : 512;
+
+// A block's items: place after place of its die's.  A job of TB takes the tiles
+// whose rows fill TB of its 64s, and leaves off at the first other one.
+template <int TA>
+struct Items {
+  RowTiles<kRows<TA>> tiles;
+  int die, slot;
+  RowTile t;           // the first one not taken
+  bool any;
+
+  __device__ inline void init(const Grouped& g, int parts) {
+    tiles.init(g, parts);
+    die = blockIdx.x & 7;
+    slot = (int)(blockIdx.x >> 3) - kBlocks<TA> / 8;
+    step();
+  }
+  __device__ inline void step() {
+    any = false;
+    while (!any && (slot += kBlocks<TA> / 8) < tiles.slots) any = tiles.get(die, slot, t);
+  }
+  __device__ inline int size() const { return (t.n + 63) >> 6; }
+};
+
+// Whether blocks of 256 columns and rows are enough to fill the chip.
+inline bool large_blocks(const Grouped& g, int cols) {
+  const int active = g.E < g.n ? g.E : g.n;
+  const int tiles = g.n / 256 + active / 2;
+  return (int64_t)(tiles > active ? tiles : active) * ((cols + 255) / 256) >= 256;
 }
 
 }  // namespace moe

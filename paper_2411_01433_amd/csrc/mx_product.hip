@@ -1,82 +1,92 @@
 // Products grouped by expert with weights in MXFP4, and activations of 16 bits
-// or in MXFP4 too.
+// or in MXFP4 too, on the tiles of tile.h.
+//
+// With both in MXFP4 the matrix cores take codes and scales as they are.
+// With activations of 16 bits a code becomes an activation's type after it was
+// read from LDS (v_cvt_scalef32_pk: exact wherever the type holds the value).
 #include "grouped.h"
 
 namespace moe {
 
 namespace {
 
-constexpr int kTile = 64, kDepth = 32;
+using namespace tile;
 
-// (in 64 bits: 6 * 2^127 is beyond fp32, its product with a small partner is not)
-__device__ inline double mx_value(const uint8_t* row, const uint8_t* scales, int k) {
-  const uint32_t b = scales[k / 32];
-  const uint32_t c = row[k / 2] >> (4 * (k & 1)) & 15;
-  const uint32_t m = c & 7;
-  const float v = m < 2 ? 0.5f * m : (float)(2 + (m & 1)) * (float)(1 << (m >> 1)) * 0.25f;
-  const uint64_t s = b == 255 ? 0x7FF8ull << 48 : (uint64_t)(b + 896) << 52;
-  return (double)(c & 8 ? -v : v) * __builtin_bit_cast(double, s);
-}
+template <int TYPE, int TA, int TB, bool CODED>
+struct MxJob {
+  typedef RowTile Tile;
+  typedef typename Elem<TYPE>::T T;
+  const Grouped& g;
+  const uint8_t *x, *xs, *w, *ws;
+  T* y;
+  Items<TA>& items;
 
-template <class T, bool MX>
-__global__ __launch_bounds__(256) void mx_product_kernel(Grouped g, const void* x,
-                                                         const uint8_t* xs, const uint8_t* w,
-                                                         const uint8_t* ws, T* y) {
-  __shared__ double as[kDepth][kTile + 1], bs[kDepth][kTile + 1];
-  const Rows rows = expert_rows(g, blockIdx.z);
-  const int n0 = blockIdx.x * kTile;
-  const int64_t wb = (int64_t)blockIdx.z * g.d_out + n0;
-  for (int r0 = blockIdx.y * kTile; r0 < rows.n; r0 += gridDim.y * kTile) {
-    const int64_t xb = rows.first + r0;
-    float c[4][4] = {};
-    for (int k0 = 0; k0 < g.d_in; k0 += kDepth) {
-      for (int i = threadIdx.x; i < kTile * kDepth; i += 256) {
-        const int r = i / kDepth, k = i % kDepth;
-        double a = 0.0;
-        if (r0 + r < rows.n) {
-          if (MX)
-            a = mx_value(static_cast<const uint8_t*>(x) + (xb + r) * (g.d_in / 2),
-                         xs + (xb + r) * (g.d_in / 32), k0 + k);
-          else
-            a = (double)(float)static_cast<const T*>(x)[(xb + r) * g.d_in + k0 + k];
-        }
-        as[k][r] = a;
-        const double v = mx_value(w + (wb + r) * (g.d_in / 2), ws + (wb + r) * (g.d_in / 32), k0 + k);
-        bs[k][r] = MX ? v : (double)(float)(T)(float)v;
-      }
-      __syncthreads();
-      for (int k = 0; k < kDepth; ++k)
-        for (int i = 0; i < 4; ++i)
-          for (int j = 0; j < 4; ++j)
-            c[i][j] += (float)(as[k][(threadIdx.x >> 4) * 4 + i] * bs[k][(threadIdx.x & 15) * 4 + j]);
-      __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i)
-      for (int j = 0; j < 4; ++j) {
-        const int r = (threadIdx.x >> 4) * 4 + i, n = (threadIdx.x & 15) * 4 + j;
-        if (r0 + r < rows.n) y[(xb + r) * g.d_out + n0 + n] = (T)c[i][j];
-      }
+  __device__ inline bool next(Tile& t) {
+    if (!items.any || items.size() != TB) return false;
+    t = items.t;
+    items.step();
+    return true;
+  }
+  __device__ inline int steps(const Tile&) const { return g.d_in; }
+  __device__ inline int64_t column(const Tile& t) const { return (int64_t)t.expert * g.d_out + t.part * 64 * TA; }
+  __device__ inline Operand a(const Tile& t) const {
+    return {w + column(t) * (g.d_in / 2), (uint32_t)(g.d_in / 2), g.d_out - t.part * 64 * TA};
+  }
+  __device__ inline Operand b(const Tile& t) const {
+    const int bytes = CODED ? g.d_in / 2 : g.d_in * 2;
+    return {x + (int64_t)t.row * bytes, (uint32_t)bytes, t.n};
+  }
+  __device__ inline Scales a_scales(const Tile& t) const { return {ws + column(t) * (g.d_in / 32), g.d_in / 32}; }
+  __device__ inline Scales b_scales(const Tile& t) const { return {xs + (int64_t)t.row * (g.d_in / 32), g.d_in / 32}; }
+  __device__ inline void store(const Tile& t, Acc<TA, TB>& acc) const {
+    const int col = t.part * 64 * TA;
+    store_rows<T, TA, TB>(acc, y + (int64_t)t.row * g.d_out + col, g.d_out, t.n, g.d_out - col);
+  }
+};
+
+template <int TYPE, int TA, bool CODED>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(TA == 4 ? 1 : 2, TA == 4 ? 1 : 2)))
+void mx_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
+               void* y, int parts) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds<TA>];
+  lds_u8* lds = (lds_u8*)smem;
+  Items<TA> items;
+  items.init(g, parts);
+  auto take = [&](auto size) {
+    constexpr int TB = decltype(size)::value;
+    MxJob<TYPE, TA, TB, CODED> job = {g, x, xs, w, ws, (typename Elem<TYPE>::T*)y, items};
+    stream<CODED ? F4 : TYPE, CODED ? ROWS : CODES, ROWS, TA, TB, kLds<TA>>(job, lds);
+  };
+  while (items.any) {
+    const int n = items.size();
+    if (n == 1) take(std::integral_constant<int, 1>());
+    else if (n == 2) take(std::integral_constant<int, 2>());
+    else if (TA == 4 && n == 3) take(std::integral_constant<int, TA == 4 ? 3 : 1>());
+    else if (TA == 4) take(std::integral_constant<int, TA == 4 ? 4 : 1>());
   }
 }
 
-template <class T>
-void launch(const Grouped& g, const void* x, const uint8_t* xs, const uint8_t* w,
-            const uint8_t* ws, T* y, hipStream_t s) {
-  const dim3 grid(g.d_out / kTile, min((g.n + kTile - 1) / kTile, 256), g.E);
-  if (xs)
-    mx_product_kernel<T, true><<<grid, 256, 0, s>>>(g, x, xs, w, ws, y);
+template <int TYPE, bool CODED>
+void launch(const Grouped& g, const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
+            void* y, hipStream_t s) {
+  if (large_blocks(g, g.d_out))
+    mx_kernel<TYPE, 4, CODED><<<kBlocks<4>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 255) / 256);
   else
-    mx_product_kernel<T, false><<<grid, 256, 0, s>>>(g, x, xs, w, ws, y);
+    mx_kernel<TYPE, 2, CODED><<<kBlocks<2>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 127) / 128);
 }
 
 }  // namespace
 
 hipError_t launch_mx_product(const Grouped& g, const void* x, const uint8_t* xs,
                              const uint8_t* w, const uint8_t* ws, void* y, hipStream_t s) {
-  if (g.type == TYPE_F16)
-    launch(g, x, xs, w, ws, (f16*)y, s);
-  else
-    launch(g, x, xs, w, ws, (bf16*)y, s);
+  const uint8_t* xb = static_cast<const uint8_t*>(x);
+  if (g.type == TYPE_F16) {
+    if (xs) launch<F16, true>(g, xb, xs, w, ws, y, s);
+    else launch<F16, false>(g, xb, xs, w, ws, y, s);
+  } else {
+    if (xs) launch<BF16, true>(g, xb, xs, w, ws, y, s);
+    else launch<BF16, false>(g, xb, xs, w, ws, y, s);
+  }
   return hipGetLastError();
 }
 

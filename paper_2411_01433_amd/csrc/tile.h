@@ -15,11 +15,14 @@
 // takes 64 rows of 128 T bytes and is transposed by the fragment reads
 // (ds_read_b64_tr_b16: four elements of a column).  What lies outside of the
 // matrices - rows and columns past the ends, reduction steps past the last -
-// is masked by the buffer's range check and arrives as zeros.
+// is masked by the buffer's range check and arrives as zeros.  Codes beside a
+// partner of 16 bits (CODES) take 32 bytes of each row and become 16-bit
+// fragments after the read, each by two waves.
 //
 // Bank conflicts.  ROWS: the 16-byte chunk c of row r sits at position
 // c ^ (r / 2 % 8).  COLS: 64-byte pieces are permuted by the row's last bits,
 // so that the four rows that a half-wave reads 64 bytes of cover all banks.
+// CODES: a row's two chunks trade places in every second eight rows.
 //
 // Order of the reduction.  It is free as long as both operands agree: lane
 // half h takes steps 32 h + 8 s .. + 7 of the stage in step s = 0..3 (in MXFP4
@@ -96,56 +99,55 @@ struct Operand {
   int valid;
 };
 
-// An operand's loads: per lane the source of each of a wave's 2 T loads per
+// An operand's loads: per lane the source of each of a wave's kN loads per
 // stage, relative to the stage's base.  Load i of wave w fills 1024 bytes of
 // the slot from 1024 (w + 4 i) on.
 template <int KIND, int T>
 struct Loads {
-  static constexpr int kN = 2 * T;
-  static constexpr uint32_t kSlot = 8192 * T;
-  uint32_t off[KIND == CODES ? 1 : kN];
-  uint32_t chunk;       // ROWS, CODES: the lane's 16 bytes of each row's 128
+  static_assert(KIND != CODES || T % 2 == 0, "whole loads");
+  static constexpr int kN = KIND == CODES ? T / 2 : 2 * T;
+  static constexpr uint32_t kSlot = 4096 * kN;
+  uint32_t off[kN];
   const uint8_t* base;
   uint32_t row_bytes;
-  int row0, valid;      // CODES: the lane's row of load 0
+
+  // ROWS: the lane's 16 bytes of each row's 128 (of every load the same)
+  static __device__ inline uint32_t chunk(int wave) {
+    const int l = threadIdx.x & 63;
+    return 16 * ((l & 7) ^ ((4 * (wave & 1) + (l >> 4)) & 7));
+  }
+  // COLS: what row r's chunks are permuted by (64-byte pieces: bits 2 and up)
+  static __device__ inline int piece(int r) { return T % 2 ? (r & 2) << 1 : (r & 3) << 2; }
 
   __device__ inline void init(const Operand& o, int wave) {
     const int l = threadIdx.x & 63;
     base = uniform(o.base);
     row_bytes = o.row_bytes;
-    chunk = 16 * ((l & 7) ^ ((4 * (wave & 1) + (l >> 4)) & 7));
-    row0 = 8 * wave + (l >> 3);
-    valid = o.valid;
 #pragma unroll
-    for (int i = 0; i < (KIND == CODES ? 0 : kN); ++i) {
+    for (int i = 0; i < kN; ++i) {
       const int q = wave + 4 * i;
       if (KIND == COLS) {
-        const int at = 64 * q + l, row = at / (8 * T), pos = at % (8 * T);
-        const int c = pos ^ piece(row);
+        const int at = 64 * q + l, row = at / (8 * T), c = (at % (8 * T)) ^ piece(row);
         off[i] = 8 * c < o.valid ? (uint32_t)row * row_bytes + 16 * c : kMasked;
-      } else {
+      } else if (KIND == ROWS) {
         const int row = 8 * q + (l >> 3);
-        off[i] = row < valid ? (uint32_t)row * row_bytes + chunk : kMasked;
+        off[i] = row < o.valid ? (uint32_t)row * row_bytes + chunk(wave) : kMasked;
+      } else {
+        const int row = 32 * q + (l >> 1), c = (l & 1) ^ ((row >> 3) & 1);
+        off[i] = row < o.valid ? (uint32_t)row * row_bytes + 16 * c : kMasked;
       }
     }
   }
-  // (a unit's loads are spread over four stages: their number is not known
-  // where they are issued)
-  __device__ inline uint32_t source(int i) const {
-    if constexpr (KIND != CODES) return off[i];
-    const int row = row0 + 32 * i;
-    return row < valid ? (uint32_t)row * row_bytes + chunk : kMasked;
-  }
-  // COLS: what row r's chunks are permuted by (64-byte pieces: bits 2 and up)
-  static __device__ inline int piece(int r) { return T % 2 ? (r & 2) << 1 : (r & 3) << 2; }
 
-  // stage k of `steps` reduction steps in all (ROWS, CODES: bytes of a row)
-  __device__ inline void load(int k, int steps, int i, uint32_t lds, uint32_t tail) const {
+  // load i of stage k of `steps` reduction steps (ROWS, CODES: of `steps`
+  // bytes of a row) in all
+  __device__ inline void load(int k, int steps, int i, uint32_t lds, uint32_t mask) const {
     if (KIND == COLS) {
       const int left = __builtin_amdgcn_readfirstlane(max(0, min(steps - kStage * k, kStage)));
-      load_lds(lds, base + (int64_t)k * kStage * row_bytes, (uint32_t)left * row_bytes, source(i));
+      load_lds(lds, base + (int64_t)k * kStage * row_bytes, (uint32_t)left * row_bytes, off[i]);
     } else {
-      load_lds(lds, base + (int64_t)k * 128, 128 * k < steps ? kMasked - 1 : 0, source(i) | tail);
+      constexpr int kBytes = KIND == CODES ? 32 : 128;
+      load_lds(lds, base + (int64_t)k * kBytes, kBytes * k < steps ? kMasked - 1 : 0, off[i] | mask);
     }
   }
 };
@@ -177,24 +179,26 @@ __device__ inline float scale_of(uint32_t byte) {
   return __builtin_bit_cast(float, max(byte << 23, 0x00400000u));
 }
 
-// LDS of a tile: rings of SA and SB slots (a slot of CODES holds 4 stages),
-// then two slots of scales, 8 bytes per row.
+// LDS of a tile: rings of SA and SB slots, then two slots of scales (F4: 8
+// bytes per row and stage, CODES: 2).
 template <int TYPE, int KA, int KB, int TA, int TB, int LDS>
 struct Ring {
   static constexpr bool kScales = TYPE == F4 || KA == CODES;
-  static constexpr uint32_t kA = 8192 * TA, kB = 8192 * TB;
-  static constexpr uint32_t kScaleSlot = kScales ? 512 * (TA + (TYPE == F4 ? TB : 0)) : 0;
+  static constexpr uint32_t kA = Loads<KA, TA>::kSlot, kB = Loads<KB, TB>::kSlot;
+  static constexpr uint32_t kScaleSlot = TYPE == F4 ? 512 * (TA + TB) : KA == CODES ? 128 * TA : 0;
   static constexpr uint32_t kRoom = LDS - 2 * kScaleSlot;
   static constexpr int kBoth = (int)(kRoom / (kA + kB));
   // with scales, whose loads the compiler waits for, no load is left in
   // flight at a barrier, and deeper rings would be waited for in vain
-  static constexpr int SB = kScales ? 2 : kBoth > 8 ? 8 : kBoth;
+  static constexpr int SB = kScales ? 2 : kBoth > 4 ? 4 : kBoth;
   static constexpr int SA = kScales ? 2 : SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
   static constexpr uint32_t kBBase = SA * kA, kScaleBase = kBBase + SB * kB;
   static_assert(SB >= 2 && kScaleBase + 2 * kScaleSlot <= LDS, "LDS");
+  // stages ahead of the products that anything is fetched for
+  static constexpr int kAhead = kScales ? 2 : SA - 1;
   // loads that may be in flight when a stage ends: those of the stages after
   // the next one
-  static constexpr int kPending = (SA - 2) * 2 * TA + (SB - 2) * 2 * TB;
+  static constexpr int kPending = (SA - 2) * Loads<KA, TA>::kN + (SB - 2) * Loads<KB, TB>::kN;
 };
 
 // The accumulators of a wave: acc[i][j] is A tile i, B tile j of its own.
@@ -206,95 +210,161 @@ struct Scales {
   int bytes;
 };
 
-// acc = the tile's product over `steps` reduction steps (F4: columns).
-template <int TYPE, int KA, int KB, int TA, int TB, int LDS>
-__device__ __forceinline__ void product(const Operand& oa, const Operand& ob, int steps, lds_u8* lds,
-                                        Acc<TA, TB>& acc, Scales as = {nullptr, 0},
-                                        Scales bs = {nullptr, 0}) {
+// The products of a sequence of tiles, one after another through the same
+// rings: the loads of a tile's first stages are in flight while the products
+// of the last one's end and its results are stored.  Job:
+//   struct Tile          uniform, trivially copied
+//   bool next(Tile&)     the tile after the last one given; false: none (again
+//                        and again, once it was)
+//   int steps(Tile)      reduction steps (F4: columns)
+//   Operand a(Tile), b(Tile);  Scales a_scales(Tile), b_scales(Tile)
+//   void store(Tile, Acc&)
+template <int TYPE, int KA, int KB, int TA, int TB, int LDS, class Job>
+__device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   using R = Ring<TYPE, KA, KB, TA, TB, LDS>;
+  typedef typename Job::Tile Tile;
   constexpr bool kF4 = TYPE == F4, kCodes = KA == CODES;
+  constexpr int kNA = Loads<KA, TA>::kN, kNB = Loads<KB, TB>::kN;
   const int l = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = wave >> 1, wb = wave & 1;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  // stages; bytes of a row where it is the reduction
-  const int nst = kF4 ? (steps + 255) / 256 : (steps + kStage - 1) / kStage;
-  const int a_steps = KA == COLS ? steps : kF4 || kCodes ? steps / 2 : steps * 2;
-  const int b_steps = KB == COLS ? steps : kF4 ? steps / 2 : steps * 2;
+
+  // The tiles to come: eight words each in the lanes of one register, tile i in
+  // lanes 8 (i % 8) and up: its stages (0: behind the last tile; a tile without
+  // reduction steps takes one stage of zeros), its steps, and what the job says.
+  constexpr int kWords = sizeof(Tile) / 4;
+  static_assert(kWords <= 6, "a tile's words");
+  int queue = 0, made = 0;
+  auto put = [&](int lane, int v) { queue = l == lane ? v : queue; };
+  auto make = [&]() {
+    Tile tile;
+    const int at = 8 * (made++ & 7);
+    int n = 0, steps = 0;  // (behind the last tile no load reads anything)
+    if (job.next(tile)) {
+      steps = job.steps(tile);
+      n = max(1, kF4 ? (steps + 255) / 256 : (steps + kStage - 1) / kStage);
+      int w[kWords];
+      __builtin_memcpy(w, &tile, sizeof(Tile));
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) put(at + 2 + i, w[i]);
+    }
+    put(at, n);
+    put(at + 1, steps);
+  };
+  auto tile_of = [&](int i) {
+    Tile tile;
+    int w[kWords];
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) w[j] = __builtin_amdgcn_readlane(queue, 8 * (i & 7) + 2 + j);
+    __builtin_memcpy(&tile, w, sizeof(Tile));
+    return tile;
+  };
+  // A stage: stage k of n of tile i.  p[j] is the one j stages after that of the
+  // products.
+  struct Stage {
+    int i, k, n, steps;
+  };
+  auto begin = [&](int i) -> Stage {
+    return {i, 0, __builtin_amdgcn_readlane(queue, 8 * (i & 7)),
+            __builtin_amdgcn_readlane(queue, 8 * (i & 7) + 1)};
+  };
+  // (tile i + 1 is there, or tile i is the end, which stays)
+  auto after = [&](const Stage& q) {
+    Stage x = q;
+    if (++x.k >= x.n) x = begin(q.n ? q.i + 1 : q.i);
+    return x;
+  };
+  Stage p[R::kAhead + 1];
+#pragma unroll 1
+  for (int i = 0; i < R::kAhead + 2; ++i) make();
+  p[0] = begin(0);
+  if (p[0].n == 0) return;
+#pragma unroll
+  for (int j = 0; j < R::kAhead; ++j) p[j + 1] = after(p[j]);
 
   Loads<KA, TA> la;
   Loads<KB, TB> lb;
-  la.init(oa, wave);
-  lb.init(ob, wave);
-  // In MXFP4 a row's last line may be partial: its missing chunks are masked
-  // (both operands' chunks are the same).
-  auto tail = [&](int k, int bytes) -> uint32_t {
-    return (uint32_t)(128 * k) + la.chunk < (uint32_t)bytes ? 0 : kMasked;
+  auto open_a = [&](const Stage& q) {
+    if (q.k == 0 && q.n) la.init(job.a(tile_of(q.i)), wave);
   };
-  auto load_a = [&](int k, int i, uint32_t slot) {
-    la.load(k, a_steps, i, lds0 + slot * R::kA + (wave + 4 * i) * 1024,
-            kF4 || kCodes ? tail(k, a_steps) : 0);
+  auto open_b = [&](const Stage& q) {
+    if (q.k == 0 && q.n) lb.init(job.b(tile_of(q.i)), wave);
   };
-  auto load_b = [&](int k, int i, uint32_t slot) {
-    lb.load(k, b_steps, i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024,
-            kF4 ? tail(k, b_steps) : 0);
+  // (behind the last stage no step is left, and the loads read nothing)
+  auto load_a = [&](const Stage& q, int i, uint32_t slot) {
+    const int steps = KA == COLS ? q.steps : kF4 || kCodes ? q.steps / 2 : q.steps * 2;
+    // In MXFP4 a row's last line may be partial.
+    const uint32_t mask = kF4 && (uint32_t)(128 * q.k) + la.chunk(wave) >= (uint32_t)steps ? kMasked : 0;
+    la.load(q.k, steps, i, lds0 + slot * R::kA + (wave + 4 * i) * 1024, mask);
+  };
+  auto load_b = [&](const Stage& q, int i, uint32_t slot) {
+    const int steps = KB == COLS ? q.steps : kF4 ? q.steps / 2 : q.steps * 2;
+    const uint32_t mask = kF4 && (uint32_t)(128 * q.k) + lb.chunk(wave) >= (uint32_t)steps ? kMasked : 0;
+    lb.load(q.k, steps, i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
   };
 
-  // Scales of 256 columns (8 bytes) of the thread's row of A, and in F4 of B:
-  // from memory to registers, a unit later to LDS.  Past the row: 2^0.
+  // Scales of 256 columns (8 bytes) of the thread's row of A, and in F4 of B,
+  // into registers; a stage later to LDS.  Past the row: 2^0.
   const int t = threadIdx.x;
   auto fetch = [&](const Scales& s, int row, int u) -> uint64_t {
-    const uint8_t* p = s.at + (int64_t)row * s.bytes + 8 * u;
+    const uint8_t* at = s.at + (int64_t)row * s.bytes + 8 * u;
     uint64_t v = 0x7F7F7F7F7F7F7F7Full;
     if (8 * u + 8 <= s.bytes) {
-      __builtin_memcpy(&v, p, 8);
+      __builtin_memcpy(&v, at, 8);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (8 * u + 2 * i < s.bytes) {
           uint16_t w;
-          __builtin_memcpy(&w, p + 2 * i, 2);
+          __builtin_memcpy(&w, at + 2 * i, 2);
           v = (v & ~(0xFFFFull << (16 * i))) | (uint64_t)w << (16 * i);
         }
     }
     return v;
   };
-  uint64_t sa_next = 0, sb_next = 0;
-  auto fetch_scales = [&](int u) {
-    if constexpr (R::kScales) {
-      if (t < 64 * TA) sa_next = fetch(as, min(t, oa.valid - 1), u);
-      if (kF4 && t < 64 * TB) sb_next = fetch(bs, min(t, ob.valid - 1), u);
+  uint64_t sa_next = 0, sb_next = 0, sa_unit = 0;
+  auto fetch_scales = [&](const Stage& q) {
+    if constexpr (kF4) {
+      if (q.n) {
+        const Tile x = tile_of(q.i);
+        if (t < 64 * TA) sa_next = fetch(job.a_scales(x), min(t, job.a(x).valid - 1), q.k);
+        if (t < 64 * TB) sb_next = fetch(job.b_scales(x), min(t, job.b(x).valid - 1), q.k);
+      }
+    } else if constexpr (kCodes) {
+      if (q.n && (q.k & 3) == 0) {
+        const Tile x = tile_of(q.i);
+        if (t < 64 * TA) sa_next = fetch(job.a_scales(x), min(t, job.a(x).valid - 1), q.k >> 2);
+      }
     }
   };
-  auto put_scales = [&](int u) {
-    if constexpr (R::kScales) {
-      const uint32_t at = R::kScaleBase + (u & 1) * R::kScaleSlot;
+  auto put_scales = [&](const Stage& q, uint32_t slot) {
+    const uint32_t at = R::kScaleBase + slot * R::kScaleSlot;
+    if constexpr (kF4) {
       if (t < 64 * TA) lds_write(lds, at + 8 * t, sa_next);
-      if (kF4 && t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
+      if (t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
+    } else if constexpr (kCodes) {
+      if ((q.k & 3) == 0) sa_unit = sa_next;
+      if (t < 64 * TA) lds_write(lds, at + 2 * t, (uint16_t)(sa_unit >> (16 * (q.k & 3))));
     }
   };
 
-  fetch_scales(0);
-  put_scales(0);
-  fetch_scales(1);
+  fetch_scales(p[0]);
+  put_scales(p[0], 0);
+  if (R::kScales) fetch_scales(p[1]);
   // the rings' first stages; what the first stage needs comes first
 #pragma unroll
-  for (int v = 0; v < (R::SA > R::SB ? R::SA : R::SB) - 1; ++v) {
+  for (int v = 0; v < R::SA - 1; ++v) {
     if (v < R::SB - 1) {
+      open_b(p[v]);
 #pragma unroll
-      for (int i = 0; i < 2 * TB; ++i) load_b(v, i, v);
+      for (int i = 0; i < kNB; ++i) load_b(p[v], i, v);
     }
-    if (v < R::SA - 1) {
+    open_a(p[v]);
 #pragma unroll
-      for (int i = 0; i < 2 * TA; ++i) load_a(v, i, v);
-    }
+    for (int i = 0; i < kNA; ++i) load_a(p[v], i, v);
   }
-#pragma unroll
-  for (int i = 0; i < TA; ++i)
-#pragma unroll
-    for (int j = 0; j < TB; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+  Acc<TA, TB> acc;
 
   // where the lane's fragments lie in a slot
   const int half = l >> 5, sw = (l >> 1) & 7;
@@ -303,7 +373,7 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   for (int s = 0; s < 4; ++s) cat[s] = 16 * ((4 * half + s) ^ sw);
   const uint32_t arow = (uint32_t)(wa * TA * 32 + (l & 31)) * 128;
   const uint32_t brow = (uint32_t)(wb * TB * 32 + (l & 31)) * 128;
-  // COLS: the lane's row within a step's four, and its 8 bytes of tile i
+  // COLS: the lane's row within a step's four, and its 8 bytes of a tile
   const int cr = (l & 15) >> 2;
   auto col_at = [&](int T, int tile_) -> uint32_t {
     const int x = T % 2 ? cr >> 1 : cr;
@@ -319,12 +389,12 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   float scale[kCodes ? TA : 1];
   uint32_t sa[kF4 ? TA : 1], sb[kF4 ? TB : 1], sa1[kF4 ? TA : 1], sb1[kF4 ? TB : 1];
   auto transposed = [&](uint32_t at, uint32_t four_rows) -> u32x4 {
-    const auto p = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at);
-    const auto q = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at + four_rows);
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q);
-    const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
-    return u32x4{x.x, x.y, y.x, y.y};
+    const auto x = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at);
+    const auto y = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at + four_rows);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(x);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(y);
+    const u32x2 u = __builtin_bit_cast(u32x2, lo), w = __builtin_bit_cast(u32x2, hi);
+    return u32x4{u.x, u.y, w.x, w.y};
   };
   auto read_a = [&](int s, int i, uint32_t slot) {
     const uint32_t at = slot * R::kA;
@@ -337,17 +407,16 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     if constexpr (KB == COLS) b[s & 1][j] = transposed(at + bcol[j] + s * 1024 * TB, 512 * TB);
     else b[s & 1][j] = lds_read<u32x4>(lds, at + brow + j * 4096 + cat[s]);
   };
-  // CODES: the lane's 32 codes of stage k and their scale
-  auto read_raw = [&](int k, int i, uint32_t slot) {
+  // CODES: the lane's 32 codes of a stage and their scale
+  auto read_raw = [&](int i, uint32_t slot, uint32_t scales) {
     if constexpr (kCodes) {
-      raw[i] = lds_read<u32x4>(lds, slot * R::kA + arow + i * 4096 + 16 * ((2 * (k & 3) + half) ^ sw));
-      const uint32_t at = R::kScaleBase + ((k >> 2) & 1) * R::kScaleSlot + (arow >> 4) + i * 256;
-      scale[i] = scale_of(lds_read<uint8_t>(lds, at + 2 * (k & 3) + half));
+      raw[i] = lds_read<u32x4>(lds, slot * R::kA + (arow >> 2) + i * 1024 + 16 * (half ^ ((l >> 3) & 1)));
+      scale[i] = scale_of(lds_read<uint8_t>(lds, R::kScaleBase + scales * R::kScaleSlot + (arow >> 6) + i * 64 + half));
     }
   };
-  auto read_scales = [&](int k, uint32_t (&x)[kF4 ? TA : 1], uint32_t (&y)[kF4 ? TB : 1]) {
+  auto read_scales = [&](uint32_t slot, uint32_t (&x)[kF4 ? TA : 1], uint32_t (&y)[kF4 ? TB : 1]) {
     if constexpr (kF4) {
-      const uint32_t at = R::kScaleBase + (k & 1) * R::kScaleSlot + 4 * half;
+      const uint32_t at = R::kScaleBase + slot * R::kScaleSlot + 4 * half;
 #pragma unroll
       for (int i = 0; i < TA; ++i) x[i] = lds_read<uint32_t>(lds, at + (arow >> 4) + i * 256);
 #pragma unroll
@@ -365,9 +434,9 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
     } else if constexpr (TYPE == BF16) {
       c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
     } else {
-      const i32x8 p = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
-      const i32x8 q = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
-      c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(p, q, c, 4, 4, s, (int)sa[m % TA], s, (int)sb[m / TA]);
+      const i32x8 u = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
+      const i32x8 w = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
+      c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(u, w, c, 4, 4, s, (int)sa[m % TA], s, (int)sb[m / TA]);
     }
   };
   auto products = [&](auto sc, int c) {
@@ -386,43 +455,34 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   };
 
   auto next = [](uint32_t slot, int slots) { return slot + 1 == (uint32_t)slots ? 0u : slot + 1; };
-  uint32_t ac = 0, bc = 0;                          // slots of stage k (CODES: of its unit)
+  uint32_t ac = 0, bc = 0, sc = 0;                  // slots of the products' stage
   uint32_t al = R::SA - 1, bl = R::SB - 1;          // slots loaded next
-  // Quarter c's share (of 16) of the loads issued between the barrier before
-  // stage k and the one in it: B's first, whose ring is never the deeper one.
-  // CODES: a quarter of a unit's per stage.
-  static_assert(!kCodes || TA % 2 == 0, "whole loads per stage");
-  constexpr int kAStage = kCodes ? TA / 2 : 2 * TA;
-  constexpr int kAll = 2 * TB + kAStage;
-  constexpr int kSpread = 12;
-  auto loads = [&](int k, int c) {
+  // Quarter c's share (of 16) of the loads issued between two barriers: B's
+  // first, whose ring is never the deeper one.
+  constexpr int kAll = kNB + kNA, kSpread = 12;
+  auto loads = [&](int c) {
 #pragma unroll
     for (int i = c * kAll / kSpread; i < min((c + 1) * kAll / kSpread, kAll); ++i) {
-      if (i < 2 * TB) {
-        load_b(k + R::SB - 1, i, bl);
-      } else if constexpr (kCodes) {
-        load_a((k >> 2) + 1, (k & 3) * kAStage + i - 2 * TB, al);
-      } else {
-        load_a(k + R::SA - 1, i - 2 * TB, al);
-      }
+      if (i < kNB) load_b(p[R::SB - 1], i, bl);
+      else load_a(p[R::SA - 1], i - kNB, al);
     }
   };
   constexpr std::integral_constant<int, 0> s0;
   constexpr std::integral_constant<int, 1> s1;
   constexpr std::integral_constant<int, 2> s2;
   constexpr std::integral_constant<int, 3> s3;
-  auto step = [&](auto sc, int k) {
-    constexpr int s = decltype(sc)::value;
+  auto step = [&](auto st) {
+    constexpr int s = decltype(st)::value;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      loads(k, 4 + 4 * s + c);
+      loads(4 + 4 * s + c);
 #pragma unroll
       for (int i = 0; i < TA; ++i)
         if (3 * i / TA == c) read_a(s + 1, i, ac);
 #pragma unroll
       for (int j = 0; j < TB; ++j)
         if (3 * j / TB == c) read_b(s + 1, j, bc);
-      products(sc, c);
+      products(st, c);
       pin(c);
     }
   };
@@ -431,67 +491,93 @@ __device__ __forceinline__ void product(const Operand& oa, const Operand& ob, in
   read_scales(0, sa, sb);
 #pragma unroll
   for (int i = 0; i < TA; ++i) {
-    read_raw(0, i, 0);
+    read_raw(i, 0, 0);
     read_a(0, i, 0);
   }
 #pragma unroll
   for (int j = 0; j < TB; ++j) read_b(0, j, 0);
-  // scales one unit ahead: into LDS, whose slot the last barrier freed, and
-  // the unit after it into registers
-  auto scales_ahead = [&](int k) {
-    if constexpr (kF4) {
-      put_scales(k + 1);
-      fetch_scales(k + 2);
-    } else if constexpr (kCodes) {
-      if ((k & 3) == 0) {
-        put_scales((k >> 2) + 1);
-        fetch_scales((k >> 2) + 2);
-      }
-    }
-  };
-  scales_ahead(0);
+  if (R::kScales) {
+    put_scales(p[1], 1);
+    fetch_scales(p[2 < R::kAhead ? 2 : R::kAhead]);
+  }
+  open_b(p[R::SB - 1]);
+  open_a(p[R::SA - 1]);
 #pragma unroll
-  for (int c = 0; c < 4; ++c) loads(0, c);
-  for (int k = 0; k < nst; ++k) {
-    step(s0, k);
-    step(s1, k);
-    step(s2, k);
-    // every load of stage k + 1 has arrived; the slots of stage k are free
-    stage_barrier<R::kPending>();
-    if (!kCodes || (k & 3) == 3) {
-      ac = next(ac, R::SA);
-      al = next(al, R::SA);
-    }
-    bc = next(bc, R::SB);
-    bl = next(bl, R::SB);
-    scales_ahead(k + 1);
-    read_scales(k + 1, sa1, sb1);
-    // (after the last stage: reads that are not multiplied)
+  for (int c = 0; c < 4; ++c) loads(c);
+  while (p[0].n) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      loads(k + 1, c);
-      if (c == 0) {
-#pragma unroll
-        for (int i = 0; i < TA; ++i) read_raw(k + 1, i, ac);
-      }
-#pragma unroll
-      for (int i = 0; i < TA; ++i)
-        if (kCodes ? 1 + i * 3 / TA == c : 3 * i / TA == c) read_a(0, i, ac);
+    for (int i = 0; i < TA; ++i)
 #pragma unroll
       for (int j = 0; j < TB; ++j)
-        if (3 * j / TB == c) read_b(0, j, bc);
-      products(s3, c);
-      pin(c);
-    }
-    if constexpr (kF4) {
 #pragma unroll
-      for (int i = 0; i < TA; ++i) sa[i] = sa1[i];
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    const int done = p[0].i;
+    int left = p[0].n;
+    do {
+      step(s0);
+      step(s1);
+      step(s2);
+      // every load of the next stage has arrived; this stage's slots are free
+      stage_barrier<R::kPending>();
+      ac = next(ac, R::SA);
+      al = next(al, R::SA);
+      bc = next(bc, R::SB);
+      bl = next(bl, R::SB);
+      sc ^= 1;
 #pragma unroll
-      for (int j = 0; j < TB; ++j) sb[j] = sb1[j];
-    }
+      for (int j = 0; j < R::kAhead; ++j) p[j] = p[j + 1];
+      p[R::kAhead] = after(p[R::kAhead]);
+      // (a new tile was taken: the one after it has to be there in turn; the
+      // tile being finished is kAhead + 1 tiles behind at most)
+      if (p[R::kAhead].k == 0 && p[R::kAhead].n && made <= p[R::kAhead].i + 1) make();
+      // scales of the stage after the next into LDS, whose slot the barrier
+      // freed, those of the one behind it into registers
+      if (R::kScales) {
+        put_scales(p[1], sc ^ 1);
+        fetch_scales(p[R::kAhead]);
+      }
+      open_b(p[R::SB - 1]);
+      open_a(p[R::SA - 1]);
+      read_scales(sc, sa1, sb1);
+      // (after the last stage of all: reads that are not multiplied)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        loads(c);
+        if (c == 0) {
+#pragma unroll
+          for (int i = 0; i < TA; ++i) read_raw(i, ac, sc);
+        }
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+          if (kCodes ? 1 + i * 3 / TA == c : 3 * i / TA == c) read_a(0, i, ac);
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+          if (3 * j / TB == c) read_b(0, j, bc);
+        products(s3, c);
+        pin(c);
+      }
+      if constexpr (kF4) {
+#pragma unroll
+        for (int i = 0; i < TA; ++i) sa[i] = sa1[i];
+#pragma unroll
+        for (int j = 0; j < TB; ++j) sb[j] = sb1[j];
+      }
+    } while (--left);
+    job.store(tile_of(done), acc);
   }
-  // the LDS must not be handed on with loads in flight
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // the LDS must not be handed on with loads in flight, nor while another wave
+  // reads it
+  stage_barrier<0>();
+}
+
+// A tile stays in the accumulation registers until it is stored: all of them
+// copied at once would not fit the others.  (The host's pass knows no such
+// registers.)
+template <int TILES>
+__device__ inline void keep(f32x16& c) {
+#ifdef __HIP_DEVICE_COMPILE__
+  if constexpr (TILES > 8) asm volatile("" : "+a"(c));
+#endif
 }
 
 // Stores a wave's tiles as 16-bit rows: C's b is the row, a the column, whose
@@ -508,9 +594,7 @@ __device__ __forceinline__ void store_rows(Acc<TA, TB>& acc, T* out, int64_t ld,
 #pragma unroll
     for (int i = 0; i < TA; ++i) {
       if (a0 + 32 * i >= cols) continue;
-      // (a tile stays where the products left it until it is converted: all of
-      // them copied at once would not fit the other registers)
-      if constexpr (TA * TB > 8) asm volatile("" : "+v"(acc[i][j]));
+      keep<TA * TB>(acc[i][j]);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         uint32_t v[4];
