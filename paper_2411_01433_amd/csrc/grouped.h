@@ -165,6 +165,13 @@ struct RowTiles {
   }
 };
 
+// Blocks of one item each that any counts can fill: a tile of the first run has
+// more than 3/4 M rows, and an expert at most one of the second.
+inline unsigned row_tile_blocks(const Grouped& g, int M, int parts) {
+  const int64_t tiles = g.n / (3 * M / 4 + 1) + (g.E < g.n ? g.E : g.n);
+  return (unsigned)((tiles * parts + 7) / 8 + 2) * 8;
+}
+
 template <int TYPE> struct Elem { typedef f16 T; };
 template <> struct Elem<tile::BF16> { typedef bf16 T; };
 

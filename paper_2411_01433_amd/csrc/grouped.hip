@@ -6,7 +6,7 @@
 //
 // All three on the tiles of tile.h; the operand whose index is contiguous in
 // the output is A.
-#include "grouped.h"
+#include "few_rows.h"
 
 namespace moe {
 
@@ -204,8 +204,13 @@ void launch_dw(const Grouped& g, const void* dy, const void* x, float* dw, bool 
 
 hipError_t launch_grouped_product(const Grouped& g, const void* x, const void* w, void* y,
                                   hipStream_t s) {
-  if (g.type == TYPE_F16) launch_rows<F16, false>(g, x, w, y, s);
-  else launch_rows<BF16, false>(g, x, w, y, s);
+  if (few::takes(g)) {
+    if (g.type == TYPE_F16) few::launch<F16, false, false>(g, x, nullptr, w, nullptr, y, s);
+    else few::launch<BF16, false, false>(g, x, nullptr, w, nullptr, y, s);
+  } else {
+    if (g.type == TYPE_F16) launch_rows<F16, false>(g, x, w, y, s);
+    else launch_rows<BF16, false>(g, x, w, y, s);
+  }
   return hipGetLastError();
 }
 

@@ -4,7 +4,7 @@
 // With both in MXFP4 the matrix cores take codes and scales as they are.
 // With activations of 16 bits a code becomes an activation's type after it was
 // read from LDS (v_cvt_scalef32_pk: exact wherever the type holds the value).
-#include "grouped.h"
+#include "few_rows.h"
 
 namespace moe {
 
@@ -80,7 +80,15 @@ void launch(const Grouped& g, const uint8_t* x, const uint8_t* xs, const uint8_t
 hipError_t launch_mx_product(const Grouped& g, const void* x, const uint8_t* xs,
                              const uint8_t* w, const uint8_t* ws, void* y, hipStream_t s) {
   const uint8_t* xb = static_cast<const uint8_t*>(x);
-  if (g.type == TYPE_F16) {
+  if (few::takes(g)) {
+    if (g.type == TYPE_F16) {
+      if (xs) few::launch<F16, true, true>(g, x, xs, w, ws, y, s);
+      else few::launch<F16, true, false>(g, x, xs, w, ws, y, s);
+    } else {
+      if (xs) few::launch<BF16, true, true>(g, x, xs, w, ws, y, s);
+      else few::launch<BF16, true, false>(g, x, xs, w, ws, y, s);
+    }
+  } else if (g.type == TYPE_F16) {
     if (xs) launch<F16, true>(g, xb, xs, w, ws, y, s);
     else launch<F16, false>(g, xb, xs, w, ws, y, s);
   } else {

@@ -179,6 +179,25 @@ __device__ inline float scale_of(uint32_t byte) {
   return __builtin_bit_cast(float, max(byte << 23, 0x00400000u));
 }
 
+// Scale bytes 8 u .. 8 u + 7 of a row of `bytes` (256 columns of it; the row
+// lies on an even address); those past the row: 2^0.
+__device__ inline uint64_t scale_unit(const uint8_t* row, int bytes, int u) {
+  const uint8_t* at = row + 8 * u;
+  uint64_t v = 0x7F7F7F7F7F7F7F7Full;
+  if (8 * u + 8 <= bytes) {
+    __builtin_memcpy(&v, at, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (8 * u + 2 * i < bytes) {
+        uint16_t w;
+        __builtin_memcpy(&w, at + 2 * i, 2);
+        v = (v & ~(0xFFFFull << (16 * i))) | (uint64_t)w << (16 * i);
+      }
+  }
+  return v;
+}
+
 // LDS of a tile: rings of SA and SB slots, then two slots of scales (F4: 8
 // bytes per row and stage, CODES: 2).
 template <int TYPE, int KA, int KB, int TA, int TB, int LDS>
@@ -305,23 +324,10 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   };
 
   // Scales of 256 columns (8 bytes) of the thread's row of A, and in F4 of B,
-  // into registers; a stage later to LDS.  Past the row: 2^0.
+  // into registers; a stage later to LDS.
   const int t = threadIdx.x;
-  auto fetch = [&](const Scales& s, int row, int u) -> uint64_t {
-    const uint8_t* at = s.at + (int64_t)row * s.bytes + 8 * u;
-    uint64_t v = 0x7F7F7F7F7F7F7F7Full;
-    if (8 * u + 8 <= s.bytes) {
-      __builtin_memcpy(&v, at, 8);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (8 * u + 2 * i < s.bytes) {
-          uint16_t w;
-          __builtin_memcpy(&w, at + 2 * i, 2);
-          v = (v & ~(0xFFFFull << (16 * i))) | (uint64_t)w << (16 * i);
-        }
-    }
-    return v;
+  auto fetch = [&](const Scales& s, int row, int u) {
+    return scale_unit(s.at + (int64_t)row * s.bytes, s.bytes, u);
   };
   uint64_t sa_next = 0, sb_next = 0, sa_unit = 0;
   auto fetch_scales = [&](const Stage& q) {
