@@ -155,8 +155,8 @@ moe_status moe_mx_product(const void* x, const void* x_scales, const void* w_cod
     return efail(MOE_EINVAL, "x, w_codes, w_scales and y must not be NULL");
   if (!aligned(x, 16) || !aligned(w_codes, 16) || !aligned(y, 16))
     return efail(MOE_EINVAL, "x, w_codes and y must be 16-byte aligned");
-  if (!aligned(x_scales, 2) || !aligned(w_scales, 2))
-    return efail(MOE_EINVAL, "scales must be 2-byte aligned");
+  if (!aligned(x_scales, 4) || !aligned(w_scales, 4))
+    return efail(MOE_EINVAL, "scales must be 4-byte aligned");
   if (n_rows == 0) return MOE_OK;
   const Grouped g = {expert_count, type, n_rows, d_in, d_out, n_experts};
   const hipError_t he = launch_mx_product(g, x, static_cast<const uint8_t*>(x_scales),

@@ -67,6 +67,14 @@ __device__ inline void load_lds(uint32_t lds, const uint8_t* base, uint32_t limi
                :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
 }
 
+// 4 bytes per lane to LDS at lds + 4 * lane, likewise.
+__device__ inline void load_lds4(uint32_t lds, const uint8_t* base, uint32_t limit, uint32_t off) {
+  const uint64_t p = (uint64_t)(uintptr_t)base;
+  const u32x4 d = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, limit, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
+}
+
 // All but the N newest loads of this wave are in LDS and every LDS read of it
 // has returned, then the block's barrier.
 template <int N>
@@ -198,26 +206,35 @@ __device__ inline uint64_t scale_unit(const uint8_t* row, int bytes, int u) {
   return v;
 }
 
-// LDS of a tile: rings of SA and SB slots, then two slots of scales (F4: 8
-// bytes per row and stage, CODES: 2).
+// LDS of a tile: rings of SA and SB slots, then slots of scales.
+//
+// F4: two slots of 8 bytes per row, a stage's.  They come through registers
+// (a row of scales may lie on any even address), and the compiler waits for
+// these loads as if the others were not there: so none is left in flight at a
+// barrier, and deeper rings would be waited for in vain.
+//
+// CODES: four slots of three dwords per row, the 8 bytes of a unit of four
+// stages and what is before or behind them up to whole dwords, by direct loads:
+// dword j of all rows lies at 256 TA j.
 template <int TYPE, int KA, int KB, int TA, int TB, int LDS>
 struct Ring {
-  static constexpr bool kScales = TYPE == F4 || KA == CODES;
   static constexpr uint32_t kA = Loads<KA, TA>::kSlot, kB = Loads<KB, TB>::kSlot;
-  static constexpr uint32_t kScaleSlot = TYPE == F4 ? 512 * (TA + TB) : KA == CODES ? 128 * TA : 0;
-  static constexpr uint32_t kRoom = LDS - 2 * kScaleSlot;
+  static constexpr uint32_t kScaleSlot = TYPE == F4 ? 512 * (TA + TB) : KA == CODES ? 768 * TA : 0;
+  static constexpr int kScaleSlots = TYPE == F4 ? 2 : 4;
+  static constexpr uint32_t kRoom = LDS - kScaleSlots * kScaleSlot;
   static constexpr int kBoth = (int)(kRoom / (kA + kB));
-  // with scales, whose loads the compiler waits for, no load is left in
-  // flight at a barrier, and deeper rings would be waited for in vain
-  static constexpr int SB = kScales ? 2 : kBoth > 4 ? 4 : kBoth;
-  static constexpr int SA = kScales ? 2 : SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
+  static constexpr int SB = TYPE == F4 ? 2 : kBoth > 4 ? 4 : kBoth;
+  static constexpr int SA = KA != CODES && TYPE != F4 && SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
   static constexpr uint32_t kBBase = SA * kA, kScaleBase = kBBase + SB * kB;
-  static_assert(SB >= 2 && kScaleBase + 2 * kScaleSlot <= LDS, "LDS");
+  static_assert(SB >= 2 && kScaleBase + kScaleSlots * kScaleSlot <= LDS, "LDS");
   // stages ahead of the products that anything is fetched for
-  static constexpr int kAhead = kScales ? 2 : SA - 1;
+  static constexpr int kAhead = TYPE == F4 ? 2 : SA - 1;
   // loads that may be in flight when a stage ends: those of the stages after
   // the next one
   static constexpr int kPending = (SA - 2) * Loads<KA, TA>::kN + (SB - 2) * Loads<KB, TB>::kN;
+  // quarters (of 16 between two barriers) that the loads are spread over: all
+  // of a ring of two have to arrive within these
+  static constexpr int kSpread = SA == 2 ? 4 : 12;
 };
 
 // The accumulators of a wave: acc[i][j] is A tile i, B tile j of its own.
@@ -323,41 +340,68 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     lb.load(q.k, steps, i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
   };
 
-  // Scales of 256 columns (8 bytes) of the thread's row of A, and in F4 of B,
-  // into registers; a stage later to LDS.
+  // F4: scales of 256 columns (8 bytes) of the thread's row of A and of B, into
+  // registers; a stage later to LDS.  Past the row (256 columns at least): 2^0.
+  // No branch: the compiler would move products across it.
   const int t = threadIdx.x;
-  auto fetch = [&](const Scales& s, int row, int u) {
-    return scale_unit(s.at + (int64_t)row * s.bytes, s.bytes, u);
-  };
-  uint64_t sa_next = 0, sb_next = 0, sa_unit = 0;
-  auto fetch_scales = [&](const Stage& q) {
+  const uint8_t *sa_row = nullptr, *sb_row = nullptr;
+  uint64_t sa_next = 0, sb_next = 0;
+  auto open_scales = [&](const Stage& q) {
     if constexpr (kF4) {
-      if (q.n) {
+      if (q.k == 0 && q.n) {
         const Tile x = tile_of(q.i);
-        if (t < 64 * TA) sa_next = fetch(job.a_scales(x), min(t, job.a(x).valid - 1), q.k);
-        if (t < 64 * TB) sb_next = fetch(job.b_scales(x), min(t, job.b(x).valid - 1), q.k);
-      }
-    } else if constexpr (kCodes) {
-      if (q.n && (q.k & 3) == 0) {
-        const Tile x = tile_of(q.i);
-        if (t < 64 * TA) sa_next = fetch(job.a_scales(x), min(t, job.a(x).valid - 1), q.k >> 2);
+        const Scales u = job.a_scales(x), w = job.b_scales(x);
+        sa_row = u.at + (int64_t)min(t, min(64 * TA, job.a(x).valid) - 1) * u.bytes;
+        sb_row = w.at + (int64_t)min(t, min(64 * TB, job.b(x).valid) - 1) * w.bytes;
       }
     }
   };
-  auto put_scales = [&](const Stage& q, uint32_t slot) {
+  auto fetch_scales = [&](const Stage& q) {
+    if constexpr (kF4) {
+      // (behind the last stage: the last tile's first ones again)
+      const int bytes = p[0].steps / 32, at = min(8 * q.k, bytes - 8), past = 8 * (8 * q.k - at);
+      const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
+      __builtin_memcpy(&sa_next, sa_row + at, 8);
+      __builtin_memcpy(&sb_next, sb_row + at, 8);
+      sa_next = sa_next >> past | fill;
+      sb_next = sb_next >> past | fill;
+    }
+  };
+  auto put_scales = [&](uint32_t slot) {
     const uint32_t at = R::kScaleBase + slot * R::kScaleSlot;
     if constexpr (kF4) {
-      if (t < 64 * TA) lds_write(lds, at + 8 * t, sa_next);
-      if (t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
-    } else if constexpr (kCodes) {
-      if ((q.k & 3) == 0) sa_unit = sa_next;
-      if (t < 64 * TA) lds_write(lds, at + 2 * t, (uint16_t)(sa_unit >> (16 * (q.k & 3))));
+      if (64 * TA >= kThreads || t < 64 * TA) lds_write(lds, at + 8 * t, sa_next);
+      if (64 * TB >= kThreads || t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
+    }
+  };
+  // CODES: the scales of a unit that begins at stage q.  An odd row whose scales
+  // fill no whole dwords begins two bytes earlier.
+  uint32_t unit = 0, unit_read = 0;                 // slots written next, read
+  auto load_unit = [&](const Stage& q) {
+    if constexpr (kCodes) {
+      if (q.n && (q.k & 3) == 0) {
+        const Tile x = tile_of(q.i);
+        const Scales s = job.a_scales(x);
+        const int valid = min(job.a(x).valid, 64 * TA);
+        const uint8_t* base = uniform(s.at + 2 * q.k);
+        const uint32_t limit = valid * s.bytes - 2 * q.k;
+#pragma unroll
+        for (int i = 0; i < 3 * TA / 4 + (TA % 4 != 0); ++i) {
+          const int piece = wave + 4 * i;            // 64 rows of a dword
+          const int j = piece / TA, r = piece % TA * 64 + l;
+          const uint32_t off = r < valid && j < 3 ? r * s.bytes - (r * s.bytes & 2) + 4 * j : kMasked;
+          if (piece < 3 * TA) load_lds4(lds0 + R::kScaleBase + unit * R::kScaleSlot + 256 * piece, base, limit, off);
+        }
+        unit = (unit + 1) & 3;
+      }
     }
   };
 
+  open_scales(p[0]);
   fetch_scales(p[0]);
-  put_scales(p[0], 0);
-  if (R::kScales) fetch_scales(p[1]);
+  put_scales(0);
+  open_scales(p[1]);
+  fetch_scales(p[1]);
   // the rings' first stages; what the first stage needs comes first
 #pragma unroll
   for (int v = 0; v < R::SA - 1; ++v) {
@@ -367,6 +411,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       for (int i = 0; i < kNB; ++i) load_b(p[v], i, v);
     }
     open_a(p[v]);
+    load_unit(p[v]);
 #pragma unroll
     for (int i = 0; i < kNA; ++i) load_a(p[v], i, v);
   }
@@ -413,11 +458,14 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     if constexpr (KB == COLS) b[s & 1][j] = transposed(at + bcol[j] + s * 1024 * TB, 512 * TB);
     else b[s & 1][j] = lds_read<u32x4>(lds, at + brow + j * 4096 + cat[s]);
   };
-  // CODES: the lane's 32 codes of a stage and their scale
-  auto read_raw = [&](int i, uint32_t slot, uint32_t scales) {
+  // CODES: the lane's 32 codes of a stage and their scale, byte `at` of the
+  // row's 12
+  auto read_raw = [&](int i, uint32_t slot, const Stage& q) {
     if constexpr (kCodes) {
       raw[i] = lds_read<u32x4>(lds, slot * R::kA + (arow >> 2) + i * 1024 + 16 * (half ^ ((l >> 3) & 1)));
-      scale[i] = scale_of(lds_read<uint8_t>(lds, R::kScaleBase + scales * R::kScaleSlot + (arow >> 6) + i * 64 + half));
+      const int at = 2 * (q.k & 3) + half + ((l & 1) & (q.steps >> 6)) * 2;
+      scale[i] = scale_of(lds_read<uint8_t>(lds, R::kScaleBase + unit_read * R::kScaleSlot + (arow >> 5) + i * 128 +
+                                                     (at >> 2) * 256 * TA + (at & 3)));
     }
   };
   auto read_scales = [&](uint32_t slot, uint32_t (&x)[kF4 ? TA : 1], uint32_t (&y)[kF4 ? TB : 1]) {
@@ -465,7 +513,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   uint32_t al = R::SA - 1, bl = R::SB - 1;          // slots loaded next
   // Quarter c's share (of 16) of the loads issued between two barriers: B's
   // first, whose ring is never the deeper one.
-  constexpr int kAll = kNB + kNA, kSpread = 12;
+  constexpr int kAll = kNB + kNA, kSpread = R::kSpread;
   auto loads = [&](int c) {
 #pragma unroll
     for (int i = c * kAll / kSpread; i < min((c + 1) * kAll / kSpread, kAll); ++i) {
@@ -497,17 +545,17 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   read_scales(0, sa, sb);
 #pragma unroll
   for (int i = 0; i < TA; ++i) {
-    read_raw(i, 0, 0);
+    read_raw(i, 0, p[0]);
     read_a(0, i, 0);
   }
 #pragma unroll
   for (int j = 0; j < TB; ++j) read_b(0, j, 0);
-  if (R::kScales) {
-    put_scales(p[1], 1);
-    fetch_scales(p[2 < R::kAhead ? 2 : R::kAhead]);
-  }
+  put_scales(1);
+  open_scales(p[R::kAhead]);
+  fetch_scales(p[R::kAhead]);
   open_b(p[R::SB - 1]);
   open_a(p[R::SA - 1]);
+  load_unit(p[R::SA - 1]);
 #pragma unroll
   for (int c = 0; c < 4; ++c) loads(c);
   while (p[0].n) {
@@ -523,6 +571,16 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       step(s0);
       step(s1);
       step(s2);
+#ifdef __HIP_DEVICE_COMPILE__
+      // (a use here: the compiler would move the products behind the branches
+      // below, away from their operands' reads)
+      if constexpr (kF4) {
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+#pragma unroll
+          for (int j = 0; j < TB; ++j) asm volatile("" :: "a"(acc[i][j][0]));
+      }
+#endif
       // every load of the next stage has arrived; this stage's slots are free
       stage_barrier<R::kPending>();
       ac = next(ac, R::SA);
@@ -538,12 +596,13 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       if (p[R::kAhead].k == 0 && p[R::kAhead].n && made <= p[R::kAhead].i + 1) make();
       // scales of the stage after the next into LDS, whose slot the barrier
       // freed, those of the one behind it into registers
-      if (R::kScales) {
-        put_scales(p[1], sc ^ 1);
-        fetch_scales(p[R::kAhead]);
-      }
+      put_scales(sc ^ 1);
+      open_scales(p[R::kAhead]);
+      fetch_scales(p[R::kAhead]);
       open_b(p[R::SB - 1]);
       open_a(p[R::SA - 1]);
+      load_unit(p[R::SA - 1]);
+      if (kCodes && (p[0].k & 3) == 0) unit_read = (unit_read + 1) & 3;
       read_scales(sc, sa1, sb1);
       // (after the last stage of all: reads that are not multiplied)
 #pragma unroll
@@ -551,7 +610,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         loads(c);
         if (c == 0) {
 #pragma unroll
-          for (int i = 0; i < TA; ++i) read_raw(i, ac, sc);
+          for (int i = 0; i < TA; ++i) read_raw(i, ac, p[0]);
         }
 #pragma unroll
         for (int i = 0; i < TA; ++i)
@@ -582,7 +641,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
 template <int TILES>
 __device__ inline void keep(f32x16& c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  if constexpr (TILES > 8) asm volatile("" : "+a"(c));
+  if constexpr (TILES >= 8) asm volatile("" : "+a"(c));
 #endif
 }
 

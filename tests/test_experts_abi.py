@@ -73,8 +73,9 @@ def test_mx_product_pointers():
         assert _mx(**{name: None}) == B.MOE_EINVAL
     for name in ("x", "w", "y"):
         assert _mx(**{name: P8}) == B.MOE_EINVAL
-    assert _mx(ws=P1) == B.MOE_EINVAL
-    assert _mx(xs=P1) == B.MOE_EINVAL
+    for odd in (P1, P2):
+        assert _mx(ws=odd) == B.MOE_EINVAL
+        assert _mx(xs=odd) == B.MOE_EINVAL
     assert _mx(n_rows=0, x=None, y=None) == B.MOE_OK
 
 
