@@ -187,21 +187,51 @@ template <int TA> constexpr int kBlocks = TA == 4 ? 256 : 512;
 template <int TA>
 struct Items {
   RowTiles<kRows<TA>> tiles;
-  int die, slot;
-  RowTile t;           // the first one not taken
-  bool any;
+  int slot;
+  RowTile t;           // the first one not taken; n = 0: none
 
   __device__ inline void init(const Grouped& g, int parts) {
     tiles.init(g, parts);
-    die = blockIdx.x & 7;
+    tile::set_aside(tiles.parts);
+    tile::set_aside(tiles.n_big);
+    tile::set_aside(tiles.n_rest);
+    tile::set_aside(tiles.slots_big);
+    tile::set_aside(tiles.slots);
+    tile::set_aside(tiles.counts.per);
     slot = (int)(blockIdx.x >> 3) - kBlocks<TA> / 8;
+    tile::set_aside(slot);
     step();
   }
   __device__ inline void step() {
-    any = false;
-    while (!any && (slot += kBlocks<TA> / 8) < tiles.slots) any = tiles.get(die, slot, t);
+    RowTiles<kRows<TA>> now = tiles;  // (in scalar registers for as long as this takes)
+    now.parts = __builtin_amdgcn_readfirstlane(tiles.parts);
+    now.n_big = __builtin_amdgcn_readfirstlane(tiles.n_big);
+    now.n_rest = __builtin_amdgcn_readfirstlane(tiles.n_rest);
+    now.slots_big = __builtin_amdgcn_readfirstlane(tiles.slots_big);
+    now.slots = __builtin_amdgcn_readfirstlane(tiles.slots);
+    now.counts.per = __builtin_amdgcn_readfirstlane(tiles.counts.per);
+    int at = __builtin_amdgcn_readfirstlane(slot);
+    RowTile x = {0, 0, 0, 0};
+    bool any = false;
+    while (!any && (at += kBlocks<TA> / 8) < now.slots) any = now.get(blockIdx.x & 7, at, x);
+    if (!any) x.n = 0;
+    t = x;
+    slot = at;
+    tile::set_aside(slot);
+    tile::set_aside(t.expert);
+    tile::set_aside(t.row);
+    tile::set_aside(t.n);
+    tile::set_aside(t.part);
   }
-  __device__ inline int size() const { return (t.n + 63) >> 6; }
+  __device__ inline int rows() const { return __builtin_amdgcn_readfirstlane(t.n); }
+  __device__ inline int size() const { return (rows() + 63) >> 6; }
+  __device__ inline bool next(int tb, RowTile& x) {
+    if (size() != tb) return false;
+    x = {__builtin_amdgcn_readfirstlane(t.expert), __builtin_amdgcn_readfirstlane(t.row), rows(),
+         __builtin_amdgcn_readfirstlane(t.part)};
+    step();
+    return true;
+  }
 };
 
 // Whether blocks of 256 columns and rows are enough to fill the chip.

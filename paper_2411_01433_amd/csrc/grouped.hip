@@ -27,12 +27,7 @@ struct RowJob {
 
   __device__ inline int n_in() const { return BACK ? g.d_out : g.d_in; }
   __device__ inline int n_out() const { return BACK ? g.d_in : g.d_out; }
-  __device__ inline bool next(Tile& t) {
-    if (!items.any || items.size() != TB) return false;
-    t = items.t;
-    items.step();
-    return true;
-  }
+  __device__ inline bool next(Tile& t) { return items.next(TB, t); }
   __device__ inline int steps(const Tile&) const { return n_in(); }
   __device__ inline Operand a(const Tile& t) const {
     const int col = t.part * 64 * TA;
@@ -57,13 +52,15 @@ void rows_kernel(Grouped g, const void* in, const void* w, void* out, int parts)
   lds_u8* lds = (lds_u8*)smem;
   Items<TA> items;
   items.init(g, parts);
+  set_aside(in);
+  set_aside(w);
+  set_aside(out);
   auto take = [&](auto size) {
     constexpr int TB = decltype(size)::value;
     RowJob<TYPE, TA, TB, BACK> job = {g, (const T*)in, (const T*)w, (T*)out, items};
     stream<TYPE, KA, ROWS, TA, TB, kLds<TA>>(job, lds);
   };
-  while (items.any) {
-    const int n = items.size();
+  while (const int n = items.size()) {
     if (n == 1) take(std::integral_constant<int, 1>());
     else if (n == 2) take(std::integral_constant<int, 2>());
     else if (TA == 4 && n == 3) take(std::integral_constant<int, TA == 4 ? 3 : 1>());
@@ -82,37 +79,57 @@ struct WeightItems {
   const Grouped& g;
   bool accumulate;
   Counts counts;
-  int die, slot, na, nb, per, n;
-  WeightTile t;
-  bool any;
+  int slot;
+  WeightTile t;        // the first one not taken; n < 0: none
 
   __device__ inline void init() {
     counts.init(g);
-    na = (g.d_out + kRows<TA> - 1) / kRows<TA>;
-    nb = (g.d_in + kRows<TA> - 1) / kRows<TA>;
-    per = na * nb;
-    n = g.E * per;
-    die = blockIdx.x & 7;
+    set_aside(counts.per);
     slot = (int)(blockIdx.x >> 3) - kBlocks<TA> / 8;
+    set_aside(slot);
     step();
   }
   __device__ inline void step() {
     constexpr int kSuper = 8;  // tiles of d_in that alternate fastest
-    any = false;
-    while (!any && (slot += kBlocks<TA> / 8) < die_slots(n)) {
-      const int item = die_item(n, die, slot);
+    const int na = (g.d_out + kRows<TA> - 1) / kRows<TA>, nb = (g.d_in + kRows<TA> - 1) / kRows<TA>;
+    const int per = na * nb, n = g.E * per;
+    Counts now = counts;
+    now.per = __builtin_amdgcn_readfirstlane(counts.per);
+    int at = __builtin_amdgcn_readfirstlane(slot);
+    WeightTile x = {0, 0, -1, 0, 0};
+    while (x.n < 0 && (at += kBlocks<TA> / 8) < die_slots(n)) {
+      const int item = die_item(n, blockIdx.x & 7, at);
       if (item < 0) continue;
       const int e = item / per, in = item - e * per;
-      const Rows rows = counts.rows(e);
+      const Rows rows = now.rows(e);
       if (accumulate && rows.n == 0) continue;
       const int sup = in / (kSuper * na), left = in - sup * (kSuper * na);
       const int width = min(kSuper, nb - sup * kSuper);
       const int ia = left / width, ib = sup * kSuper + left - ia * width;
-      t = {e, rows.first, rows.n, ia * kRows<TA>, ib * kRows<TA>};
-      any = true;
+      x = {e, rows.first, rows.n, ia * kRows<TA>, ib * kRows<TA>};
     }
+    t = x;
+    slot = at;
+    set_aside(slot);
+    set_aside(t.expert);
+    set_aside(t.first);
+    set_aside(t.n);
+    set_aside(t.a0);
+    set_aside(t.b0);
   }
-  __device__ inline int size() const { return min(kRows<TA>, g.d_in - t.b0) >> 6; }
+  // 64s of columns of the tile (0: no tile)
+  __device__ inline int size() const {
+    const int n = __builtin_amdgcn_readfirstlane(t.n);
+    return n < 0 ? 0 : min(kRows<TA>, g.d_in - __builtin_amdgcn_readfirstlane(t.b0)) >> 6;
+  }
+  __device__ inline bool next(int tb, WeightTile& x) {
+    if (size() != tb) return false;
+    x = {__builtin_amdgcn_readfirstlane(t.expert), __builtin_amdgcn_readfirstlane(t.first),
+         __builtin_amdgcn_readfirstlane(t.n), __builtin_amdgcn_readfirstlane(t.a0),
+         __builtin_amdgcn_readfirstlane(t.b0)};
+    step();
+    return true;
+  }
 };
 
 template <int TYPE, int TA, int TB>
@@ -124,12 +141,7 @@ struct WeightJob {
   float* dw;
   WeightItems<TA>& items;
 
-  __device__ inline bool next(Tile& t) {
-    if (!items.any || items.size() != TB) return false;
-    t = items.t;
-    items.step();
-    return true;
-  }
+  __device__ inline bool next(Tile& t) { return items.next(TB, t); }
   __device__ inline int steps(const Tile& t) const { return t.n; }
   __device__ inline Operand a(const Tile& t) const {
     return {(const uint8_t*)(dy + (int64_t)t.first * g.d_out + t.a0), (uint32_t)(2 * g.d_out), g.d_out - t.a0};
@@ -152,7 +164,7 @@ struct WeightJob {
         keep<TA * TB>(acc[i][j]);
 #pragma unroll
         for (int q = 0; q < 16; ++q) {
-          float* to = out + (int64_t)(32 * i + 8 * (q >> 2) + (q & 3)) * g.d_in + 32 * j;
+          auto* to = global_ptr<float>(out + (int64_t)(32 * i + 8 * (q >> 2) + (q & 3)) * g.d_in + 32 * j);
           const float v = acc[i][j][q];
           __builtin_nontemporal_store(items.accumulate ? *to + v : v, to);
         }
@@ -169,13 +181,15 @@ void dw_kernel(Grouped g, const void* dy, const void* x, float* dw, bool accumul
   lds_u8* lds = (lds_u8*)smem;
   WeightItems<TA> items = {g, accumulate};
   items.init();
+  set_aside(dy);
+  set_aside(x);
+  set_aside(dw);
   auto take = [&](auto size) {
     constexpr int TB = decltype(size)::value;
     WeightJob<TYPE, TA, TB> job = {g, (const T*)dy, (const T*)x, dw, items};
     stream<TYPE, COLS, COLS, TA, TB, kLds<TA>>(job, lds);
   };
-  while (items.any) {
-    const int n = items.size();
+  while (const int n = items.size()) {
     if (n == 1) take(std::integral_constant<int, 1>());
     else if (n == 2) take(std::integral_constant<int, 2>());
     else if (TA == 4 && n == 3) take(std::integral_constant<int, TA == 4 ? 3 : 1>());

@@ -21,12 +21,7 @@ struct MxJob {
   T* y;
   Items<TA>& items;
 
-  __device__ inline bool next(Tile& t) {
-    if (!items.any || items.size() != TB) return false;
-    t = items.t;
-    items.step();
-    return true;
-  }
+  __device__ inline bool next(Tile& t) { return items.next(TB, t); }
   __device__ inline int steps(const Tile&) const { return g.d_in; }
   __device__ inline int64_t column(const Tile& t) const { return (int64_t)t.expert * g.d_out + t.part * 64 * TA; }
   __device__ inline Operand a(const Tile& t) const {
@@ -52,13 +47,17 @@ void mx_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w,
   lds_u8* lds = (lds_u8*)smem;
   Items<TA> items;
   items.init(g, parts);
+  set_aside(x);
+  set_aside(xs);
+  set_aside(w);
+  set_aside(ws);
+  set_aside(y);
   auto take = [&](auto size) {
     constexpr int TB = decltype(size)::value;
     MxJob<TYPE, TA, TB, CODED> job = {g, x, xs, w, ws, (typename Elem<TYPE>::T*)y, items};
     stream<CODED ? F4 : TYPE, CODED ? ROWS : CODES, ROWS, TA, TB, kLds<TA>>(job, lds);
   };
-  while (items.any) {
-    const int n = items.size();
+  while (const int n = items.size()) {
     if (n == 1) take(std::integral_constant<int, 1>());
     else if (n == 2) take(std::integral_constant<int, 2>());
     else if (TA == 4 && n == 3) take(std::integral_constant<int, TA == 4 ? 3 : 1>());

@@ -90,6 +90,21 @@ __device__ inline const uint8_t* uniform(const void* p) {
   return reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
 }
 
+// A uniform value into vector registers: what is needed once a tile would crowd
+// the scalar ones out of the loop.
+template <class T>
+__device__ inline void set_aside(T& v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(v));
+#endif
+}
+
+// (a pointer that was set aside has lost its address space)
+template <class T>
+__device__ inline __attribute__((address_space(1))) T* global_ptr(const void* p) {
+  return (__attribute__((address_space(1))) T*)(uintptr_t)p;
+}
+
 template <class T>
 __device__ inline T lds_read(const lds_u8* lds, uint32_t at) {
   return *reinterpret_cast<const __attribute__((address_space(3))) T*>(lds + at);
@@ -108,15 +123,16 @@ struct Operand {
 };
 
 // An operand's loads: per lane the source of each of a wave's kN loads per
-// stage, relative to the stage's base.  Load i of wave w fills 1024 bytes of
-// the slot from 1024 (w + 4 i) on.
+// stage, relative to the stage's place, which moves on.  Load i of wave w fills
+// 1024 bytes of the slot from 1024 (w + 4 i) on.
 template <int KIND, int T>
 struct Loads {
   static_assert(KIND != CODES || T % 2 == 0, "whole loads");
   static constexpr int kN = KIND == CODES ? T / 2 : 2 * T;
   static constexpr uint32_t kSlot = 4096 * kN;
   uint32_t off[kN];
-  const uint8_t* base;
+  const uint8_t* at;
+  uint32_t limit;       // what of it may be read (0: nothing)
   uint32_t row_bytes;
 
   // ROWS: the lane's 16 bytes of each row's 128 (of every load the same)
@@ -127,15 +143,15 @@ struct Loads {
   // COLS: what row r's chunks are permuted by (64-byte pieces: bits 2 and up)
   static __device__ inline int piece(int r) { return T % 2 ? (r & 2) << 1 : (r & 3) << 2; }
 
-  __device__ inline void init(const Operand& o, int wave) {
+  __device__ inline void open(const Operand& o, int wave) {
     const int l = threadIdx.x & 63;
-    base = uniform(o.base);
-    row_bytes = o.row_bytes;
+    at = uniform(o.base);
+    row_bytes = __builtin_amdgcn_readfirstlane(o.row_bytes);
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const int q = wave + 4 * i;
       if (KIND == COLS) {
-        const int at = 64 * q + l, row = at / (8 * T), c = (at % (8 * T)) ^ piece(row);
+        const int to = 64 * q + l, row = to / (8 * T), c = (to % (8 * T)) ^ piece(row);
         off[i] = 8 * c < o.valid ? (uint32_t)row * row_bytes + 16 * c : kMasked;
       } else if (KIND == ROWS) {
         const int row = 8 * q + (l >> 3);
@@ -146,18 +162,16 @@ struct Loads {
       }
     }
   }
-
-  // load i of stage k of `steps` reduction steps (ROWS, CODES: of `steps`
-  // bytes of a row) in all
-  __device__ inline void load(int k, int steps, int i, uint32_t lds, uint32_t mask) const {
-    if (KIND == COLS) {
-      const int left = __builtin_amdgcn_readfirstlane(max(0, min(steps - kStage * k, kStage)));
-      load_lds(lds, base + (int64_t)k * kStage * row_bytes, (uint32_t)left * row_bytes, off[i]);
-    } else {
-      constexpr int kBytes = KIND == CODES ? 32 : 128;
-      load_lds(lds, base + (int64_t)k * kBytes, kBytes * k < steps ? kMasked - 1 : 0, off[i] | mask);
-    }
+  // to the next stage of the same tile, or (another) just opened
+  __device__ inline void advance(bool another) {
+    at += another ? 0 : KIND == COLS ? (int64_t)kStage * row_bytes : KIND == CODES ? 32 : 128;
   }
+  // `left` reduction steps from the stage's first on (0: none are read)
+  __device__ inline void bound(int left) {
+    limit = __builtin_amdgcn_readfirstlane(
+        KIND == COLS ? max(0, min(left, kStage)) * row_bytes : left > 0 ? kMasked - 1 : 0);
+  }
+  __device__ inline void load(int i, uint32_t lds, uint32_t mask) const { load_lds(lds, at, limit, off[i] | mask); }
 };
 
 __device__ inline uint32_t as_u32(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
@@ -213,19 +227,22 @@ __device__ inline uint64_t scale_unit(const uint8_t* row, int bytes, int u) {
 // these loads as if the others were not there: so none is left in flight at a
 // barrier, and deeper rings would be waited for in vain.
 //
-// CODES: four slots of three dwords per row, the 8 bytes of a unit of four
+// CODES: eight slots of three dwords per row, the 8 bytes of a unit of four
 // stages and what is before or behind them up to whole dwords, by direct loads:
 // dword j of all rows lies at 256 TA j.
 template <int TYPE, int KA, int KB, int TA, int TB, int LDS>
 struct Ring {
   static constexpr uint32_t kA = Loads<KA, TA>::kSlot, kB = Loads<KB, TB>::kSlot;
   static constexpr uint32_t kScaleSlot = TYPE == F4 ? 512 * (TA + TB) : KA == CODES ? 768 * TA : 0;
-  static constexpr int kScaleSlots = TYPE == F4 ? 2 : 4;
+  static constexpr int kScaleSlots = TYPE == F4 ? 2 : 8;
   static constexpr uint32_t kRoom = LDS - kScaleSlots * kScaleSlot;
   static constexpr int kBoth = (int)(kRoom / (kA + kB));
-  static constexpr int SB = TYPE == F4 ? 2 : kBoth > 4 ? 4 : kBoth;
+  static constexpr int SB = TYPE == F4 ? 2 : kBoth > 6 ? 6 : kBoth;
   static constexpr int SA = KA != CODES && TYPE != F4 && SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
   static constexpr uint32_t kBBase = SA * kA, kScaleBase = kBBase + SB * kB;
+  // (a tile of one stage has a slot of scales of its own, and the queue of
+  // stream() holds the tile of the products and seven behind it)
+  static_assert(SA <= 6 && SB <= 6, "stages ahead");
   static_assert(SB >= 2 && kScaleBase + kScaleSlots * kScaleSlot <= LDS, "LDS");
   // stages ahead of the products that anything is fetched for
   static constexpr int kAhead = TYPE == F4 ? 2 : SA - 1;
@@ -296,48 +313,56 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     __builtin_memcpy(&tile, w, sizeof(Tile));
     return tile;
   };
-  // A stage: stage k of n of tile i.  p[j] is the one j stages after that of the
-  // products.
-  struct Stage {
+  // Where an operand's loads are: at stage k of n of tile i (n = 0: behind the
+  // last), which takes `steps` reduction steps.
+  struct Place {
     int i, k, n, steps;
   };
-  auto begin = [&](int i) -> Stage {
+  auto begin = [&](int i) -> Place {
     return {i, 0, __builtin_amdgcn_readlane(queue, 8 * (i & 7)),
             __builtin_amdgcn_readlane(queue, 8 * (i & 7) + 1)};
   };
-  // (tile i + 1 is there, or tile i is the end, which stays)
-  auto after = [&](const Stage& q) {
-    Stage x = q;
-    if (++x.k >= x.n) x = begin(q.n ? q.i + 1 : q.i);
-    return x;
+  // Moves on; true: to another tile (that is there), or behind the last.
+  auto move = [&](Place& p) {
+    if (++p.k < p.n) return false;
+    p = begin(p.n ? p.i + 1 : p.i);
+    return true;
   };
-  Stage p[R::kAhead + 1];
 #pragma unroll 1
   for (int i = 0; i < R::kAhead + 2; ++i) make();
-  p[0] = begin(0);
-  if (p[0].n == 0) return;
-#pragma unroll
-  for (int j = 0; j < R::kAhead; ++j) p[j + 1] = after(p[j]);
+  Place pa = begin(0), pb = pa;
+  if (pa.n == 0) return;
+  int tile = 0, left = pa.n, k_now = 0;             // of the products: stages left, stage
+  // (of all tiles the same where codes or scales are read)
+  const int columns = pa.steps;
 
   Loads<KA, TA> la;
   Loads<KB, TB> lb;
-  auto open_a = [&](const Stage& q) {
-    if (q.k == 0 && q.n) la.init(job.a(tile_of(q.i)), wave);
+  la.open(job.a(tile_of(0)), wave);
+  lb.open(job.b(tile_of(0)), wave);
+  la.bound(pa.steps);
+  lb.bound(pb.steps);
+  auto move_a = [&]() {
+    const bool another = move(pa);
+    if (another && pa.n) la.open(job.a(tile_of(pa.i)), wave);
+    la.advance(another);
+    la.bound(pa.steps - (kF4 ? 256 : kStage) * pa.k);
   };
-  auto open_b = [&](const Stage& q) {
-    if (q.k == 0 && q.n) lb.init(job.b(tile_of(q.i)), wave);
+  auto move_b = [&]() {
+    const bool another = move(pb);
+    if (another && pb.n) lb.open(job.b(tile_of(pb.i)), wave);
+    lb.advance(another);
+    lb.bound(pb.steps - (kF4 ? 256 : kStage) * pb.k);
   };
-  // (behind the last stage no step is left, and the loads read nothing)
-  auto load_a = [&](const Stage& q, int i, uint32_t slot) {
-    const int steps = KA == COLS ? q.steps : kF4 || kCodes ? q.steps / 2 : q.steps * 2;
-    // In MXFP4 a row's last line may be partial.
-    const uint32_t mask = kF4 && (uint32_t)(128 * q.k) + la.chunk(wave) >= (uint32_t)steps ? kMasked : 0;
-    la.load(q.k, steps, i, lds0 + slot * R::kA + (wave + 4 * i) * 1024, mask);
+  // In MXFP4 a row's last line may be partial: the chunks behind it are masked
+  // (of either operand, whose loads are at the same stage).
+  auto load_a = [&](int i, uint32_t slot) {
+    const uint32_t mask = kF4 && (uint32_t)(128 * pa.k) + la.chunk(wave) >= (uint32_t)columns / 2 ? kMasked : 0;
+    la.load(i, lds0 + slot * R::kA + (wave + 4 * i) * 1024, mask);
   };
-  auto load_b = [&](const Stage& q, int i, uint32_t slot) {
-    const int steps = KB == COLS ? q.steps : kF4 ? q.steps / 2 : q.steps * 2;
-    const uint32_t mask = kF4 && (uint32_t)(128 * q.k) + lb.chunk(wave) >= (uint32_t)steps ? kMasked : 0;
-    lb.load(q.k, steps, i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
+  auto load_b = [&](int i, uint32_t slot) {
+    const uint32_t mask = kF4 && (uint32_t)(128 * pb.k) + la.chunk(wave) >= (uint32_t)columns / 2 ? kMasked : 0;
+    lb.load(i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
   };
 
   // F4: scales of 256 columns (8 bytes) of the thread's row of A and of B, into
@@ -346,25 +371,30 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   const int t = threadIdx.x;
   const uint8_t *sa_row = nullptr, *sb_row = nullptr;
   uint64_t sa_next = 0, sb_next = 0;
-  auto open_scales = [&](const Stage& q) {
+  Place ps = pa;
+  auto open_scales = [&]() {
     if constexpr (kF4) {
-      if (q.k == 0 && q.n) {
-        const Tile x = tile_of(q.i);
-        const Scales u = job.a_scales(x), w = job.b_scales(x);
-        sa_row = u.at + (int64_t)min(t, min(64 * TA, job.a(x).valid) - 1) * u.bytes;
-        sb_row = w.at + (int64_t)min(t, min(64 * TB, job.b(x).valid) - 1) * w.bytes;
-      }
+      const Tile x = tile_of(ps.i);
+      const Scales u = job.a_scales(x), w = job.b_scales(x);
+      sa_row = u.at + (int64_t)min(t, min(64 * TA, job.a(x).valid) - 1) * u.bytes;
+      sb_row = w.at + (int64_t)min(t, min(64 * TB, job.b(x).valid) - 1) * w.bytes;
     }
   };
-  auto fetch_scales = [&](const Stage& q) {
+  auto fetch_scales = [&]() {
     if constexpr (kF4) {
       // (behind the last stage: the last tile's first ones again)
-      const int bytes = p[0].steps / 32, at = min(8 * q.k, bytes - 8), past = 8 * (8 * q.k - at);
+      const int bytes = columns / 32, at = min(8 * ps.k, bytes - 8), past = 8 * (8 * ps.k - at);
       const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
-      __builtin_memcpy(&sa_next, sa_row + at, 8);
-      __builtin_memcpy(&sb_next, sb_row + at, 8);
+      typedef uint64_t __attribute__((aligned(2))) any_u64;
+      sa_next = *global_ptr<any_u64>(sa_row + at);
+      sb_next = *global_ptr<any_u64>(sb_row + at);
       sa_next = sa_next >> past | fill;
       sb_next = sb_next >> past | fill;
+    }
+  };
+  auto move_scales = [&]() {
+    if constexpr (kF4) {
+      if (move(ps) && ps.n) open_scales();
     }
   };
   auto put_scales = [&](uint32_t slot) {
@@ -374,17 +404,17 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       if (64 * TB >= kThreads || t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
     }
   };
-  // CODES: the scales of a unit that begins at stage q.  An odd row whose scales
-  // fill no whole dwords begins two bytes earlier.
+  // CODES: the scales of a unit that begins where A's loads are.  An odd row
+  // whose scales fill no whole dwords begins two bytes earlier.
   uint32_t unit = 0, unit_read = 0;                 // slots written next, read
-  auto load_unit = [&](const Stage& q) {
+  auto load_unit = [&]() {
     if constexpr (kCodes) {
-      if (q.n && (q.k & 3) == 0) {
-        const Tile x = tile_of(q.i);
+      if (pa.n && (pa.k & 3) == 0) {
+        const Tile x = tile_of(pa.i);
         const Scales s = job.a_scales(x);
         const int valid = min(job.a(x).valid, 64 * TA);
-        const uint8_t* base = uniform(s.at + 2 * q.k);
-        const uint32_t limit = valid * s.bytes - 2 * q.k;
+        const uint8_t* base = uniform(s.at + 2 * pa.k);
+        const uint32_t limit = valid * s.bytes - 2 * pa.k;
 #pragma unroll
         for (int i = 0; i < 3 * TA / 4 + (TA % 4 != 0); ++i) {
           const int piece = wave + 4 * i;            // 64 rows of a dword
@@ -392,28 +422,30 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
           const uint32_t off = r < valid && j < 3 ? r * s.bytes - (r * s.bytes & 2) + 4 * j : kMasked;
           if (piece < 3 * TA) load_lds4(lds0 + R::kScaleBase + unit * R::kScaleSlot + 256 * piece, base, limit, off);
         }
-        unit = (unit + 1) & 3;
+        unit = (unit + 1) & 7;
       }
     }
   };
 
-  open_scales(p[0]);
-  fetch_scales(p[0]);
-  put_scales(0);
-  open_scales(p[1]);
-  fetch_scales(p[1]);
+  if constexpr (kF4) {
+    open_scales();
+    fetch_scales();
+    put_scales(0);
+    move_scales();
+    fetch_scales();
+  }
   // the rings' first stages; what the first stage needs comes first
 #pragma unroll
   for (int v = 0; v < R::SA - 1; ++v) {
     if (v < R::SB - 1) {
-      open_b(p[v]);
 #pragma unroll
-      for (int i = 0; i < kNB; ++i) load_b(p[v], i, v);
+      for (int i = 0; i < kNB; ++i) load_b(i, v);
+      move_b();
     }
-    open_a(p[v]);
-    load_unit(p[v]);
+    load_unit();
 #pragma unroll
-    for (int i = 0; i < kNA; ++i) load_a(p[v], i, v);
+    for (int i = 0; i < kNA; ++i) load_a(i, v);
+    move_a();
   }
   Acc<TA, TB> acc;
 
@@ -460,10 +492,10 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   };
   // CODES: the lane's 32 codes of a stage and their scale, byte `at` of the
   // row's 12
-  auto read_raw = [&](int i, uint32_t slot, const Stage& q) {
+  auto read_raw = [&](int i, uint32_t slot, int k) {
     if constexpr (kCodes) {
       raw[i] = lds_read<u32x4>(lds, slot * R::kA + (arow >> 2) + i * 1024 + 16 * (half ^ ((l >> 3) & 1)));
-      const int at = 2 * (q.k & 3) + half + ((l & 1) & (q.steps >> 6)) * 2;
+      const int at = 2 * (k & 3) + half + ((l & 1) & (columns >> 6)) * 2;
       scale[i] = scale_of(lds_read<uint8_t>(lds, R::kScaleBase + unit_read * R::kScaleSlot + (arow >> 5) + i * 128 +
                                                      (at >> 2) * 256 * TA + (at & 3)));
     }
@@ -517,8 +549,8 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   auto loads = [&](int c) {
 #pragma unroll
     for (int i = c * kAll / kSpread; i < min((c + 1) * kAll / kSpread, kAll); ++i) {
-      if (i < kNB) load_b(p[R::SB - 1], i, bl);
-      else load_a(p[R::SA - 1], i - kNB, al);
+      if (i < kNB) load_b(i, bl);
+      else load_a(i - kNB, al);
     }
   };
   constexpr std::integral_constant<int, 0> s0;
@@ -545,28 +577,26 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   read_scales(0, sa, sb);
 #pragma unroll
   for (int i = 0; i < TA; ++i) {
-    read_raw(i, 0, p[0]);
+    read_raw(i, 0, 0);
     read_a(0, i, 0);
   }
 #pragma unroll
   for (int j = 0; j < TB; ++j) read_b(0, j, 0);
-  put_scales(1);
-  open_scales(p[R::kAhead]);
-  fetch_scales(p[R::kAhead]);
-  open_b(p[R::SB - 1]);
-  open_a(p[R::SA - 1]);
-  load_unit(p[R::SA - 1]);
+  if constexpr (kF4) {
+    put_scales(1);
+    move_scales();
+    fetch_scales();
+  }
+  load_unit();
 #pragma unroll
   for (int c = 0; c < 4; ++c) loads(c);
-  while (p[0].n) {
+  do {
 #pragma unroll
     for (int i = 0; i < TA; ++i)
 #pragma unroll
       for (int j = 0; j < TB; ++j)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-    const int done = p[0].i;
-    int left = p[0].n;
     do {
       step(s0);
       step(s1);
@@ -578,7 +608,10 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
-          for (int j = 0; j < TB; ++j) asm volatile("" :: "a"(acc[i][j][0]));
+          for (int j = 0; j < TB; ++j) {
+            if constexpr (TA == 4) asm volatile("" :: "a"(acc[i][j][0]));
+            else asm volatile("" :: "v"(acc[i][j][0]));
+          }
       }
 #endif
       // every load of the next stage has arrived; this stage's slots are free
@@ -588,21 +621,18 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       bc = next(bc, R::SB);
       bl = next(bl, R::SB);
       sc ^= 1;
-#pragma unroll
-      for (int j = 0; j < R::kAhead; ++j) p[j] = p[j + 1];
-      p[R::kAhead] = after(p[R::kAhead]);
-      // (a new tile was taken: the one after it has to be there in turn; the
-      // tile being finished is kAhead + 1 tiles behind at most)
-      if (p[R::kAhead].k == 0 && p[R::kAhead].n && made <= p[R::kAhead].i + 1) make();
-      // scales of the stage after the next into LDS, whose slot the barrier
-      // freed, those of the one behind it into registers
-      put_scales(sc ^ 1);
-      open_scales(p[R::kAhead]);
-      fetch_scales(p[R::kAhead]);
-      open_b(p[R::SB - 1]);
-      open_a(p[R::SA - 1]);
-      load_unit(p[R::SA - 1]);
-      if (kCodes && (p[0].k & 3) == 0) unit_read = (unit_read + 1) & 3;
+      k_now = left > 1 ? k_now + 1 : 0;             // (of the next stage)
+      move_b();
+      move_a();
+      if constexpr (kF4) {
+        // scales of the stage after the next into LDS, whose slot the barrier
+        // freed, those of the one behind it into registers
+        put_scales(sc ^ 1);
+        move_scales();
+        fetch_scales();
+      }
+      load_unit();
+      if (kCodes && (k_now & 3) == 0) unit_read = (unit_read + 1) & 7;
       read_scales(sc, sa1, sb1);
       // (after the last stage of all: reads that are not multiplied)
 #pragma unroll
@@ -610,7 +640,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         loads(c);
         if (c == 0) {
 #pragma unroll
-          for (int i = 0; i < TA; ++i) read_raw(i, ac, p[0]);
+          for (int i = 0; i < TA; ++i) read_raw(i, ac, k_now);
         }
 #pragma unroll
         for (int i = 0; i < TA; ++i)
@@ -628,8 +658,12 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         for (int j = 0; j < TB; ++j) sb[j] = sb1[j];
       }
     } while (--left);
-    job.store(tile_of(done), acc);
-  }
+    job.store(tile_of(tile), acc);
+    // the next tile; what is read ahead of it has one more to go to
+    const Place now = begin(++tile);
+    left = now.n;
+    while (made <= tile + R::kAhead + 1) make();
+  } while (left);
   // the LDS must not be handed on with loads in flight, nor while another wave
   // reads it
   stage_barrier<0>();
@@ -672,7 +706,7 @@ __device__ __forceinline__ void store_rows(Acc<TA, TB>& acc, T* out, int64_t ld,
         const auto x = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
         const auto y = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
         if (row < rows)
-          *reinterpret_cast<u32x4*>(to + 32 * i + 16 * q) =
+          *global_ptr<u32x4>(to + 32 * i + 16 * q) =
               u32x4{(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
       }
     }
