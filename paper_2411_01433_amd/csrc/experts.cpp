@@ -218,7 +218,7 @@ moe_status moe_gradients_init(int32_t n, const void* const* grads, void* const* 
     }
     auto al = [](size_t b) { return (b + 255) & ~(size_t)255; };
     const size_t count = pieces.size();
-    const size_t o_sums = al(count * sizeof(GradPiece)), o_done = o_sums + al(count * sizeof(double));
+    const size_t o_sums = al(count * sizeof(GradPiece)), o_done = o_sums + al(kGradBlocks * sizeof(double));
     he = hipMalloc(&h->arena, o_done + 256);
     if (he != hipSuccess) {
       delete h;
@@ -227,7 +227,8 @@ moe_status moe_gradients_init(int32_t n, const void* const* grads, void* const* 
     }
     char* base = static_cast<char*>(h->arena);
     h->list = {reinterpret_cast<const GradPiece*>(base), reinterpret_cast<double*>(base + o_sums),
-               reinterpret_cast<unsigned*>(base + o_done), (int32_t)count};
+               reinterpret_cast<unsigned*>(base + o_done), (int32_t)count,
+               (int32_t)std::min<size_t>(count, kGradBlocks)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     he = hipMemcpyAsync(base, pieces.data(), count * sizeof(GradPiece), hipMemcpyHostToDevice, s);
     const uint32_t zero = 0;
@@ -253,16 +254,13 @@ moe_status moe_gradients_init(int32_t n, const void* const* grads, void* const* 
   return MOE_OK;
 }
 
-// The steps of a handle's calls; the checks were made.
-static moe_status gradients_run(moe_gradients_t g, bool sum, bool scale, float max_norm,
-                                float* norm, void* stream) {
-  hipError_t he = hipSetDevice(g->device);
-  if (he != hipSuccess) return ehfail(he, "hipSetDevice");
-  const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (sum) he = launch_gradients_norm(g->list, norm, s);
-  if (he == hipSuccess && scale) he = launch_gradients_scale(g->list, max_norm, norm, s);
-  if (he != hipSuccess) return ehfail(he, "gradient kernel launch");
-  return MOE_OK;
+// After the checks: the handle's device, and what a launch answered.
+static moe_status on_device(moe_gradients_t g) {
+  const hipError_t he = hipSetDevice(g->device);
+  return he == hipSuccess ? MOE_OK : ehfail(he, "hipSetDevice");
+}
+static moe_status launched(hipError_t he) {
+  return he == hipSuccess ? MOE_OK : ehfail(he, "gradient kernel launch");
 }
 
 static moe_status check_gradients(moe_gradients_t g, float max_norm, const float* norm) {
@@ -276,19 +274,23 @@ static moe_status check_gradients(moe_gradients_t g, float max_norm, const float
 }
 
 moe_status moe_gradients_norm(moe_gradients_t g, float* norm, void* stream) {
-  const moe_status st = check_gradients(g, 1.0f, norm);
-  return st != MOE_OK ? st : gradients_run(g, true, false, 1.0f, norm, stream);
+  moe_status st = check_gradients(g, 1.0f, norm);
+  if (st == MOE_OK) st = on_device(g);
+  return st != MOE_OK ? st : launched(launch_gradients_norm(g->list, norm, static_cast<hipStream_t>(stream)));
 }
 
 moe_status moe_gradients_scale(moe_gradients_t g, float max_norm, const float* norm, void* stream) {
-  const moe_status st = check_gradients(g, max_norm, norm);
+  moe_status st = check_gradients(g, max_norm, norm);
+  if (st == MOE_OK) st = on_device(g);
   return st != MOE_OK ? st
-                      : gradients_run(g, false, true, max_norm, const_cast<float*>(norm), stream);
+                      : launched(launch_gradients_scale(g->list, max_norm, norm, static_cast<hipStream_t>(stream)));
 }
 
 moe_status moe_gradients_clip(moe_gradients_t g, float max_norm, float* norm, void* stream) {
-  const moe_status st = check_gradients(g, max_norm, norm);
-  return st != MOE_OK ? st : gradients_run(g, true, true, max_norm, norm, stream);
+  moe_status st = check_gradients(g, max_norm, norm);
+  if (st == MOE_OK) st = on_device(g);
+  return st != MOE_OK ? st
+                      : launched(launch_gradients_clip(g->list, max_norm, norm, static_cast<hipStream_t>(stream)));
 }
 
 moe_status moe_gradients_destroy(moe_gradients_t g) {

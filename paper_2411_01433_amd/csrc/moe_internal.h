@@ -322,13 +322,14 @@ struct GradPiece {
   void* out;
   int32_t n, type;
 };
-constexpr int kPieceElems = 1 << 15;
+constexpr int kPieceElems = 1 << 13;
+constexpr int kGradBlocks = 2048;
 
 struct GradList {
   const GradPiece* pieces;  // device
-  double* sums;             // one per piece
-  unsigned* done;           // pieces summed (zero between launches)
-  int32_t n;
+  double* sums;             // one per block
+  unsigned* done;           // blocks that left their sum (zero between launches)
+  int32_t n, blocks;        // pieces; blocks of a launch
 };
 
 // Static scratch of the allocation-free decode step (noalloc.hip): its size,
@@ -376,6 +377,7 @@ hipError_t launch_mx_product(const Grouped& g, const void* x, const uint8_t* xs,
 hipError_t launch_gradients_norm(const GradList& g, float* norm, hipStream_t s);
 hipError_t launch_gradients_scale(const GradList& g, float max_norm, const float* norm,
                                   hipStream_t s);
+hipError_t launch_gradients_clip(const GradList& g, float max_norm, float* norm, hipStream_t s);
 hipError_t launch_decode_up(const ExpertEntry* table, const WorkList* wl,
                             const int32_t* perm, const f16* x, f16* h,
                             int T, int d, int f, int K, int max_groups,

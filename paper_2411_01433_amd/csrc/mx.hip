@@ -12,6 +12,9 @@ namespace moe {
 
 namespace {
 
+constexpr int kThreads = 256, kChunks = 4;
+constexpr int kPerBlock = kThreads / 4 * kChunks;  // blocks of 32 columns
+
 template <class T> struct Pair;
 template <> struct Pair<f16> {
   typedef f16 x2 __attribute__((ext_vector_type(2)));
@@ -39,49 +42,53 @@ __device__ inline float scale_of(uint32_t byte) {
 
 }  // namespace
 
-// One thread per block of 32 columns.
+// Four lanes share a block, 8 columns each, so that loads and stores are
+// contiguous over a wave; chunk c of lane l is columns 8 (l % 4) .. + 7 of block
+// 16 c + l / 4 of the wave's 64.
 template <class T>
-__global__ __launch_bounds__(256) void mx_quantize_kernel(const T* v, int64_t n_blocks,
-                                                          uint8_t* codes, uint8_t* scales,
-                                                          T* values) {
+__global__ __launch_bounds__(kThreads) void mx_quantize_kernel(const T* v, int64_t n_blocks,
+                                                               uint8_t* codes, uint8_t* scales,
+                                                               T* values) {
   typedef typename Pair<T>::x2 x2;
-  const int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (b >= n_blocks) return;
-  u32x4 in[4];
-  uint32_t top = 0;
+  const int lane = threadIdx.x & 63;
+  const int64_t b0 = (int64_t)blockIdx.x * kPerBlock + (threadIdx.x >> 6) * (16 * kChunks) + (lane >> 2);
+  u32x4 in[kChunks];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    in[i] = reinterpret_cast<const u32x4*>(v)[4 * b + i];
+  for (int c = 0; c < kChunks; ++c) {
+    const int64_t b = b0 + 16 * c;
+    in[c] = b < n_blocks ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v) + 4 * b + (lane & 3))
+                         : u32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int64_t b = b0 + 16 * c;
+    uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t u = in[i][j];
+      const uint32_t u = in[c][j];
       const x2 p = __builtin_bit_cast(x2, u);
-      top = max(top, __builtin_bit_cast(uint32_t, (float)p.x) & 0x7FFFFFFFu);
-      top = max(top, __builtin_bit_cast(uint32_t, (float)p.y) & 0x7FFFFFFFu);
+      const uint32_t lo = __builtin_bit_cast(uint32_t, (float)p.x) & 0x7FFFFFFFu;
+      const uint32_t hi = __builtin_bit_cast(uint32_t, (float)p.y) & 0x7FFFFFFFu;
+      top = max(top, max(lo, hi));
     }
-  }
-  const uint32_t field = top >> 23;
-  const uint32_t byte = field == 255 ? 255 : field < 2 ? 0 : field - 2;
-  const float s = scale_of(byte);
-  u32x4 out;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t c = 0;
-    c = Pair<T>::template code<0>(c, in[i][0], s);
-    c = Pair<T>::template code<1>(c, in[i][1], s);
-    c = Pair<T>::template code<2>(c, in[i][2], s);
-    c = Pair<T>::template code<3>(c, in[i][3], s);
-    out[i] = c;
-  }
-  reinterpret_cast<u32x4*>(codes)[b] = out;
-  scales[b] = (uint8_t)byte;
-  if (values) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t c = out[i];
-      reinterpret_cast<u32x4*>(values)[4 * b + i] =
-          u32x4{Pair<T>::template value<0>(c, s), Pair<T>::template value<1>(c, s),
-                Pair<T>::template value<2>(c, s), Pair<T>::template value<3>(c, s)};
+    top = dpp_max<0xB1>(top);  // quad_perm [1,0,3,2]
+    top = dpp_max<0x4E>(top);  // quad_perm [2,3,0,1]
+    const uint32_t field = top >> 23;
+    const uint32_t byte = field == 255 ? 255 : field < 2 ? 0 : field - 2;
+    const float s = scale_of(byte);
+    uint32_t k = 0;
+    k = Pair<T>::template code<0>(k, in[c][0], s);
+    k = Pair<T>::template code<1>(k, in[c][1], s);
+    k = Pair<T>::template code<2>(k, in[c][2], s);
+    k = Pair<T>::template code<3>(k, in[c][3], s);
+    if (b < n_blocks) {
+      reinterpret_cast<uint32_t*>(codes)[4 * b + (lane & 3)] = k;
+      if ((lane & 3) == 0) scales[b] = (uint8_t)byte;
+      if (values)
+        __builtin_nontemporal_store(
+            u32x4{Pair<T>::template value<0>(k, s), Pair<T>::template value<1>(k, s),
+                  Pair<T>::template value<2>(k, s), Pair<T>::template value<3>(k, s)},
+            reinterpret_cast<u32x4*>(values) + 4 * b + (lane & 3));
     }
   }
 }
@@ -91,11 +98,11 @@ hipError_t launch_mx_quantize(const void* v, int type, int64_t rows, int64_t col
   const int64_t n = rows * (cols / kMxBlock);
   if (n == 0) return hipSuccess;
   // (a launch has less than 2^32 threads)
-  const unsigned blocks = (unsigned)((n + 255) / 256);
+  const unsigned blocks = (unsigned)((n + kPerBlock - 1) / kPerBlock);
   if (type == TYPE_F16)
-    mx_quantize_kernel<<<blocks, 256, 0, s>>>((const f16*)v, n, codes, scales, (f16*)values);
+    mx_quantize_kernel<<<blocks, kThreads, 0, s>>>((const f16*)v, n, codes, scales, (f16*)values);
   else
-    mx_quantize_kernel<<<blocks, 256, 0, s>>>((const bf16*)v, n, codes, scales, (bf16*)values);
+    mx_quantize_kernel<<<blocks, kThreads, 0, s>>>((const bf16*)v, n, codes, scales, (bf16*)values);
   return hipGetLastError();
 }
 
