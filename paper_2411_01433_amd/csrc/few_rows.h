@@ -39,13 +39,6 @@ constexpr uint32_t kXScale = kWScale + kWScaleArea, kXScaleArea = 16 * (128 + kS
 constexpr uint32_t kLdsFew = kXScale + kXScaleArea;  // two blocks per unit
 static_assert(2 * kLdsFew <= 160 * 1024, "LDS");
 
-// As load_lds, past the caches.
-__device__ inline void load_lds_stream(uint32_t lds, const uint8_t* base, uint32_t limit, uint32_t off) {
-  const uint64_t p = (uint64_t)(uintptr_t)base;
-  const u32x4 d = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, limit, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
-               :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
-}
 template <int N>
 __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
@@ -98,8 +91,8 @@ void few_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w
     const bool tail = CODED && K % 256 != 0;       // the last line is partial
     const uint32_t m0 = tail && 128 * k + chunk >= row_bytes ? kMasked : 0;
     const uint32_t m1 = tail && 128 * k + (chunk ^ 64) >= row_bytes ? kMasked : 0;
-    load_lds_stream(ring + slot * 2048, at, limit, off0 | m0);
-    load_lds_stream(ring + slot * 2048 + 1024, at, limit, off1 | m1);
+    load_lds<true>(ring + slot * 2048, at, limit, off0 | m0);
+    load_lds<true>(ring + slot * 2048 + 1024, at, limit, off1 | m1);
   };
 
   // Slabs: whole pieces, as many columns as the areas hold.

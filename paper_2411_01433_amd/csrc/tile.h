@@ -16,13 +16,14 @@
 // (ds_read_b64_tr_b16: four elements of a column).  What lies outside of the
 // matrices - rows and columns past the ends, reduction steps past the last -
 // is masked by the buffer's range check and arrives as zeros.  Codes beside a
-// partner of 16 bits (CODES) take 32 bytes of each row and become 16-bit
-// fragments after the read, each by two waves.
+// partner of 16 bits (CODES) come in units of four stages, whole lines too, and
+// become 16-bit fragments after the read, each by two waves.  Weights of tiles
+// of up to 128 rows, which few other tiles share, pass the caches by: 60 experts
+// of 1472 x 2048 with 89 rows each took 111 us without that, 97 with it.
 //
 // Bank conflicts.  ROWS: the 16-byte chunk c of row r sits at position
-// c ^ (r / 2 % 8).  COLS: 64-byte pieces are permuted by the row's last bits,
+// c ^ (r / 2 % 8), CODES likewise.  COLS: 64-byte pieces are permuted by the row's last bits,
 // so that the four rows that a half-wave reads 64 bytes of cover all banks.
-// CODES: a row's two chunks trade places in every second eight rows.
 //
 // Order of the reduction.  It is free as long as both operands agree: lane
 // half h takes steps 32 h + 8 s .. + 7 of the stage in step s = 0..3 (in MXFP4
@@ -59,12 +60,18 @@ constexpr uint32_t kMasked = 1u << 31;            // an offset outside of every 
 
 // 16 bytes per lane from base + off to LDS at lds + 16 * lane; zeros where
 // off >= limit.  lds, base and limit are wave-uniform.  m0 holds the LDS
-// address; one wait state is required between its write and the load.
+// address; one wait state is required between its write and the load.  STREAM:
+// what is read once, past the caches.
+template <bool STREAM = false>
 __device__ inline void load_lds(uint32_t lds, const uint8_t* base, uint32_t limit, uint32_t off) {
   const uint64_t p = (uint64_t)(uintptr_t)base;
   const u32x4 d = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, limit, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
+  if constexpr (STREAM)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+                 :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(off), "s"(d) : "memory", "m0");
 }
 
 // 4 bytes per lane to LDS at lds + 4 * lane, likewise.
@@ -127,15 +134,14 @@ struct Operand {
 // 1024 bytes of the slot from 1024 (w + 4 i) on.
 template <int KIND, int T>
 struct Loads {
-  static_assert(KIND != CODES || T % 2 == 0, "whole loads");
-  static constexpr int kN = KIND == CODES ? T / 2 : 2 * T;
+  static constexpr int kN = 2 * T;
   static constexpr uint32_t kSlot = 4096 * kN;
   uint32_t off[kN];
   const uint8_t* at;
   uint32_t limit;       // what of it may be read (0: nothing)
   uint32_t row_bytes;
 
-  // ROWS: the lane's 16 bytes of each row's 128 (of every load the same)
+  // ROWS, CODES: the lane's 16 bytes of each row's 128 (of every load the same)
   static __device__ inline uint32_t chunk(int wave) {
     const int l = threadIdx.x & 63;
     return 16 * ((l & 7) ^ ((4 * (wave & 1) + (l >> 4)) & 7));
@@ -153,25 +159,25 @@ struct Loads {
       if (KIND == COLS) {
         const int to = 64 * q + l, row = to / (8 * T), c = (to % (8 * T)) ^ piece(row);
         off[i] = 8 * c < o.valid ? (uint32_t)row * row_bytes + 16 * c : kMasked;
-      } else if (KIND == ROWS) {
+      } else {
         const int row = 8 * q + (l >> 3);
         off[i] = row < o.valid ? (uint32_t)row * row_bytes + chunk(wave) : kMasked;
-      } else {
-        const int row = 32 * q + (l >> 1), c = (l & 1) ^ ((row >> 3) & 1);
-        off[i] = row < o.valid ? (uint32_t)row * row_bytes + 16 * c : kMasked;
       }
     }
   }
   // to the next stage of the same tile, or (another) just opened
   __device__ inline void advance(bool another) {
-    at += another ? 0 : KIND == COLS ? (int64_t)kStage * row_bytes : KIND == CODES ? 32 : 128;
+    at += another ? 0 : KIND == COLS ? (int64_t)kStage * row_bytes : 128;
   }
   // `left` reduction steps from the stage's first on (0: none are read)
   __device__ inline void bound(int left) {
     limit = __builtin_amdgcn_readfirstlane(
         KIND == COLS ? max(0, min(left, kStage)) * row_bytes : left > 0 ? kMasked - 1 : 0);
   }
-  __device__ inline void load(int i, uint32_t lds, uint32_t mask) const { load_lds(lds, at, limit, off[i] | mask); }
+  template <bool STREAM>
+  __device__ inline void load(int i, uint32_t lds, uint32_t mask) const {
+    load_lds<STREAM>(lds, at, limit, off[i] | mask);
+  }
 };
 
 __device__ inline uint32_t as_u32(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
@@ -237,21 +243,28 @@ struct Ring {
   static constexpr int kScaleSlots = TYPE == F4 ? 2 : 8;
   static constexpr uint32_t kRoom = LDS - kScaleSlots * kScaleSlot;
   static constexpr int kBoth = (int)(kRoom / (kA + kB));
-  static constexpr int SB = TYPE == F4 ? 2 : kBoth > 6 ? 6 : kBoth;
-  static constexpr int SA = KA != CODES && TYPE != F4 && SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
+  // CODES: units of A, and stages of B ahead.  A unit's loads go out when the
+  // products begin the one SA - 1 before it, and these may have a stage each:
+  // no more stages of B than that may be in flight behind them.
+  static constexpr int kUnits = kRoom >= 3 * kA + 4 * kB ? 3 : 2;
+  static constexpr int kBeside = (int)((kRoom - kUnits * kA) / kB);
+  static constexpr int SB = TYPE == F4 ? 2 : KA == CODES ? (kBeside > kUnits + 1 ? kUnits + 1 : kBeside)
+                            : kBoth > 6 ? 6 : kBoth;
+  static constexpr int SA = KA == CODES ? kUnits : TYPE != F4 && SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
   static constexpr uint32_t kBBase = SA * kA, kScaleBase = kBBase + SB * kB;
   // (a tile of one stage has a slot of scales of its own, and the queue of
   // stream() holds the tile of the products and seven behind it)
   static_assert(SA <= 6 && SB <= 6, "stages ahead");
   static_assert(SB >= 2 && kScaleBase + kScaleSlots * kScaleSlot <= LDS, "LDS");
   // stages ahead of the products that anything is fetched for
-  static constexpr int kAhead = TYPE == F4 ? 2 : SA - 1;
+  static constexpr int kAhead = TYPE == F4 ? 2 : (SA > SB ? SA : SB) - 1;
   // loads that may be in flight when a stage ends: those of the stages after
-  // the next one
-  static constexpr int kPending = (SA - 2) * Loads<KA, TA>::kN + (SB - 2) * Loads<KB, TB>::kN;
+  // the next one (CODES: B's; a unit of A has as many stages to arrive)
+  static constexpr int kPending = (KA == CODES ? 0 : SA - 2) * Loads<KA, TA>::kN + (SB - 2) * Loads<KB, TB>::kN;
   // quarters (of 16 between two barriers) that the loads are spread over: all
   // of a ring of two have to arrive within these
-  static constexpr int kSpread = SA == 2 ? 4 : 12;
+  static constexpr int kSpread = SB == 2 && SA == 2 ? 4 : 12;
+  static constexpr bool kStream = TB <= (TA == 4 ? 2 : 1);
 };
 
 // The accumulators of a wave: acc[i][j] is A tile i, B tile j of its own.
@@ -333,6 +346,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   Place pa = begin(0), pb = pa;
   if (pa.n == 0) return;
   int tile = 0, left = pa.n, k_now = 0;             // of the products: stages left, stage
+  if (kCodes) pa.n = (pa.n + 3) >> 2;               // A's stages are units
   // (of all tiles the same where codes or scales are read)
   const int columns = pa.steps;
 
@@ -344,9 +358,10 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   lb.bound(pb.steps);
   auto move_a = [&]() {
     const bool another = move(pa);
+    if (kCodes && another) pa.n = (pa.n + 3) >> 2;
     if (another && pa.n) la.open(job.a(tile_of(pa.i)), wave);
     la.advance(another);
-    la.bound(pa.steps - (kF4 ? 256 : kStage) * pa.k);
+    la.bound(pa.steps - (kF4 || kCodes ? 256 : kStage) * pa.k);
   };
   auto move_b = [&]() {
     const bool another = move(pb);
@@ -357,12 +372,13 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   // In MXFP4 a row's last line may be partial: the chunks behind it are masked
   // (of either operand, whose loads are at the same stage).
   auto load_a = [&](int i, uint32_t slot) {
-    const uint32_t mask = kF4 && (uint32_t)(128 * pa.k) + la.chunk(wave) >= (uint32_t)columns / 2 ? kMasked : 0;
-    la.load(i, lds0 + slot * R::kA + (wave + 4 * i) * 1024, mask);
+    const uint32_t mask =
+        (kF4 || kCodes) && (uint32_t)(128 * pa.k) + la.chunk(wave) >= (uint32_t)columns / 2 ? kMasked : 0;
+    la.template load<R::kStream>(i, lds0 + slot * R::kA + (wave + 4 * i) * 1024, mask);
   };
   auto load_b = [&](int i, uint32_t slot) {
     const uint32_t mask = kF4 && (uint32_t)(128 * pb.k) + la.chunk(wave) >= (uint32_t)columns / 2 ? kMasked : 0;
-    lb.load(i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
+    lb.template load<false>(i, lds0 + R::kBBase + slot * R::kB + (wave + 4 * i) * 1024, mask);
   };
 
   // F4: scales of 256 columns (8 bytes) of the thread's row of A and of B, into
@@ -404,17 +420,17 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       if (64 * TB >= kThreads || t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
     }
   };
-  // CODES: the scales of a unit that begins where A's loads are.  An odd row
+  // CODES: the scales of the unit where A's loads are.  An odd row
   // whose scales fill no whole dwords begins two bytes earlier.
   uint32_t unit = 0, unit_read = 0;                 // slots written next, read
   auto load_unit = [&]() {
     if constexpr (kCodes) {
-      if (pa.n && (pa.k & 3) == 0) {
+      if (pa.n) {
         const Tile x = tile_of(pa.i);
         const Scales s = job.a_scales(x);
         const int valid = min(job.a(x).valid, 64 * TA);
-        const uint8_t* base = uniform(s.at + 2 * pa.k);
-        const uint32_t limit = valid * s.bytes - 2 * pa.k;
+        const uint8_t* base = uniform(s.at + 8 * pa.k);
+        const uint32_t limit = valid * s.bytes - 8 * pa.k;
 #pragma unroll
         for (int i = 0; i < 3 * TA / 4 + (TA % 4 != 0); ++i) {
           const int piece = wave + 4 * i;            // 64 rows of a dword
@@ -436,16 +452,18 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   }
   // the rings' first stages; what the first stage needs comes first
 #pragma unroll
-  for (int v = 0; v < R::SA - 1; ++v) {
+  for (int v = 0; v < R::kAhead; ++v) {
     if (v < R::SB - 1) {
 #pragma unroll
       for (int i = 0; i < kNB; ++i) load_b(i, v);
       move_b();
     }
-    load_unit();
+    if (v < R::SA - 1) {
+      load_unit();
 #pragma unroll
-    for (int i = 0; i < kNA; ++i) load_a(i, v);
-    move_a();
+      for (int i = 0; i < kNA; ++i) load_a(i, v);
+      move_a();
+    }
   }
   Acc<TA, TB> acc;
 
@@ -494,7 +512,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   // row's 12
   auto read_raw = [&](int i, uint32_t slot, int k) {
     if constexpr (kCodes) {
-      raw[i] = lds_read<u32x4>(lds, slot * R::kA + (arow >> 2) + i * 1024 + 16 * (half ^ ((l >> 3) & 1)));
+      raw[i] = lds_read<u32x4>(lds, slot * R::kA + arow + i * 4096 + 16 * ((2 * (k & 3) + half) ^ sw));
       const int at = 2 * (k & 3) + half + ((l & 1) & (columns >> 6)) * 2;
       scale[i] = scale_of(lds_read<uint8_t>(lds, R::kScaleBase + unit_read * R::kScaleSlot + (arow >> 5) + i * 128 +
                                                      (at >> 2) * 256 * TA + (at & 3)));
@@ -545,7 +563,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   uint32_t al = R::SA - 1, bl = R::SB - 1;          // slots loaded next
   // Quarter c's share (of 16) of the loads issued between two barriers: B's
   // first, whose ring is never the deeper one.
-  constexpr int kAll = kNB + kNA, kSpread = R::kSpread;
+  constexpr int kAll = kNB + (kCodes ? 0 : kNA), kSpread = R::kSpread;
   auto loads = [&](int c) {
 #pragma unroll
     for (int i = c * kAll / kSpread; i < min((c + 1) * kAll / kSpread, kAll); ++i) {
@@ -587,7 +605,13 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     move_scales();
     fetch_scales();
   }
-  load_unit();
+  // CODES: the unit SA - 1 units ahead, at once when the products begin one
+  auto load_ahead = [&]() {
+    load_unit();
+#pragma unroll
+    for (int i = 0; i < kNA; ++i) load_a(i, al);
+  };
+  if constexpr (kCodes) load_ahead();
 #pragma unroll
   for (int c = 0; c < 4; ++c) loads(c);
   do {
@@ -616,14 +640,18 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
 #endif
       // every load of the next stage has arrived; this stage's slots are free
       stage_barrier<R::kPending>();
-      ac = next(ac, R::SA);
-      al = next(al, R::SA);
       bc = next(bc, R::SB);
       bl = next(bl, R::SB);
       sc ^= 1;
       k_now = left > 1 ? k_now + 1 : 0;             // (of the next stage)
       move_b();
-      move_a();
+      if (!kCodes || (k_now & 3) == 0) {
+        ac = next(ac, R::SA);
+        al = next(al, R::SA);
+        unit_read = (unit_read + 1) & 7;
+        move_a();
+        if (kCodes) load_ahead();
+      }
       if constexpr (kF4) {
         // scales of the stage after the next into LDS, whose slot the barrier
         // freed, those of the one behind it into registers
@@ -631,8 +659,6 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         move_scales();
         fetch_scales();
       }
-      load_unit();
-      if (kCodes && (k_now & 3) == 0) unit_read = (unit_read + 1) & 7;
       read_scales(sc, sa1, sb1);
       // (after the last stage of all: reads that are not multiplied)
 #pragma unroll
