@@ -234,11 +234,18 @@ struct Items {
   }
 };
 
-// Whether blocks of 256 columns and rows are enough to fill the chip.
-inline bool large_blocks(const Grouped& g, int cols) {
+// Whether blocks of 256 columns and rows fill the chip, and the experts' rows
+// fill enough of them (`rows` each on average).  Us with large / small blocks, 16
+// experts of 6400 x 4096: forward at 32 rows each 178 / 166, 64 183 / 180, 128
+// 202 / 224; d_x at 8 rows 413 / 422, 64 425 / 479; MXFP4 on both sides at 16
+// rows 61 / 68, 128 84 / 98; MXFP4 beside 16 bits, whose blocks of few rows wait
+// for instructions more than for memory, at 64 rows 134 / 109, 256 278 / 264, 512
+// 413 / 474.
+inline bool large_blocks(const Grouped& g, int cols, int rows) {
   const int active = g.E < g.n ? g.E : g.n;
   const int tiles = g.n / 256 + active / 2;
-  return (int64_t)(tiles > active ? tiles : active) * ((cols + 255) / 256) >= 256;
+  return (int64_t)(tiles > active ? tiles : active) * ((cols + 255) / 256) >= 256 &&
+         g.n >= (int64_t)rows * active;
 }
 
 }  // namespace moe

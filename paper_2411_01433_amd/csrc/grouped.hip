@@ -200,7 +200,7 @@ void dw_kernel(Grouped g, const void* dy, const void* x, float* dw, bool accumul
 template <int TYPE, bool BACK>
 void launch_rows(const Grouped& g, const void* in, const void* w, void* out, hipStream_t s) {
   const int cols = BACK ? g.d_in : g.d_out;
-  if (large_blocks(g, cols))
+  if (large_blocks(g, cols, BACK ? 0 : 64))
     rows_kernel<TYPE, 4, BACK><<<kBlocks<4>, kThreads, 0, s>>>(g, in, w, out, (cols + 255) / 256);
   else
     rows_kernel<TYPE, 2, BACK><<<kBlocks<2>, kThreads, 0, s>>>(g, in, w, out, (cols + 127) / 128);

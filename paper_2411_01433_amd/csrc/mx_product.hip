@@ -68,7 +68,7 @@ void mx_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w,
 template <int TYPE, bool CODED>
 void launch(const Grouped& g, const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
             void* y, hipStream_t s) {
-  if (large_blocks(g, g.d_out))
+  if (large_blocks(g, g.d_out, CODED ? 0 : 384))
     mx_kernel<TYPE, 4, CODED><<<kBlocks<4>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 255) / 256);
   else
     mx_kernel<TYPE, 2, CODED><<<kBlocks<2>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 127) / 128);
