@@ -382,8 +382,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   };
 
   // F4: scales of 256 columns (8 bytes) of the thread's row of A and of B, into
-  // registers; a stage later to LDS.  Past the row (256 columns at least): 2^0.
-  // No branch: the compiler would move products across it.
+  // registers; a stage later to LDS.  Past the row: 2^0.
   const int t = threadIdx.x;
   const uint8_t *sa_row = nullptr, *sb_row = nullptr;
   uint64_t sa_next = 0, sb_next = 0;
@@ -399,13 +398,17 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   auto fetch_scales = [&]() {
     if constexpr (kF4) {
       // (behind the last stage: the last tile's first ones again)
-      const int bytes = columns / 32, at = min(8 * ps.k, bytes - 8), past = 8 * (8 * ps.k - at);
-      const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
-      typedef uint64_t __attribute__((aligned(2))) any_u64;
-      sa_next = *global_ptr<any_u64>(sa_row + at);
-      sb_next = *global_ptr<any_u64>(sb_row + at);
-      sa_next = sa_next >> past | fill;
-      sb_next = sb_next >> past | fill;
+      const int bytes = columns / 32;
+      if (bytes < 8) {
+        sa_next = scale_unit(sa_row, bytes, 0);
+        sb_next = scale_unit(sb_row, bytes, 0);
+      } else {
+        const int at = min(8 * ps.k, bytes - 8), past = 8 * (8 * ps.k - at);
+        const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
+        typedef uint64_t __attribute__((aligned(2))) any_u64;
+        sa_next = *global_ptr<any_u64>(sa_row + at) >> past | fill;
+        sb_next = *global_ptr<any_u64>(sb_row + at) >> past | fill;
+      }
     }
   };
   auto move_scales = [&]() {
