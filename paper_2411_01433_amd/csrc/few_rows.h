@@ -215,16 +215,30 @@ void few_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w
   }
 }
 
-// Whether a call goes this way, and the columns of a block.
+// Whether a call goes this way: up to 8 rows per expert on average.  Us here / on
+// tiles of 64 rows and more, 16 experts of 6400 x 4096: 2 rows each 115 / 128, 8
+// rows 153 / 169, 16 rows 195 / 168; W in MXFP4 48 / 73, 75 / 85, 118 / 86; x in
+// MXFP4 too, 8 rows 54 / 67, 16 rows 71 / 61.
 inline bool takes(const Grouped& g) { return g.n <= 8 * (int64_t)g.E; }
+
+// Whether the waves of a block share its columns: for calls of few blocks, and
+// where both operands are in MXFP4 only if the rows are long, as a stage takes
+// 256 of their columns at once.  Us with / without, one row for each of 2
+// experts: 4096 x 4096 12.9 / 15.8, 6400 x 4096 21.7 / 20.0, 6400 x 1024 10.2 /
+// 7.3, 4096 x 16384 44 / 55; W in MXFP4, 4096 x 4096 7.9 / 9.5, 5120 x 4096 11.6
+// / 9.6, 4096 x 16384 18 / 29; x too (quantised before: 5), 2048 x 4096 13.2 /
+// 12.2, 2048 x 16384 12.9 / 26.3.
+inline bool splits(const Grouped& g, bool both) {
+  const int active = g.E < g.n ? g.E : g.n;
+  return (int64_t)active * (g.d_out / 64) < 160 && (!both || g.d_in >= 8192);
+}
 
 template <int TYPE, bool CODED, bool BOTH>
 void launch(const Grouped& g, const void* x, const void* xs, const void* w, const void* ws, void* y,
             hipStream_t s) {
   const uint8_t *xb = static_cast<const uint8_t*>(x), *sb = static_cast<const uint8_t*>(xs);
   const uint8_t *wb = static_cast<const uint8_t*>(w), *tb = static_cast<const uint8_t*>(ws);
-  const int active = g.E < g.n ? g.E : g.n;
-  const bool split = (int64_t)active * (g.d_out / 64) < 256;
+  const bool split = splits(g, BOTH);
   const int parts = g.d_out / (split ? 16 : 64);
   const unsigned blocks = row_tile_blocks(g, kRowsMax, parts);
   if (split) few_kernel<TYPE, CODED, BOTH, true><<<blocks, kThreads, 0, s>>>(g, xb, sb, wb, tb, y, parts);

@@ -191,8 +191,20 @@ def test_product(counts, d_in, d_out, extra, dtype, act):
     P.mx_product(x, wc, ws, again, count, x_scales)
     assert torch.equal(again[:n], y[:n])
     if E == 1:
-        P.mx_product(x, wc, ws, again, None, x_scales)
-        assert torch.equal(again, y)
+        P.mx_product(x, wc, ws, again, None, x_scales)  # (takes the rows behind too)
+        assert torch.equal(again[:n], y[:n])
+
+
+@pytest.mark.parametrize("act", ["16", "4"])
+@pytest.mark.parametrize("counts,d_in,d_out,extra", [
+    ([1], 8192, 64, 0),
+    ([3, 0, 16, 0, 1], 8256, 192, 2),
+    ([0, 2, 11], 20544, 128, 0),
+    ([40], 16448, 192, 1),
+])
+def test_rows_of_many_columns(counts, d_in, d_out, extra, act):
+    """Blocks whose waves share the columns, and several slabs of them."""
+    test_product(counts, d_in, d_out, extra, torch.bfloat16, act)
 
 
 @pytest.mark.parametrize("rows", [1, 3, 40, 300])
