@@ -11,7 +11,12 @@
 //
 // Bound by memory: the gradients pass twice, and are written once.  The scaling
 // takes the pieces from the end of the list on, since what the norm read last
-// is still in the caches.
+// is still in the caches (405 us instead of 438 below).
+//
+// Measured: 0.81 GB of gradients in 6 tensors 405 us, 118 for the norm (6.8 TB/s)
+// and 288 for the scaling (5.6 TB/s read and written); 2.6 MB in 48 tensors 7.9, of
+// which the two kernels take 3.2 and 3.9.  One element at a time they took 834 and
+// 35.  Stores pass the caches by: 405, others 454.
 #include "moe_internal.h"
 
 namespace moe {

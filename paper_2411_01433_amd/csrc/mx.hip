@@ -6,6 +6,11 @@
 // as the bits of its fp32 form, whose order is that of the numbers and ends in
 // infinity and NaN; its exponent field less 2 is the scale byte (a number
 // below 2^-126 has the field 0, and the byte 0 is the least).
+//
+// Bound by memory.  Four lanes share a block of columns: every load and store is
+// then contiguous over the wave (a thread per block took 57 us where this takes
+// 41, of 14336 x 4096: 267 MB with the values, 6.6 TB/s).  Four chunks per thread
+// cover the way to memory; with 1, 2 or 8 it took 43, 43 or 45.
 #include "moe_internal.h"
 
 namespace moe {
