@@ -400,10 +400,12 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   };
 
   // F4: scales of 256 columns (8 bytes) of the thread's row of A and of B, into
-  // registers; a stage later to LDS.  Past the row: 2^0.
+  // registers; a stage later to LDS, and not touched before: that would wait for
+  // them.  A row's last 8 bytes are moved into place then; past the row: 2^0.
   const int t = threadIdx.x;
   const uint8_t *sa_row = nullptr, *sb_row = nullptr;
   uint64_t sa_next = 0, sb_next = 0;
+  int past = 0;                                     // bits to move by
   Place ps = pa;
   auto open_scales = [&]() {
     if constexpr (kF4) {
@@ -421,11 +423,11 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         sa_next = scale_unit(sa_row, bytes, 0);
         sb_next = scale_unit(sb_row, bytes, 0);
       } else {
-        const int at = min(8 * ps.k, bytes - 8), past = 8 * (8 * ps.k - at);
-        const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
+        const int at = min(8 * ps.k, bytes - 8);
+        past = 8 * (8 * ps.k - at);
         typedef uint64_t __attribute__((aligned(2))) any_u64;
-        sa_next = *global_ptr<any_u64>(sa_row + at) >> past | fill;
-        sb_next = *global_ptr<any_u64>(sb_row + at) >> past | fill;
+        sa_next = *global_ptr<any_u64>(sa_row + at);
+        sb_next = *global_ptr<any_u64>(sb_row + at);
       }
     }
   };
@@ -437,8 +439,9 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   auto put_scales = [&](uint32_t slot) {
     const uint32_t at = R::kScaleBase + slot * R::kScaleSlot;
     if constexpr (kF4) {
-      if (64 * TA >= kThreads || t < 64 * TA) lds_write(lds, at + 8 * t, sa_next);
-      if (64 * TB >= kThreads || t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next);
+      const uint64_t fill = past ? 0x7F7F7F7F7F7F7F7Full << (64 - past) : 0;
+      if (64 * TA >= kThreads || t < 64 * TA) lds_write(lds, at + 8 * t, sa_next >> past | fill);
+      if (64 * TB >= kThreads || t < 64 * TB) lds_write(lds, at + 512 * TA + 8 * t, sb_next >> past | fill);
     }
   };
   // CODES: the scales of the unit where A's loads are.  An odd row
