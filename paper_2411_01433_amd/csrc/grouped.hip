@@ -50,7 +50,7 @@ struct RowJob {
   }
   __device__ inline void store(const Tile& t, Acc<TA, TB>& acc) const {
     const int col = t.part * 64 * TA;
-    store_rows<T, TA, TB>(acc, out + (int64_t)t.row * n_out() + col, n_out(), t.n, n_out() - col);
+    store_rows<T, BACK ? COLS : ROWS, TA, TB>(acc, out + (int64_t)t.row * n_out() + col, n_out(), t.n, n_out() - col);
   }
 };
 

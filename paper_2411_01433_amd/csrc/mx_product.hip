@@ -40,9 +40,10 @@ struct MxJob {
   }
   __device__ inline Scales a_scales(const Tile& t) const { return {ws + column(t) * (g.d_in / 32), g.d_in / 32}; }
   __device__ inline Scales b_scales(const Tile& t) const { return {xs + (int64_t)t.row * (g.d_in / 32), g.d_in / 32}; }
-  __device__ inline void store(const Tile& t, Acc<TA, TB>& acc) const {
+  template <int NA, int NB>
+  __device__ inline void store(const Tile& t, Acc<NA, NB>& acc) const {
     const int col = t.part * 64 * TA;
-    store_rows<T, TA, TB>(acc, y + (int64_t)t.row * g.d_out + col, g.d_out, t.n, g.d_out - col);
+    store_rows<T, CODED ? ROWS : CODES, NA, NB>(acc, y + (int64_t)t.row * g.d_out + col, g.d_out, t.n, g.d_out - col);
   }
 };
 

@@ -294,6 +294,17 @@ struct Scales {
   int bytes;
 };
 
+// How the waves share a block's tile: 2 x 2; beside CODES 4 x 1, so that each
+// code is converted once.
+template <int KA>
+struct Waves {
+  static constexpr bool kLine = KA == CODES;
+  static constexpr int kA(int ta) { return kLine ? ta / 2 : ta; }
+  static constexpr int kB(int tb) { return kLine ? 2 * tb : tb; }
+  static __device__ inline int a(int wave) { return kLine ? wave : wave >> 1; }
+  static __device__ inline int b(int wave) { return kLine ? 0 : wave & 1; }
+};
+
 // The products of a sequence of tiles, one after another through the same
 // rings: the loads of a tile's first stages are in flight while the products
 // of the last one's end and its results are stored.  Job:
@@ -311,7 +322,10 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   constexpr int kNA = Loads<KA, TA>::kN, kNB = Loads<KB, TB>::kN;
   const int l = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wa = wave >> 1, wb = wave & 1;
+  // the wave's place, and its tiles of 32
+  typedef Waves<KA> W;
+  constexpr int NA = W::kA(TA), NB = W::kB(TB);
+  const int wa = W::a(wave), wb = W::b(wave);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
 
   // The tiles to come: eight words each in the lanes of one register, tile i in
@@ -489,30 +503,30 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       move_a();
     }
   }
-  Acc<TA, TB> acc;
+  Acc<NA, NB> acc;
 
   // where the lane's fragments lie in a slot
   const int half = l >> 5, sw = (l >> 1) & 7;
   uint32_t cat[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) cat[s] = 16 * ((4 * half + s) ^ sw);
-  const uint32_t arow = (uint32_t)(wa * TA * 32 + (l & 31)) * 128;
-  const uint32_t brow = (uint32_t)(wb * TB * 32 + (l & 31)) * 128;
+  const uint32_t arow = (uint32_t)(wa * NA * 32 + (l & 31)) * 128;
+  const uint32_t brow = (uint32_t)(wb * NB * 32 + (l & 31)) * 128;
   // COLS: the lane's row within a step's four, and its 8 bytes of a tile
   const int cr = (l & 15) >> 2;
   auto col_at = [&](int T, int tile_) -> uint32_t {
     const int x = T % 2 ? cr >> 1 : cr;
     return (uint32_t)(32 * half + cr) * (128 * T) + 64 * (tile_ ^ x) + 32 * ((l >> 4) & 1) + 8 * (l & 3);
   };
-  uint32_t acol[TA], bcol[TB];
+  uint32_t acol[NA], bcol[NB];
 #pragma unroll
-  for (int i = 0; i < TA; ++i) acol[i] = KA == COLS ? col_at(TA, wa * TA + i) : 0;
+  for (int i = 0; i < NA; ++i) acol[i] = KA == COLS ? col_at(TA, wa * NA + i) : 0;
 #pragma unroll
-  for (int j = 0; j < TB; ++j) bcol[j] = KB == COLS ? col_at(TB, wb * TB + j) : 0;
+  for (int j = 0; j < NB; ++j) bcol[j] = KB == COLS ? col_at(TB, wb * NB + j) : 0;
 
-  u32x4 a[2][TA], b[2][TB], raw[kCodes ? TA : 1];
-  float scale[kCodes ? TA : 1];
-  uint32_t sa[kF4 ? TA : 1], sb[kF4 ? TB : 1], sa1[kF4 ? TA : 1], sb1[kF4 ? TB : 1];
+  u32x4 a[2][NA], b[2][NB], raw[kCodes ? NA : 1];
+  float scale[kCodes ? NA : 1];
+  uint32_t sa[kF4 ? NA : 1], sb[kF4 ? NB : 1], sa1[kF4 ? NA : 1], sb1[kF4 ? NB : 1];
   auto transposed = [&](uint32_t at, uint32_t four_rows) -> u32x4 {
     const auto x = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at);
     const auto y = reinterpret_cast<__attribute__((address_space(3))) s16x4*>(lds + at + four_rows);
@@ -542,21 +556,21 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
                                                      (at >> 2) * 256 * TA + (at & 3)));
     }
   };
-  auto read_scales = [&](uint32_t slot, uint32_t (&x)[kF4 ? TA : 1], uint32_t (&y)[kF4 ? TB : 1]) {
+  auto read_scales = [&](uint32_t slot, uint32_t (&x)[kF4 ? NA : 1], uint32_t (&y)[kF4 ? NB : 1]) {
     if constexpr (kF4) {
       const uint32_t at = R::kScaleBase + slot * R::kScaleSlot + 4 * half;
 #pragma unroll
-      for (int i = 0; i < TA; ++i) x[i] = lds_read<uint32_t>(lds, at + (arow >> 4) + i * 256);
+      for (int i = 0; i < NA; ++i) x[i] = lds_read<uint32_t>(lds, at + (arow >> 4) + i * 256);
 #pragma unroll
-      for (int j = 0; j < TB; ++j) y[j] = lds_read<uint32_t>(lds, at + 512 * TA + (brow >> 4) + j * 256);
+      for (int j = 0; j < NB; ++j) y[j] = lds_read<uint32_t>(lds, at + 512 * TA + (brow >> 4) + j * 256);
     }
   };
   // quarter c of the products of step s
-  constexpr int kProducts = TA * TB;
+  constexpr int kProducts = NA * NB;
   auto one = [&](auto sc, int m) {
     constexpr int s = decltype(sc)::value;
-    const u32x4 x = a[s & 1][m % TA], y = b[s & 1][m / TA];
-    f32x16& c = acc[m % TA][m / TA];
+    const u32x4 x = a[s & 1][m % NA], y = b[s & 1][m / NA];
+    f32x16& c = acc[m % NA][m / NA];
     if constexpr (TYPE == F16) {
       c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
     } else if constexpr (TYPE == BF16) {
@@ -564,7 +578,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     } else {
       const i32x8 u = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
       const i32x8 w = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
-      c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(u, w, c, 4, 4, s, (int)sa[m % TA], s, (int)sb[m / TA]);
+      c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(u, w, c, 4, 4, s, (int)sa[m % NA], s, (int)sb[m / NA]);
     }
   };
   auto products = [&](auto sc, int c) {
@@ -605,11 +619,11 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
     for (int c = 0; c < 4; ++c) {
       loads(4 + 4 * s + c);
 #pragma unroll
-      for (int i = 0; i < TA; ++i)
-        if (3 * i / TA == c) read_a(s + 1, i, ac);
+      for (int i = 0; i < NA; ++i)
+        if (3 * i / NA == c) read_a(s + 1, i, ac);
 #pragma unroll
-      for (int j = 0; j < TB; ++j)
-        if (3 * j / TB == c) read_b(s + 1, j, bc);
+      for (int j = 0; j < NB; ++j)
+        if (3 * j / NB == c) read_b(s + 1, j, bc);
       products(st, c);
       pin(c);
     }
@@ -618,12 +632,12 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   stage_barrier<0>();
   read_scales(0, sa, sb);
 #pragma unroll
-  for (int i = 0; i < TA; ++i) {
+  for (int i = 0; i < NA; ++i) {
     read_raw(i, 0, 0);
     read_a(0, i, 0);
   }
 #pragma unroll
-  for (int j = 0; j < TB; ++j) read_b(0, j, 0);
+  for (int j = 0; j < NB; ++j) read_b(0, j, 0);
   if constexpr (kF4) {
     put_scales(1);
     move_scales();
@@ -640,9 +654,9 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   for (int c = 0; c < 4; ++c) loads(c);
   do {
 #pragma unroll
-    for (int i = 0; i < TA; ++i)
+    for (int i = 0; i < NA; ++i)
 #pragma unroll
-      for (int j = 0; j < TB; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
     do {
@@ -654,9 +668,9 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
       // below, away from their operands' reads)
       if constexpr (kF4) {
 #pragma unroll
-        for (int i = 0; i < TA; ++i)
+        for (int i = 0; i < NA; ++i)
 #pragma unroll
-          for (int j = 0; j < TB; ++j) {
+          for (int j = 0; j < NB; ++j) {
             if constexpr (TA == 4) asm volatile("" :: "a"(acc[i][j][0]));
             else asm volatile("" :: "v"(acc[i][j][0]));
           }
@@ -690,22 +704,22 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
         loads(c);
         if (c == 0) {
 #pragma unroll
-          for (int i = 0; i < TA; ++i) read_raw(i, ac, k_now);
+          for (int i = 0; i < NA; ++i) read_raw(i, ac, k_now);
         }
 #pragma unroll
-        for (int i = 0; i < TA; ++i)
-          if (kCodes ? 1 + i * 3 / TA == c : 3 * i / TA == c) read_a(0, i, ac);
+        for (int i = 0; i < NA; ++i)
+          if (kCodes ? 1 + i * 3 / NA == c : 3 * i / NA == c) read_a(0, i, ac);
 #pragma unroll
-        for (int j = 0; j < TB; ++j)
-          if (3 * j / TB == c) read_b(0, j, bc);
+        for (int j = 0; j < NB; ++j)
+          if (3 * j / NB == c) read_b(0, j, bc);
         products(s3, c);
         pin(c);
       }
       if constexpr (kF4) {
 #pragma unroll
-        for (int i = 0; i < TA; ++i) sa[i] = sa1[i];
+        for (int i = 0; i < NA; ++i) sa[i] = sa1[i];
 #pragma unroll
-        for (int j = 0; j < TB; ++j) sb[j] = sb1[j];
+        for (int j = 0; j < NB; ++j) sb[j] = sb1[j];
       }
     } while (--left);
     job.store(tile_of(tile), acc);
@@ -732,11 +746,11 @@ __device__ inline void keep(f32x16& c) {
 // Stores a wave's tiles as 16-bit rows: C's b is the row, a the column, whose
 // eight values go out as 16 bytes (the lane halves trade four each).  The fp32
 // sums are rounded here, once, to the type of the output.
-template <class T, int TA, int TB>
+template <class T, int KA, int TA, int TB>
 __device__ __forceinline__ void store_rows(Acc<TA, TB>& acc, T* out, int64_t ld, int rows, int cols) {
   typedef T x2 __attribute__((ext_vector_type(2)));
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int a0 = (wave >> 1) * TA * 32, b0 = (wave & 1) * TB * 32;
+  const int a0 = Waves<KA>::a(wave) * TA * 32, b0 = Waves<KA>::b(wave) * TB * 32;
 #pragma unroll
   for (int j = 0; j < TB; ++j) {
     const int row = b0 + 32 * j + (l & 31);
