@@ -175,11 +175,11 @@ inline unsigned row_tile_blocks(const Grouped& g, int M, int parts) {
 template <int TYPE> struct Elem { typedef f16 T; };
 template <> struct Elem<tile::BF16> { typedef bf16 T; };
 
-// Blocks of 64 TA columns and up to 64 TA rows, with the LDS of one (TA 4) or
-// two (TA 2) blocks per unit, and as many blocks as the chip holds: each takes
+// Blocks of 64 TA columns and up to 64 TA rows (TA 1: 128), with the LDS of one
+// (TA 4) or two blocks per unit, and as many blocks as the chip holds: each takes
 // one item after another.
 template <int TA> constexpr int kLds = TA == 4 ? 160 * 1024 : 80 * 1024;
-template <int TA> constexpr int kRows = 64 * TA;
+template <int TA> constexpr int kRows = TA == 1 ? 128 : 64 * TA;
 template <int TA> constexpr int kBlocks = TA == 4 ? 256 : 512;
 
 // A block's items: place after place of its die's.  A job of TB takes the tiles
@@ -233,6 +233,19 @@ struct Items {
     return true;
   }
 };
+
+// Whether a call has so few tiles that blocks of 64 columns and up to 128 rows
+// do not outnumber the units.  Us with these / with blocks of 128 columns, fp16:
+// 64 rows of one expert, 4096 x 4096 (64 tiles of 64 columns) 23.6 / 35.2, 14336
+// x 4096 (224) 27.6 / 38.2, 28672 x 4096 (448) 52 / 48; 512 rows, 4096 x 4096
+// (256) 30 / 39, 1024 rows (512) 55 / 42; 8 experts of 2048 x 4096, 25 rows each
+// (256) 30 / 38.  MXFP4 beside 16 bits, 64 rows, 4096 x 4096: 27.6 / 34.5, on
+// both sides 21.2 / 23.6 (512 rows 25.7 / 23.0).
+inline bool narrow_blocks(const Grouped& g, int cols) {
+  const int active = g.E < g.n ? g.E : g.n;
+  const int tiles = g.n / 128 + active / 2;
+  return (int64_t)(tiles > active ? tiles : active) * (cols / 64) <= 256;
+}
 
 // Whether blocks of 256 columns and rows fill the chip, and the experts' rows
 // fill enough of them (`rows` each on average).  Us with large / small blocks, 16

@@ -50,7 +50,7 @@ struct RowJob {
   }
   __device__ inline void store(const Tile& t, Acc<TA, TB>& acc) const {
     const int col = t.part * 64 * TA;
-    store_rows<T, BACK ? COLS : ROWS, TA, TB>(acc, out + (int64_t)t.row * n_out() + col, n_out(), t.n, n_out() - col);
+    store_rows<T, Waves<BACK ? COLS : ROWS, TA>, TA, TB>(acc, out + (int64_t)t.row * n_out() + col, n_out(), t.n, n_out() - col);
   }
 };
 
@@ -211,7 +211,9 @@ void dw_kernel(Grouped g, const void* dy, const void* x, float* dw, bool accumul
 template <int TYPE, bool BACK>
 void launch_rows(const Grouped& g, const void* in, const void* w, void* out, hipStream_t s) {
   const int cols = BACK ? g.d_in : g.d_out;
-  if (large_blocks(g, cols, BACK ? 0 : 64))
+  if (narrow_blocks(g, cols))
+    rows_kernel<TYPE, 1, BACK><<<kBlocks<1>, kThreads, 0, s>>>(g, in, w, out, cols / 64);
+  else if (large_blocks(g, cols, BACK ? 0 : 64))
     rows_kernel<TYPE, 4, BACK><<<kBlocks<4>, kThreads, 0, s>>>(g, in, w, out, (cols + 255) / 256);
   else
     rows_kernel<TYPE, 2, BACK><<<kBlocks<2>, kThreads, 0, s>>>(g, in, w, out, (cols + 127) / 128);

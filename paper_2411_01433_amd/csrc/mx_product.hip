@@ -43,7 +43,7 @@ struct MxJob {
   template <int NA, int NB>
   __device__ inline void store(const Tile& t, Acc<NA, NB>& acc) const {
     const int col = t.part * 64 * TA;
-    store_rows<T, CODED ? ROWS : CODES, NA, NB>(acc, y + (int64_t)t.row * g.d_out + col, g.d_out, t.n, g.d_out - col);
+    store_rows<T, Waves<CODED ? ROWS : CODES, TA>, NA, NB>(acc, y + (int64_t)t.row * g.d_out + col, g.d_out, t.n, g.d_out - col);
   }
 };
 
@@ -76,7 +76,9 @@ void mx_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w,
 template <int TYPE, bool CODED>
 void launch(const Grouped& g, const uint8_t* x, const uint8_t* xs, const uint8_t* w, const uint8_t* ws,
             void* y, hipStream_t s) {
-  if (large_blocks(g, g.d_out, CODED ? 0 : 384))
+  if (narrow_blocks(g, g.d_out))
+    mx_kernel<TYPE, 1, CODED><<<kBlocks<1>, kThreads, 0, s>>>(g, x, xs, w, ws, y, g.d_out / 64);
+  else if (large_blocks(g, g.d_out, CODED ? 0 : 384))
     mx_kernel<TYPE, 4, CODED><<<kBlocks<4>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 255) / 256);
   else
     mx_kernel<TYPE, 2, CODED><<<kBlocks<2>, kThreads, 0, s>>>(g, x, xs, w, ws, y, (g.d_out + 127) / 128);

@@ -266,7 +266,7 @@ struct Ring {
   static constexpr int kBeside = (int)((kRoom - kUnits * kA) / kB);
   static constexpr int SB = TYPE == F4 ? 2 : KA == CODES ? (kBeside > kUnits + 1 ? kUnits + 1 : kBeside)
                             : kBoth > 6 ? 6 : kBoth;
-  static constexpr int SA = KA == CODES ? kUnits : TYPE != F4 && SB == 2 && 3 * kA + 2 * kB <= kRoom ? 3 : SB;
+  static constexpr int SA = KA == CODES ? kUnits : TYPE != F4 && SB < 6 && (SB + 1) * kA + SB * kB <= kRoom ? SB + 1 : SB;
   static constexpr uint32_t kBBase = SA * kA, kScaleBase = kBBase + SB * kB;
   // (a tile of one stage has a slot of scales of its own, and the queue of
   // stream() holds the tile of the products and seven behind it)
@@ -282,7 +282,7 @@ struct Ring {
   // them 186, 183, 184, 189 us at the rows above)
   static constexpr int kSpread = SB == 2 && SA == 2 ? 4 : 12;
   // A passes the caches by: tiles of up to 128 rows
-  static constexpr bool kStream = TB <= (TA == 4 ? 2 : 1);
+  static constexpr bool kStream = TB <= (TA == 2 ? 1 : 2);
 };
 
 // The accumulators of a wave: acc[i][j] is A tile i, B tile j of its own.
@@ -294,11 +294,11 @@ struct Scales {
   int bytes;
 };
 
-// How the waves share a block's tile: 2 x 2; beside CODES 4 x 1, so that each
-// code is converted once.
-template <int KA>
+// How the waves share a block's tile: 2 x 2; CODES of two tiles and more 4 x 1,
+// so that each is converted once.
+template <int KA, int TA>
 struct Waves {
-  static constexpr bool kLine = KA == CODES;
+  static constexpr bool kLine = KA == CODES && TA > 1;
   static constexpr int kA(int ta) { return kLine ? ta / 2 : ta; }
   static constexpr int kB(int tb) { return kLine ? 2 * tb : tb; }
   static __device__ inline int a(int wave) { return kLine ? wave : wave >> 1; }
@@ -323,7 +323,7 @@ __device__ __forceinline__ void stream(Job& job, lds_u8* lds) {
   const int l = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // the wave's place, and its tiles of 32
-  typedef Waves<KA> W;
+  typedef Waves<KA, TA> W;
   constexpr int NA = W::kA(TA), NB = W::kB(TB);
   const int wa = W::a(wave), wb = W::b(wave);
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -746,11 +746,11 @@ __device__ inline void keep(f32x16& c) {
 // Stores a wave's tiles as 16-bit rows: C's b is the row, a the column, whose
 // eight values go out as 16 bytes (the lane halves trade four each).  The fp32
 // sums are rounded here, once, to the type of the output.
-template <class T, int KA, int TA, int TB>
+template <class T, class W, int TA, int TB>
 __device__ __forceinline__ void store_rows(Acc<TA, TB>& acc, T* out, int64_t ld, int rows, int cols) {
   typedef T x2 __attribute__((ext_vector_type(2)));
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int a0 = Waves<KA>::a(wave) * TA * 32, b0 = Waves<KA>::b(wave) * TB * 32;
+  const int a0 = W::a(wave) * TA * 32, b0 = W::b(wave) * TB * 32;
 #pragma unroll
   for (int j = 0; j < TB; ++j) {
     const int row = b0 + 32 * j + (l & 31);

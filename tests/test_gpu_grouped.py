@@ -136,6 +136,24 @@ def test_backward(counts, d_in, d_out, extra, dtype):
     assert ((dw1 - (base + dw)).abs() <= 2 * U * (base + dw).abs() + 1e-30).all()
 
 
+WIDE = pytest.mark.parametrize("counts,extra", [
+    ([70, 0, 128, 129, 33, 255, 1, 64], 3),
+    ([(11 * e) % 40 for e in range(20)], 0),
+    ([260], 1),
+])
+
+
+@TYPES
+@WIDE
+@pytest.mark.parametrize("d_in,d_out", [(192, 2112), (2112, 192), (5568, 5504)])
+def test_wide_rows(counts, extra, d_in, d_out, dtype):
+    """More tiles than the calls above have, of columns of y and of d_x."""
+    if d_in * d_out * len(counts) > 8 * 5568 * 2112:
+        counts, extra = [90], 0
+    test_forward(counts, d_in, d_out, extra, dtype)
+    test_backward(counts, d_in, d_out, extra, dtype)
+
+
 @pytest.mark.parametrize("counts", [[-3, 5, -2147483648, 2], [4, 2147483647, 3],
                                     [2147483647] * 4, [20, 0, 0, 0], [3, 9, 1, 1]])
 def test_counts_that_do_not_fit(counts):

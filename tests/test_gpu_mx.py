@@ -207,6 +207,19 @@ def test_rows_of_many_columns(counts, d_in, d_out, extra, act):
     test_product(counts, d_in, d_out, extra, torch.bfloat16, act)
 
 
+@pytest.mark.parametrize("act", ["16", "4"])
+@TYPES
+@pytest.mark.parametrize("counts,extra", [
+    ([70, 0, 128, 129, 33, 255, 1, 64], 3),
+    ([(11 * e) % 40 for e in range(20)], 0),
+    ([520], 1),
+])
+@pytest.mark.parametrize("d_in,d_out", [(192, 2112), (832, 3520)])
+def test_wide_rows(counts, extra, d_in, d_out, dtype, act):
+    """More tiles than the calls above have."""
+    test_product(counts, d_in, d_out, extra, dtype, act)
+
+
 @pytest.mark.parametrize("rows", [1, 3, 40, 300])
 def test_scales_over_the_whole_range(rows):
     """Scale bytes 0 (2^-127) to 254 in bf16 and 4-bit products, whose partner
