@@ -12,10 +12,10 @@
 //
 // d_W is 4 bytes per 2 rows' products: few rows per expert bound it by its own
 // writing.  Kernels in us (what bounds them):
-//   16 experts of 6400 x 4096, fp16: y of 16384 rows 777 to 879 (power: 1.1 PF),
-//     d_x of 8192 rows 443 to 477 (power: 0.97 PF), d_W 585 to 616 (tiles of
+//   16 experts of 6400 x 4096, fp16: y of 16384 rows 776 to 872 (power: 1.1 PF),
+//     d_x of 8192 rows 450 to 471 (power: 0.95 PF), d_W 582 to 615 (tiles of
 //     eight stages, whose stores nothing runs beside: 0.73 PF, 2.9 TB/s)
-//   60 experts of 1472 x 2048, bf16, 5348 rows: y 96 to 103 (W's way from memory,
+//   60 experts of 1472 x 2048, bf16, 5348 rows: y 95 to 102 (W's way from memory,
 //     4.1 TB/s), d_x 77 to 86 (5.2 TB/s), d_W 140 to 158 (5.4 TB/s written)
 #include "few_rows.h"
 

@@ -4,11 +4,12 @@
 // With both in MXFP4 the matrix cores take codes and scales as they are.
 // With activations of 16 bits a code becomes an activation's type after it was
 // read from LDS (v_cvt_scalef32_pk: exact wherever the type holds the value),
-// eight for four of these instructions, in both waves that need it.
+// eight for four of these instructions.
 //
-// Kernels in us, 16 experts of 6400 x 4096: 1024 bf16 rows 116 to 124 (245 MB and
-// 54 GF; the conversions and their waits bound it, the products take a third of
-// the time), 8192 rows in MXFP4 174 to 193 (tile.h).  On few_rows.h one row for
+// Kernels in us, 16 experts of 6400 x 4096: 1024 bf16 rows 114 to 122 (244 MB and
+// 54 GF; a stage's chain of reads, conversions and products bounds it, the
+// products are a third of the time), 16384 fp16 rows 743 (power), 8192 rows in
+// MXFP4 160 to 188 (tile.h).  On few_rows.h one row for
 // two experts of 14336 x 4096, 62 MB: 12.7 to 14.5 (4.5 TB/s, the start and the
 // end of a launch among it).
 #include "few_rows.h"

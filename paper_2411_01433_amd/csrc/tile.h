@@ -3,8 +3,8 @@
 //
 //   C[a, b] = sum_k A[a, k] B[b, k]
 //
-// A block is 4 waves, one per SIMD, 2 x 2 over a tile of 64 TA x 64 TB; a wave
-// owns TA x TB tiles of 32 x 32 (v_mfma_f32_32x32x16, in MXFP4
+// A block is 4 waves, one per SIMD, 2 x 2 over a tile of 64 TA x 64 TB (Waves); a
+// wave owns TA x TB tiles of 32 x 32 (v_mfma_f32_32x32x16, in MXFP4
 // v_mfma_scale_f32_32x32x64: lane l holds 16 bytes of row l % 32 of either
 // operand and C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32]).
 //
@@ -17,7 +17,7 @@
 // matrices - rows and columns past the ends, reduction steps past the last -
 // is masked by the buffer's range check and arrives as zeros.  Codes beside a
 // partner of 16 bits (CODES) come in units of four stages, whole lines too, and
-// become 16-bit fragments after the read, each by two waves.  Weights of tiles
+// become 16-bit fragments after the read, as a rule each by one wave.  Weights of tiles
 // of up to 128 rows, which few other tiles share, pass the caches by: 60 experts
 // of 1472 x 2048 with 89 rows each took 111 us without that, 97 with it.
 //
@@ -38,17 +38,17 @@
 //
 // Blocks.  Tiles of 256 x 256 have 64 products per 16 fragments read, one wave
 // per SIMD; 160 KB of LDS hold two stages and the third of one operand.  Blocks
-// of 128 columns leave room for two of them on a unit, for calls whose large
-// tiles would not fill the chip.  Blocks are persistent: while one tile is
+// of 128 and 64 columns leave room for two of them on a unit, for calls whose
+// large tiles would not fill the chip.  Blocks are persistent: while one tile is
 // stored the next one's loads are under way.
 //
-// Measured: 16384 x 4096 by 16 experts' 6400 rows in fp16 780 to 830 us, 1.03 to
+// Measured: 16384 x 4096 by 16 experts' 6400 rows in fp16 776 to 872 us, 0.99 to
 // 1.1 PF, the matrix cores busy 75 % of the time; their power bounds it: with
 // more and more columns to sum each costs as much as at 1.35 PF, on zeros as at
-// 2.06 (products alone, nothing loaded: 1.68).  In MXFP4 8192 rows take 166 us, 2.6 PF of the 6.2 that the
-// products alone reach: at 34 % a wave's own instructions bound it, which between
-// two stages has no partner on its SIMD to fill in (without the scales' loads it
-// takes 20 us less, without any loads 16).
+// 2.06 (products alone, nothing loaded: 1.68).  In MXFP4 8192 rows take 160 to
+// 188 us, 2.3 to 2.7 PF of the 6.2 that the products alone reach: a wave has no
+// partner on its SIMD to fill in between two stages, and the matrix cores are
+// busy 36 % (without any loads it takes 16 us less).
 #pragma once
 
 #include <type_traits>
@@ -279,7 +279,7 @@ struct Ring {
   static constexpr int kPending = (KA == CODES ? 0 : SA - 2) * Loads<KA, TA>::kN + (SB - 2) * Loads<KB, TB>::kN;
   // quarters (of 16 between two barriers) that the loads are spread over: all
   // of a ring of two have to arrive within these (in MXFP4 over 2, 4, 8, 12 of
-  // them 186, 183, 184, 189 us at the rows above)
+  // them 186, 183, 184, 189 us for 8192 rows, 16 experts of 6400 x 4096)
   static constexpr int kSpread = SB == 2 && SA == 2 ? 4 : 12;
   // A passes the caches by: tiles of up to 128 rows
   static constexpr bool kStream = TB <= (TA == 2 ? 1 : 2);
