@@ -219,7 +219,17 @@ void few_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w
 // tiles of 64 rows and more, 16 experts of 6400 x 4096: 2 rows each 115 / 128, 8
 // rows 153 / 169, 16 rows 195 / 168; W in MXFP4 48 / 73, 75 / 85, 118 / 86; x in
 // MXFP4 too, 8 rows 54 / 67, 16 rows 71 / 61.
-inline bool takes(const Grouped& g) { return g.n <= 8 * (int64_t)g.E; }
+//
+// Codes in calls of few tiles, whose blocks there wait for one stage after
+// another, up to 16 rows, 24 if x's are in MXFP4 too.  One expert of 4096 x
+// 4096: 16 rows 19 / 26, 32 rows 23 / 28, 64 rows 43 / 28, of 14336 x 4096 24 /
+// 28, 28 / 28, 53 / 28; x too 16 rows 14 / 21 and 15 / 23, 32 rows 14 / 22 and
+// 18 / 23, 64 rows 14 / 22 and 29 / 23; 8 experts of 2048 x 4096, 32 rows each
+// 28 / 24.  In 16 bits 8 rows 15 / 21 and 26 / 25, 16 rows 19 / 21 and 31 / 24.
+inline bool takes(const Grouped& g, bool coded, bool both) {
+  const int rows = !coded || !narrow_blocks(g, g.d_out) ? 8 : both ? 24 : 16;
+  return g.n <= rows * (int64_t)g.E;
+}
 
 // Whether the waves of a block share its columns: for calls of few blocks, and
 // where both operands are in MXFP4 only if the rows are long, as a stage takes

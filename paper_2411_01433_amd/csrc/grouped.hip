@@ -235,7 +235,7 @@ void launch_dw(const Grouped& g, const void* dy, const void* x, float* dw, bool 
 
 hipError_t launch_grouped_product(const Grouped& g, const void* x, const void* w, void* y,
                                   hipStream_t s) {
-  if (few::takes(g)) {
+  if (few::takes(g, false, false)) {
     if (g.type == TYPE_F16) few::launch<F16, false, false>(g, x, nullptr, w, nullptr, y, s);
     else few::launch<BF16, false, false>(g, x, nullptr, w, nullptr, y, s);
   } else {

@@ -90,7 +90,7 @@ void launch(const Grouped& g, const uint8_t* x, const uint8_t* xs, const uint8_t
 hipError_t launch_mx_product(const Grouped& g, const void* x, const uint8_t* xs,
                              const uint8_t* w, const uint8_t* ws, void* y, hipStream_t s) {
   const uint8_t* xb = static_cast<const uint8_t*>(x);
-  if (few::takes(g)) {
+  if (few::takes(g, true, xs != nullptr)) {
     if (g.type == TYPE_F16) {
       if (xs) few::launch<F16, true, true>(g, x, xs, w, ws, y, s);
       else few::launch<F16, true, false>(g, x, xs, w, ws, y, s);

@@ -201,6 +201,9 @@ def test_product(counts, d_in, d_out, extra, dtype, act):
     ([3, 0, 16, 0, 1], 8256, 192, 2),
     ([0, 2, 11], 20544, 128, 0),
     ([40], 16448, 192, 1),
+    ([0] * 7 + [61], 448, 192, 2),
+    ([14], 448, 64, 0),
+    ([3, 45, 17], 1088, 192, 0),
 ])
 def test_rows_of_many_columns(counts, d_in, d_out, extra, act):
     """Blocks whose waves share the columns, and several slabs of them."""
