@@ -281,7 +281,8 @@ struct Ring {
   // of a ring of two have to arrive within these (in MXFP4 over 2, 4, 8, 12 of
   // them 186, 183, 184, 189 us for 8192 rows, 16 experts of 6400 x 4096)
   static constexpr int kSpread = SB == 2 && SA == 2 ? 4 : 12;
-  // A passes the caches by: tiles of up to 128 rows
+  // A passes the caches by: tiles of up to 128 rows; in blocks of 128 columns,
+  // which hold no more rows and meet an expert's others as neighbours, of 64
   static constexpr bool kStream = TB <= (TA == 2 ? 1 : 2);
 };
 
