@@ -137,7 +137,7 @@ def _mx_pack(v):
     """codes [.., cols / 2] and scales [.., cols / 32] (uint8) of v."""
     m, neg, e = _mx(v)
     k = torch.where(m < 2, 2 * m, torch.where(m < 4, m + 2, m / 2 + 4)).to(torch.uint8)
-    k = (k + 8 * neg.to(torch.uint8)).view(*v.shape[:-1], -1, 2)
+    k = (k + 8 * neg).view(*v.shape[:-1], -1, 2)
     return k[..., 0] + 16 * k[..., 1], (e + 127).to(torch.uint8)
 
 
