@@ -228,6 +228,14 @@ def run(s):
     return _run_own(s) if own else _run_plain(s)
 
 
+def _w_codes(s):
+    """W's codes as the bytes that the calls take: laid out once for a state, as a program that
+    serves them keeps its weights (the plain form's are whole numbers of 64 bits)."""
+    if "w_codes" not in s:
+        s["w_codes"] = s["codes"].to(torch.uint8)
+    return s["w_codes"]
+
+
 def _run_own(s):
     import paper_2411_01433_amd as P
     kind = s["case"]["kind"]
@@ -239,13 +247,16 @@ def _run_own(s):
         return {"x": s["d_x"], "w": s["d_w"]}
     if kind == "quantize":
         P.mx_quantize(s["v"], s["codes"], s["scales"], s["values"])
-        return {"codes": s["codes"], "scales": s["scales"], "values": s["values"]}
+        # (the codes in the type in which the plain form has them, so that they compare: a copy
+        # of 8 bytes for each pair, which no program needs, and which is timed with the call)
+        return {"codes": s["codes"].long(), "scales": s["scales"], "values": s["values"]}
     if kind == "mx_product":
+        w = _w_codes(s)
         if s["case"]["act"] == "4":
             P.mx_quantize(s["x"], s["x_codes"], s["x_scales"])
-            P.mx_product(s["x_codes"], s["codes"], s["scales"], s["y"], s["count"], s["x_scales"])
+            P.mx_product(s["x_codes"], w, s["scales"], s["y"], s["count"], s["x_scales"])
         else:
-            P.mx_product(s["x"], s["codes"], s["scales"], s["y"], s["count"])
+            P.mx_product(s["x"], w, s["scales"], s["y"], s["count"])
         return {"y": s["y"]}
     s["grads"].clip(s["max_norm"], s["norm"])
     return {"norm": s["norm"], "out": s["out"]}
