@@ -201,9 +201,9 @@ moe_status moe_gradients_init(int32_t n, const void* const* grads, void* const* 
         return efail(MOE_EINVAL, "tensor %d must be aligned to its elements", i);
       spans.push_back({(uintptr_t)in, sizes[i] * es});
       if (to != in) spans.push_back({(uintptr_t)to, sizes[i] * es});
-      for (int64_t at = 0; at < sizes[i]; at += kPieceElems)
-        pieces.push_back({in + at * es, to + at * es,
-                          (int32_t)std::min<int64_t>(kPieceElems, sizes[i] - at), types[i]});
+      const int64_t per = kPieceBytes / es;
+      for (int64_t at = 0; at < sizes[i]; at += per)
+        pieces.push_back({in + at * es, to + at * es, (int32_t)std::min(per, sizes[i] - at), types[i]});
     }
     if (pieces.empty()) pieces.push_back({nullptr, nullptr, 0, MOE_F32});  // nothing: norm 0
     std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });

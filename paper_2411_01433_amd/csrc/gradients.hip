@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVecs = 8;   // vectors of 16 bytes that a thread has in flight
+static_assert(kPieceBytes >= kVecs * kThreads * 16, "a piece fills the unrolled loops, of any type");
 
 template <class T> struct Vec;
 template <> struct Vec<float> { typedef float V __attribute__((ext_vector_type(4))); };

@@ -316,13 +316,13 @@ struct Grouped {
   int32_t type, n, d_in, d_out, E;
 };
 
-// One piece of a gradient tensor, at most kPieceElems elements.
+// One piece of a gradient tensor, at most kPieceBytes of it.
 struct GradPiece {
   const void* in;
   void* out;
   int32_t n, type;
 };
-constexpr int kPieceElems = 1 << 13;
+constexpr int kPieceBytes = 1 << 15;
 constexpr int kGradBlocks = 2048;
 
 struct GradList {
