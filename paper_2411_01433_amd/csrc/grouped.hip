@@ -11,7 +11,12 @@
 // the 8192 rows below).
 //
 // d_W is 4 bytes per 2 rows' products: few rows per expert bound it by its own
-// writing.  Kernels in us (what bounds them):
+// writing.  Added to what is there (ADD) it reads as much: a lane fetches the 16
+// values of a tile of 32 x 32 together, since none may pass a store to the same
+// array; one at a time 16 experts of 6400 x 4096, 8192 rows, took 3183 us where it
+// takes 764 (681 at a copy's rate), 60 of 1472 x 2048, 5348 rows, 1341 where it
+// takes 276.  A kernel that can only write takes 531, one that can do both 553.
+// Kernels in us (what bounds them):
 //   16 experts of 6400 x 4096, fp16: y of 16384 rows 776 to 872 (power: 1.1 PF),
 //     d_x of 8192 rows 450 to 471 (power: 0.95 PF), d_W 582 to 615 (tiles of
 //     eight stages, whose stores nothing runs beside: 0.73 PF, 2.9 TB/s)
@@ -85,10 +90,9 @@ struct WeightTile {
   int expert, first, n, a0, b0;
 };
 
-template <int TA>
+template <int TA, bool ADD>
 struct WeightItems {
   const Grouped& g;
-  bool accumulate;
   Counts counts;
   int slot;
   WeightTile t;        // the first one not taken; n < 0: none
@@ -113,7 +117,7 @@ struct WeightItems {
       if (item < 0) continue;
       const int e = item / per, in = item - e * per;
       const Rows rows = now.rows(e);
-      if (accumulate && rows.n == 0) continue;
+      if (ADD && rows.n == 0) continue;
       const int sup = in / (kSuper * na), left = in - sup * (kSuper * na);
       const int width = min(kSuper, nb - sup * kSuper);
       const int ia = left / width, ib = sup * kSuper + left - ia * width;
@@ -143,14 +147,14 @@ struct WeightItems {
   }
 };
 
-template <int TYPE, int TA, int TB>
+template <int TYPE, int TA, int TB, bool ADD>
 struct WeightJob {
   typedef WeightTile Tile;
   typedef typename Elem<TYPE>::T T;
   const Grouped& g;
   const T *dy, *x;
   float* dw;
-  WeightItems<TA>& items;
+  WeightItems<TA, ADD>& items;
 
   __device__ inline bool next(Tile& t) { return items.next(TB, t); }
   __device__ inline int steps(const Tile& t) const { return t.n; }
@@ -173,31 +177,38 @@ struct WeightJob {
       for (int j = 0; j < TB; ++j) {
         if (t.b0 + bw + 32 * j >= g.d_in) continue;
         keep<TA * TB>(acc[i][j]);
+        auto to = [&](int q) {
+          return global_ptr<float>(out + (int64_t)(32 * i + 8 * (q >> 2) + (q & 3)) * g.d_in + 32 * j);
+        };
+        float v[16];
+        if constexpr (ADD) {
+          // (all of them before the first store, which they may not pass)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          auto* to = global_ptr<float>(out + (int64_t)(32 * i + 8 * (q >> 2) + (q & 3)) * g.d_in + 32 * j);
-          const float v = acc[i][j][q];
-          __builtin_nontemporal_store(items.accumulate ? *to + v : v, to);
+          for (int q = 0; q < 16; ++q) v[q] = __builtin_nontemporal_load(to(q));
         }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v[q] = ADD ? v[q] + acc[i][j][q] : acc[i][j][q];
+#pragma unroll
+        for (int q = 0; q < 16; ++q) __builtin_nontemporal_store(v[q], to(q));
       }
     }
   }
 };
 
-template <int TYPE, int TA>
+template <int TYPE, int TA, bool ADD>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(TA == 4 ? 1 : 2, TA == 4 ? 1 : 2)))
-void dw_kernel(Grouped g, const void* dy, const void* x, float* dw, bool accumulate) {
+void dw_kernel(Grouped g, const void* dy, const void* x, float* dw) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kLds<TA>];
   typedef typename Elem<TYPE>::T T;
   lds_u8* lds = (lds_u8*)smem;
-  WeightItems<TA> items = {g, accumulate};
+  WeightItems<TA, ADD> items = {g};
   items.init();
   set_aside(dy);
   set_aside(x);
   set_aside(dw);
   auto take = [&](auto size) {
     constexpr int TB = decltype(size)::value;
-    WeightJob<TYPE, TA, TB> job = {g, (const T*)dy, (const T*)x, dw, items};
+    WeightJob<TYPE, TA, TB, ADD> job = {g, (const T*)dy, (const T*)x, dw, items};
     stream<TYPE, COLS, COLS, TA, TB, kLds<TA>>(job, lds);
   };
   while (const int n = items.size()) {
@@ -223,12 +234,12 @@ void launch_rows(const Grouped& g, const void* in, const void* w, void* out, hip
 // with 128 x 128: 16 experts of 6400 x 4096, 8192 rows, 1040 / 1172; 60 of 1472 x
 // 2048, 5348 rows, 226 / 243; one of 4096 x 4096, 4096 rows (256 tiles) 233 / 271;
 // 64 tiles (2048 x 2048) 115 / 85, 128 tiles (8 of 1024 x 1024, 2048 rows) 34 / 29.
-template <int TYPE>
-void launch_dw(const Grouped& g, const void* dy, const void* x, float* dw, bool accumulate, hipStream_t s) {
+template <int TYPE, bool ADD>
+void launch_dw(const Grouped& g, const void* dy, const void* x, float* dw, hipStream_t s) {
   if ((int64_t)g.E * ((g.d_in + 255) / 256) * ((g.d_out + 255) / 256) >= 256)
-    dw_kernel<TYPE, 4><<<kBlocks<4>, kThreads, 0, s>>>(g, dy, x, dw, accumulate);
+    dw_kernel<TYPE, 4, ADD><<<kBlocks<4>, kThreads, 0, s>>>(g, dy, x, dw);
   else
-    dw_kernel<TYPE, 2><<<kBlocks<2>, kThreads, 0, s>>>(g, dy, x, dw, accumulate);
+    dw_kernel<TYPE, 2, ADD><<<kBlocks<2>, kThreads, 0, s>>>(g, dy, x, dw);
 }
 
 }  // namespace
@@ -254,8 +265,13 @@ hipError_t launch_grouped_dx(const Grouped& g, const void* dy, const void* w, vo
 
 hipError_t launch_grouped_dw(const Grouped& g, const void* dy, const void* x, float* dw,
                              bool accumulate, hipStream_t s) {
-  if (g.type == TYPE_F16) launch_dw<F16>(g, dy, x, dw, accumulate, s);
-  else launch_dw<BF16>(g, dy, x, dw, accumulate, s);
+  if (g.type == TYPE_F16) {
+    if (accumulate) launch_dw<F16, true>(g, dy, x, dw, s);
+    else launch_dw<F16, false>(g, dy, x, dw, s);
+  } else {
+    if (accumulate) launch_dw<BF16, true>(g, dy, x, dw, s);
+    else launch_dw<BF16, false>(g, dy, x, dw, s);
+  }
   return hipGetLastError();
 }
 
