@@ -9,7 +9,7 @@
 // operand and C[8 (i / 4) + 4 (l / 32) + i % 4][l % 32]).
 //
 // Staging.  Both operands go to LDS by direct loads of 16 bytes a lane, in
-// stages of 64 reduction steps (256 in MXFP4) and rings of 2 to 8 slots.  An
+// stages of 64 reduction steps (256 in MXFP4) and rings of 2 to 6 slots.  An
 // operand whose reduction is contiguous in memory (ROWS) takes one full
 // 128-byte line of each row; one whose reduction runs over the rows (COLS)
 // takes 64 rows of 128 T bytes and is transposed by the fragment reads
@@ -19,7 +19,8 @@
 // partner of 16 bits (CODES) come in units of four stages, whole lines too, and
 // become 16-bit fragments after the read, as a rule each by one wave.  Weights of tiles
 // of up to 128 rows, which few other tiles share, pass the caches by: 60 experts
-// of 1472 x 2048 with 89 rows each took 111 us without that, 97 with it.
+// of 1472 x 2048 with 89 rows each took 111 us without that, 97 with it.  The rows
+// of d_y that the gradient of W has in their place do not.
 //
 // Bank conflicts.  ROWS: the 16-byte chunk c of row r sits at position
 // c ^ (r / 2 % 8), CODES likewise.  COLS: 64-byte pieces are permuted by the row's last bits,
@@ -281,9 +282,14 @@ struct Ring {
   // of a ring of two have to arrive within these (in MXFP4 over 2, 4, 8, 12 of
   // them 186, 183, 184, 189 us for 8192 rows, 16 experts of 6400 x 4096)
   static constexpr int kSpread = SB == 2 && SA == 2 ? 4 : 12;
-  // A passes the caches by: tiles of up to 128 rows; in blocks of 128 columns,
-  // which hold no more rows and meet an expert's others as neighbours, of 64
-  static constexpr bool kStream = TB <= (TA == 2 ? 1 : 2);
+  // A passes the caches by: weights, of tiles of up to 128 rows; in blocks of 128
+  // columns, which hold no more rows and meet an expert's others as neighbours, of
+  // 64.  In the gradient of W (both operands COLS) A is d_y, which all column tiles
+  // of d_W read.  Us of that gradient, whose last column tile is a small one, past
+  // the caches / through them: 8 experts, 4096 rows, 4096 x 4160 191 / 179, 4096 x
+  // 1088 60.3 / 56.2; 16 experts, 8192 rows, 6400 x 1088 151 / 144, 6400 x 4160
+  // 554 / 569; 60 experts, 5348 rows, 2048 x 2112 both 194.
+  static constexpr bool kStream = KB != COLS && TB <= (TA == 2 ? 1 : 2);
 };
 
 // The accumulators of a wave: acc[i][j] is A tile i, B tile j of its own.
