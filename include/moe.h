@@ -429,8 +429,9 @@ moe_status moe_mx_quantize(const void* v, int32_t type, int64_t rows, int64_t co
  *            else device u8 [n_rows, d_in / 2], the codes of rows quantised
  *            with the scales x_scales, device u8 [n_rows, d_in / 32]
  *  y         device, `type` [n_rows, d_out]
- * Everything else as moe_grouped_product; scales 4-byte aligned.  A scale byte
- * of 255 gives NaN in every output that its block enters. */
+ * Everything else as moe_grouped_product; scales 4-byte aligned (a slice of x's
+ * rows with d_in an odd multiple of 64 begins at an even row).  A scale byte of
+ * 255 gives NaN in every output that its block enters. */
 moe_status moe_mx_product(const void* x, const void* x_scales, const void* w_codes,
                           const void* w_scales, const int32_t* expert_count, void* y, int32_t type,
                           int32_t n_rows, int32_t d_in, int32_t d_out, int32_t n_experts,

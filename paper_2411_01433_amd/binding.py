@@ -409,7 +409,8 @@ def mx_product(x, codes, scales, y, count=None, x_scales=None, stream=None):
     """grouped_product with weights in MXFP4: codes uint8 [E, d_out, d_in / 2],
     scales uint8 [E, d_out, d_in / 32], y [R, d_out] fp16 or bf16.  x [R, d_in]
     of y's type, or with x_scales uint8 [R, d_in / 32] its codes uint8
-    [R, d_in / 2]."""
+    [R, d_in / 2].  Scales begin on 4 bytes: with d_in an odd multiple of 64 a
+    slice of quantised rows does at even rows only."""
     torch = _th()
     R, cols = _rows(x, "x")
     _rows(y, "y")

@@ -5,12 +5,25 @@
 // What bounds it is the weights' way from memory.  Every wave streams 16 rows of
 // W through a ring of its own in LDS, by direct loads of whole 128-byte lines
 // that pass the caches by (64 columns of 16 bits, 256 of MXFP4 a stage), and
-// waits for nothing but its own loads.  Read as matrix fragments straight from
-// memory, 16 rows of 64 bytes at a time, a weight matrix of 235 MB took 40.4 us
-// at best, in whole lines 35.6 (6.6 TB/s).
+// within a slab of columns waits for nothing but its own loads.  Read as matrix
+// fragments straight from memory, 16 rows of 64 bytes at a time, a weight matrix
+// of 235 MB took 40.4 us at best, in whole lines 35.6 (6.6 TB/s).
 //
-// The block's rows of x (and the weights' scales) are copied to LDS once per
-// slab of columns while the first loads are under way.  The products are
+// The block's rows of x (and the weights' scales) are copied to LDS through
+// registers once per slab while the first loads are under way; these are waited
+// for with them, and at a slab's end the stream stops until the next one's copy
+// is there.  A slab is 512 floor(20 / rows) columns where x has 16 bits (one row
+// 10240, 11 to 16 rows 512: eight stages of W in 16 bits, two in MXFP4), 2048
+// floor(20 / rows), or 2048, of x in MXFP4, and beside the scales of 64 rows of W
+// 4096 at most.
+//
+// Of MXFP4, whose blocks have a quarter of the stages, that start is what bounds
+// few columns: one row for two experts, 71 MB of 1024 columns 24.7 us, 62 MB of
+// 4096 15.3, and 12.9 with x in MXFP4 too, which is without conversions.  With 64
+// rows of W to a block, 80 KB of loads are in flight on a unit at once, here as in
+// 16 bits (125 MB and 250 MB: 4.3 and 4.4 TB/s; 16 bits, 940 MB: 6.7).
+//
+//  The products are
 // v_mfma_f32_16x16x32 (both operands in MXFP4: v_mfma_scale_f32_16x16x128): lane
 // l holds 16 bytes of row l % 16, columns 8 (l / 16) and up of a step, and
 // C[4 (l / 16) + i][l % 16].  Rows of x that the tile lacks repeat its last; what
@@ -226,6 +239,14 @@ void few_kernel(Grouped g, const uint8_t* x, const uint8_t* xs, const uint8_t* w
 // 28, 28 / 28, 53 / 28; x too 16 rows 14 / 21 and 15 / 23, 32 rows 14 / 22 and
 // 18 / 23, 64 rows 14 / 22 and 29 / 23; 8 experts of 2048 x 4096, 32 rows each
 // 28 / 24.  In 16 bits 8 rows 15 / 21 and 26 / 25, 16 rows 19 / 21 and 31 / 24.
+//
+// The counts are on the device, so the rule goes by the average over all experts.
+// Counts that leave most of them empty send the others this way with many rows
+// each, and W streams once per 16 of them: 64 experts of 4096 x 4096, two of which
+// have 256 rows each, 512 rows / 520 (which go by tiles): fp16 142 / 42, W in MXFP4
+// 118 / 46, x too 55 / 35; of 1472 x 2048 35 / 23, 29 / 21, 13 / 21.  Evenly
+// spread, the same calls take 327 / 361, 161 / 168, 115 / 110 and 73 / 76, 35 / 38,
+// 26 / 29.
 inline bool takes(const Grouped& g, bool coded, bool both) {
   const int rows = !coded || !narrow_blocks(g, g.d_out) ? 8 : both ? 24 : 16;
   return g.n <= rows * (int64_t)g.E;

@@ -240,7 +240,8 @@ struct Items {
 // x 4096 (224) 27.6 / 38.2, 28672 x 4096 (448) 52 / 48; 512 rows, 4096 x 4096
 // (256) 30 / 39, 1024 rows (512) 55 / 42; 8 experts of 2048 x 4096, 25 rows each
 // (256) 30 / 38.  MXFP4 beside 16 bits, 64 rows, 4096 x 4096: 27.6 / 34.5, on
-// both sides 21.2 / 23.6 (512 rows 25.7 / 23.0).
+// both sides 21.2 / 23.6 (512 rows 25.7 / 23.0: there the narrow ones lose, as the
+// kind of operands is not asked for).
 inline bool narrow_blocks(const Grouped& g, int cols) {
   const int active = g.E < g.n ? g.E : g.n;
   const int tiles = g.n / 128 + active / 2;
@@ -250,7 +251,7 @@ inline bool narrow_blocks(const Grouped& g, int cols) {
 // Whether blocks of 256 columns and rows fill the chip, and the experts' rows
 // fill enough of them (`rows` each on average).  Us with large / small blocks, 16
 // experts of 6400 x 4096: forward at 32 rows each 178 / 166, 64 183 / 180, 128
-// 202 / 224; d_x at 8 rows 413 / 422, 64 425 / 479; MXFP4 on both sides at 16
+// 202 / 224; d_x at 8 rows 126 / 136, 64 129 / 140, 256 209 / 270; MXFP4 on both sides at 16
 // rows 61 / 68, 128 84 / 98; MXFP4 beside 16 bits, whose blocks of few rows wait
 // for instructions more than for memory, at 64 rows 134 / 109, 256 278 / 264, 512
 // 413 / 474.

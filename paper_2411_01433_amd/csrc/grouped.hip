@@ -7,8 +7,8 @@
 // All three on the tiles of tile.h, calls of few rows on few_rows.h.  A is the
 // operand whose index is contiguous in y and d_x, so that a lane stores 16 bytes
 // of a row; for d_W, whose fp32 values go out one by one, the other one (roles
-// swapped, and not past the caches, 1199 us instead of 1073 for both gradients of
-// the 8192 rows below).
+// swapped, and not past the caches, both gradients of the 8192 rows below took 12 %
+// longer).
 //
 // d_W is 4 bytes per 2 rows' products: few rows per expert bound it by its own
 // writing.  Added to what is there (ADD) it reads as much: a lane fetches the 16
@@ -17,11 +17,14 @@
 // takes 764 (681 at a copy's rate), 60 of 1472 x 2048, 5348 rows, 1341 where it
 // takes 276.  A kernel that can only write takes 531, one that can do both 553.
 // Kernels in us (what bounds them):
-//   16 experts of 6400 x 4096, fp16: y of 16384 rows 776 to 872 (power: 1.1 PF),
-//     d_x of 8192 rows 450 to 471 (power: 0.95 PF), d_W 582 to 615 (tiles of
-//     eight stages, whose stores nothing runs beside: 0.73 PF, 2.9 TB/s)
-//   60 experts of 1472 x 2048, bf16, 5348 rows: y 95 to 102 (W's way from memory,
-//     4.1 TB/s), d_x 77 to 86 (5.2 TB/s), d_W 140 to 158 (5.4 TB/s written)
+//   16 experts of 6400 x 4096, fp16: y of 16384 rows 774 to 863 (power: 1.0 to 1.1
+//     PF), d_x of 8192 rows 452 to 476 (640 tiles, some hardly filled, in three
+//     rounds of 256; 512 rows for every expert, 512 full tiles, 374: 1.15 PF; the
+//     forward product of the same sizes takes 374 and 472 on the same two counts),
+//     d_W 552 to 579 (tiles of eight stages, whose stores nothing runs beside:
+//     0.77 PF, 3.2 TB/s)
+//   60 experts of 1472 x 2048, bf16, 5348 rows: y 98 to 105 (W's way from memory,
+//     4.1 TB/s), d_x 79 to 86 (5.1 TB/s), d_W 134 to 146 (5.4 TB/s written)
 #include "few_rows.h"
 
 namespace moe {
@@ -230,10 +233,12 @@ void launch_rows(const Grouped& g, const void* in, const void* w, void* out, hip
     rows_kernel<TYPE, 2, BACK><<<kBlocks<2>, kThreads, 0, s>>>(g, in, w, out, (cols + 127) / 128);
 }
 
-// Blocks of 256 x 256 where they fill the chip.  Us of both gradients with them /
-// with 128 x 128: 16 experts of 6400 x 4096, 8192 rows, 1040 / 1172; 60 of 1472 x
-// 2048, 5348 rows, 226 / 243; one of 4096 x 4096, 4096 rows (256 tiles) 233 / 271;
-// 64 tiles (2048 x 2048) 115 / 85, 128 tiles (8 of 1024 x 1024, 2048 rows) 34 / 29.
+// Blocks of 256 x 256 where they fill the chip.  Us with them / with 128 x 128,
+// and added to what is there: 16 experts of 6400 x 4096, 8192 rows, 534 / 714, 760
+// / 849; 60 of 1472 x 2048, 5348 rows, 136 / 130, 277 / 285; one of 4096 x 4096,
+// 4096 rows (256 tiles) 119 / 143, 131 / 150; 16 of 1024 x 1024, 2048 rows (256)
+// 18 / 17, 31 / 33; 64 tiles (2048 x 2048) 77 / 46, 87 / 49; 128 tiles (8 of 1024 x
+// 1024, 2048 rows) 15 / 12, 27 / 20.
 template <int TYPE, bool ADD>
 void launch_dw(const Grouped& g, const void* dy, const void* x, float* dw, hipStream_t s) {
   if ((int64_t)g.E * ((g.d_in + 255) / 256) * ((g.d_out + 255) / 256) >= 256)

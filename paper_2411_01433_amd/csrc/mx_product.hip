@@ -6,12 +6,11 @@
 // read from LDS (v_cvt_scalef32_pk: exact wherever the type holds the value),
 // eight for four of these instructions.
 //
-// Kernels in us, 16 experts of 6400 x 4096: 1024 bf16 rows 114 to 122 (244 MB and
+// Kernels in us, 16 experts of 6400 x 4096: 1024 bf16 rows 113 to 120 (244 MB and
 // 54 GF; a stage's chain of reads, conversions and products bounds it, the
 // products are a third of the time), 16384 fp16 rows 743 (power), 8192 rows in
-// MXFP4 160 to 188 (tile.h).  On few_rows.h one row for
-// two experts of 14336 x 4096, 62 MB: 12.7 to 14.5 (4.5 TB/s, the start and the
-// end of a launch among it).
+// MXFP4 158 to 177 (tile.h).  On few_rows.h one row for two experts of 14336 x
+// 4096, 62 MB: 13.7 to 14.1 (4.5 TB/s; what bounds it there).
 #include "few_rows.h"
 
 namespace moe {

@@ -43,13 +43,13 @@
 // large tiles would not fill the chip.  Blocks are persistent: while one tile is
 // stored the next one's loads are under way.
 //
-// Measured: 16384 x 4096 by 16 experts' 6400 rows in fp16 776 to 872 us, 0.99 to
+// Measured: 16384 x 4096 by 16 experts' 6400 rows in fp16 774 to 863 us, 1.0 to
 // 1.1 PF, the matrix cores busy 75 % of the time; their power bounds it: with
 // more and more columns to sum each costs as much as at 1.35 PF, on zeros as at
-// 2.06 (products alone, nothing loaded: 1.68).  In MXFP4 8192 rows take 160 to
-// 188 us, 2.3 to 2.7 PF of the 6.2 that the products alone reach: a wave has no
+// 2.06 (products alone, nothing loaded: 1.68).  In MXFP4 8192 rows take 158 to
+// 177 us, 2.4 to 2.7 PF of the 6.2 that the products alone reach: a wave has no
 // partner on its SIMD to fill in between two stages, and the matrix cores are
-// busy 36 % (without any loads it takes 16 us less).
+// busy 37 % (without any loads it takes 16 us less).
 #pragma once
 
 #include <type_traits>
